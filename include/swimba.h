@@ -19,7 +19,8 @@
  *     row-major with the last index contiguous and must be 16-byte aligned.
  *   - The caller owns every tensor and the workspace; the library owns only the handle (a few
  *     bytes of device memory for a status word).  Nothing is allocated or freed after create.
- *   - Workspaces: swimba_workspace_bytes, _ssd_slots_, _block_, _backward_, _shard_ and
+ *   - Workspaces: swimba_workspace_bytes, _ssd_slots_, _block_, _backward_, _shard_, _linear_attention_,
+ *     _linear_attention_backward_ and
  *     _host_workspace_bytes grow with B and with L, _decode_workspace_bytes with B, so a buffer sized for
  *     a handle's largest call serves its smaller ones.  _packed_workspace_bytes is asked for every batch.
  *   - States may be updated in place: h_final may be h0 itself (forward, packed, slots, block, ssd, and
@@ -327,12 +328,95 @@ int swimba_forward_host(swimba_handle *h, const swimba_weights *w, const void *u
 int swimba_route_mix_static(swimba_handle *h, const swimba_weights *w, const void *u, int64_t T,
                             void *BC, int32_t *topk_idx, float *topk_w, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators beside the mixer: a layer whose recurrence is linear attention with a decay for each
+ * head in place of the selective SSM (Background, "Mamba-2 and SSD": both are the same linear
+ * recurrence; here every head has a transition that is constant over time, and queries, keys and
+ * values are arguments with gradients), the norm that follows it, and the loss that keeps a trained
+ * router balanced.  They use the handle's sizes, dtype, device and status word.
+ *
+ * Linear attention.  Head h of H = n_heads reads group g = h / (H/G) of the queries and keys, N =
+ * d_state entries each, and has values of P = head_dim entries:
+ *   S_t = lambda_h S_{t-1} + v_t k_t^T  [P,N],   o_t = scale S_t q_t,   lambda_h = exp(log_decay[h])
+ *   log_decay [H] float  0 or negative (0: no decay; minus infinity: nothing is kept); a constant of the
+ *                        differentiation, as slopes fixed per head are
+ *   q, k  [B,L,G,N] dtype, v [B,L,H,P] dtype: the row of token t of sequence b starts ld (ldq, ldk, ldv)
+ *         times b*L + t elements behind the pointer, so that they may be columns of a wider matrix (the
+ *         mixed streams BC [T,S] of swimba_route_mix: k = BC, q = BC + G*N, ldk = ldq = S); ld is at least
+ *         the row and a multiple of 16 bytes
+ *   state_in [B,H,P,N] float or NULL (zeros), state_out [B,H,P,N] float or NULL: the state behind the last
+ *         token, the layout of the mixer's states; state_out may be state_in itself
+ *   o     [B,L,H,P] dtype
+ * With state_in / state_out a prompt can be worked in pieces (chunked prefill) and then by steps.  A token
+ * is seen by no token before it and by no other sequence, whatever its bits.  head_dim % 8 == 0; B <= 65535;
+ * B == 0 or L == 0 is a no-op.  Sums and states are fp32. */
+size_t swimba_linear_attention_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L);
+int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void *q, int64_t ldq, const void *k,
+                            int64_t ldk, const void *v, int64_t ldv, const float *state_in, int32_t B, int32_t L,
+                            float scale, void *o, float *state_out, void *workspace, size_t workspace_bytes,
+                            void *cuda_stream);
+
+/* Its gradients: given d_o [B,L,H,P] dtype, the gradient of a scalar loss with respect to o, and d_state_out
+ * [B,H,P,N] float (NULL: zeros) that with respect to the final state, writes
+ *   dq, dk [B,L,G,N] dtype (summed over the heads of a group, in fp32 and in the order of the heads),
+ *   dv [B,L,H,P] dtype, d_state_in [B,H,P,N] float (may be NULL; may be d_state_out itself)
+ * all contiguous and overwritten.  Other arguments as above.  Results are the same bits from call to call. */
+size_t swimba_linear_attention_backward_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L);
+int swimba_linear_attention_backward(swimba_handle *h, const float *log_decay, const void *q, int64_t ldq,
+                                     const void *k, int64_t ldk, const void *v, int64_t ldv, const float *state_in,
+                                     const void *d_o, const float *d_state_out, int32_t B, int32_t L, float scale,
+                                     void *dq, void *dk, void *dv, float *d_state_in, void *workspace,
+                                     size_t workspace_bytes, void *cuda_stream);
+
+/* One token for each of B running sequences: q, k [B,G,N], v [B,H,P] (rows ldq, ldk, ldv elements apart),
+ * o [B,H,P] dtype; state_in and state_out [B,H,P,N] float, required, and may be the same. */
+int swimba_linear_attention_step(swimba_handle *h, const float *log_decay, const void *q, int64_t ldq, const void *k,
+                                 int64_t ldk, const void *v, int64_t ldv, const float *state_in, int32_t B, float scale,
+                                 void *o, float *state_out, void *cuda_stream);
+
+/* Layer norm over each of `groups` equal channel groups of `width` entries of a row (groups = H, width = P:
+ * the norm of every head behind linear attention, whose rows carry no denominator; groups = 1: the norm in
+ * front of a layer):  y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(variance + eps).
+ *   x [rows, groups*width] dtype, rows ldx elements apart; weight, bias [groups*width] float or NULL (1, 0);
+ *   y [rows, groups*width] dtype; mean, rstd [rows, groups] float, may be NULL (the backward pass wants them).
+ * width % 8 == 0, up to 16384.  rows == 0 is a no-op. */
+int swimba_layer_norm(swimba_handle *h, const void *x, int64_t ldx, const float *weight, const float *bias, int64_t rows,
+                      int32_t groups, int32_t width, float eps, void *y, float *mean, float *rstd, void *cuda_stream);
+
+/* Its gradients: dy [rows, groups*width] dtype -> dx (same), dweight, dbias [groups*width] float (overwritten, each
+ * may be NULL; sums over rows in an order that depends on the sizes alone).  The workspace is used for dweight and
+ * dbias only (swimba_layer_norm_workspace_bytes; asked for every size).  rows == 0 clears dweight and dbias. */
+size_t swimba_layer_norm_workspace_bytes(const swimba_handle *h, int64_t rows, int32_t groups, int32_t width);
+int swimba_layer_norm_backward(swimba_handle *h, const void *dy, const void *x, int64_t ldx, const float *weight,
+                               const float *mean, const float *rstd, int64_t rows, int32_t groups, int32_t width,
+                               void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                               void *cuda_stream);
+
+/* Balance loss of the router over T tokens, with per-expert counts and gradients:
+ *   p_t = softmax(W_router u_t),  f_e = counts_e / (k Tv),  m_e = mean of p_te over the Tv valid tokens
+ *   loss = coef E sum_e f_e m_e      (coef when all experts get the same share; 0 when no token is valid)
+ *   u        [T,F] dtype
+ *   topk_idx [T,k] int32   the active sets that the forward (or swimba_backward_weights) returned; an entry
+ *                          outside 0..E-1 is not counted (with SWIMBA_FLAG_CHECK_INDICES it is recorded)
+ *   valid    [T] uint8 or NULL: tokens with 0 (padding) are left out, whatever their features hold; no alignment
+ *   loss [1] float, counts [E] int32, mean_prob [E] float   out (the last two may be NULL)
+ *   dW_router [E,F] float  out, may be NULL: the loss's gradient; with accumulate != 0 it is added to what is
+ *                          there (the gradient that swimba_backward_weights left)
+ *   du       [T,F] dtype   out, may be NULL: overwritten, zero for padded tokens
+ * The shares f_e are constants of the differentiation.  coef carries any factor on the loss.  T * k < 2^31; T == 0 is a
+ * no-op.  Only w->W_router is read.  Results are the same bits from call to call. */
+size_t swimba_balance_loss_workspace_bytes(const swimba_handle *h, int64_t T);
+int swimba_balance_loss(swimba_handle *h, const swimba_weights *w, const void *u, const int32_t *topk_idx,
+                        const uint8_t *valid, int64_t T, float coef, float *loss, int32_t *counts, float *mean_prob,
+                        float *dW_router, int32_t accumulate, void *du, void *workspace, size_t workspace_bytes,
+                        void *cuda_stream);
+
 /* Optional per-kernel timing (no counterpart in the paper; measurement aid).  While enabled,
  * every kernel a call enqueues is bracketed by CUDA events on the call's stream.
  * swimba_profile_read synchronises that stream and returns how many kernels the most recent call
- * (for swimba_forward_host: its last batch slice) launched (at most max_entries), with kernel_ids[i] in 1..24 (1 router + grouping by
+ * (for swimba_forward_host: its last batch slice) launched (at most max_entries), with kernel_ids[i] in 1..37 (1 router + grouping by
  * expert (for fewer than about 28000 tokens the launch also computes the SSD step sizes), 4 expert GEMM, 5 slot mix, 6 SIMT projection, 7 fp32 chunked SSM and packed decode tokens, 8 decode update, 9 SSD
- * tile kernel, 10 segment scan, 11 SSD step sizes and decays, 12 slot stream assembly, 13 slot sum, 14 small-batch projection (short forwards too), 15 convolution + SiLU, 16 gated norm, 17 step-size columns, 18 adjoint recurrence pass, 19 clearing of a gradient call's outputs, 20 weight / logit adjoints, 21 router-matrix gradient, 22 expert-matrix gradient, 23 states at the tile boundaries for the adjoint, 24 state-only SSD pass; 2 and 3 are not in use) and ms[i] its duration in milliseconds.
+ * tile kernel, 10 segment scan, 11 SSD step sizes and decays, 12 slot stream assembly, 13 slot sum, 14 small-batch projection (short forwards too), 15 convolution + SiLU, 16 gated norm, 17 step-size columns, 18 adjoint recurrence pass, 19 clearing of a gradient call's outputs, 20 weight / logit adjoints, 21 router-matrix gradient, 22 expert-matrix gradient, 23 states at the tile boundaries for the adjoint, 24 state-only SSD pass, 25 linear attention token by token, 26 its segment states, 27 their chain, 28 linear attention by tiles, 29 sum over shared heads, 30 linear attention step, 31 layer norm, 32 its gradients, 33 sums of its weight gradients, 34 counts of the balance loss, 35 its pass over the tokens, 36 its router-matrix gradient, 37 its sums; 2 and 3 are not in use) and ms[i] its duration in milliseconds.
  * Both arrays are HOST arrays. */
 int swimba_profile(swimba_handle *h, int enable);
 int swimba_profile_read(swimba_handle *h, int32_t *kernel_ids, float *ms, int32_t max_entries);

@@ -36,6 +36,10 @@ EXPORTS = [
     "swimba_route_project_slots", "swimba_ssd_slots_workspace_bytes", "swimba_ssd_slots",
     "swimba_block_workspace_bytes", "swimba_block_forward",
     "swimba_decode_workspace_bytes", "swimba_decode_step", "swimba_host_workspace_bytes",
+    "swimba_linear_attention_workspace_bytes", "swimba_linear_attention",
+    "swimba_linear_attention_backward_workspace_bytes", "swimba_linear_attention_backward",
+    "swimba_linear_attention_step", "swimba_layer_norm", "swimba_layer_norm_workspace_bytes",
+    "swimba_layer_norm_backward", "swimba_balance_loss_workspace_bytes", "swimba_balance_loss",
     "swimba_forward_host", "swimba_route_mix_static", "swimba_profile", "swimba_profile_read",
     "swimba_selftest_wait", "swimba_last_launch_count", "swimba_status", "swimba_last_error",
     "swimba_destroy",
@@ -136,6 +140,28 @@ def lib() -> ctypes.CDLL:
         L.swimba_route_mix_static.argtypes = [vp, ctypes.POINTER(swimba_weights), vp, i64, vp, vp, vp,
                                               vp]
         L.swimba_route_mix_static.restype = ctypes.c_int
+        f32 = ctypes.c_float
+        for name in ("swimba_linear_attention_workspace_bytes", "swimba_linear_attention_backward_workspace_bytes"):
+            getattr(L, name).argtypes = [vp, i32, i32]
+            getattr(L, name).restype = sz
+        L.swimba_linear_attention.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.swimba_linear_attention.restype = ctypes.c_int
+        L.swimba_linear_attention_backward.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i32, i32, f32,
+                                                       vp, vp, vp, vp, vp, sz, vp]
+        L.swimba_linear_attention_backward.restype = ctypes.c_int
+        L.swimba_linear_attention_step.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i32, f32, vp, vp, vp]
+        L.swimba_linear_attention_step.restype = ctypes.c_int
+        L.swimba_layer_norm.argtypes = [vp, vp, i64, vp, vp, i64, i32, i32, f32, vp, vp, vp, vp]
+        L.swimba_layer_norm.restype = ctypes.c_int
+        L.swimba_layer_norm_workspace_bytes.argtypes = [vp, i64, i32, i32]
+        L.swimba_layer_norm_workspace_bytes.restype = sz
+        L.swimba_layer_norm_backward.argtypes = [vp, vp, vp, i64, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.swimba_layer_norm_backward.restype = ctypes.c_int
+        L.swimba_balance_loss_workspace_bytes.argtypes = [vp, i64]
+        L.swimba_balance_loss_workspace_bytes.restype = sz
+        L.swimba_balance_loss.argtypes = [vp, ctypes.POINTER(swimba_weights), vp, vp, vp, i64, f32, vp, vp, vp, vp, i32,
+                                          vp, vp, sz, vp]
+        L.swimba_balance_loss.restype = ctypes.c_int
         L.swimba_profile.argtypes = [vp, ctypes.c_int]
         L.swimba_profile.restype = ctypes.c_int
         L.swimba_profile_read.argtypes = [vp, vp, vp, i32]
@@ -416,12 +442,110 @@ def swimba_forward_host(h: Handle, w: swimba_weights, u_host, x_host, dt_host, B
     return rc
 
 
+def _rows(t: torch.Tensor, B: int, L: int):
+    """(address, elements from token to token) of [B, L, heads, entries]: the heads of a token side by side, tokens
+    evenly apart (a column range of a wider matrix will do).  [B, heads, entries] counts as one token each."""
+    if t.dim() == 3:
+        t = t.unsqueeze(1)
+    assert t.dim() == 4 and t.shape[0] == B and t.shape[1] == L, "rows must be [B, L, heads, entries]"
+    n, m = t.shape[2], t.shape[3]
+    assert (m == 1 or t.stride(3) == 1) and (n == 1 or t.stride(2) == m), "the heads of a token must lie side by side"
+    ld = t.stride(1) if L > 1 else t.stride(0) if B > 1 else n * m
+    assert B == 1 or t.stride(0) == L * ld, "tokens must be evenly apart"
+    return t.data_ptr(), ld
+
+
+def swimba_linear_attention_workspace_bytes(h: Handle, B: int, L: int) -> int:
+    return int(lib().swimba_linear_attention_workspace_bytes(h.ptr, B, L))
+
+
+def swimba_linear_attention(h: Handle, log_decay, q, k, v, state_in, B: int, L: int, scale: float, o, state_out,
+                            workspace, stream=None, check: bool = True) -> int:
+    wp, wb = _ws(workspace)
+    rc = lib().swimba_linear_attention(h.ptr, _ptr(log_decay), *_rows(q, B, L), *_rows(k, B, L), *_rows(v, B, L),
+                                       _ptr(state_in), B, L, scale, _ptr(o), _ptr(state_out), wp, wb, _stream(stream))
+    if check and rc != OK:
+        h._raise(rc)
+    return rc
+
+
+def swimba_linear_attention_backward_workspace_bytes(h: Handle, B: int, L: int) -> int:
+    return int(lib().swimba_linear_attention_backward_workspace_bytes(h.ptr, B, L))
+
+
+def swimba_linear_attention_backward(h: Handle, log_decay, q, k, v, state_in, d_o, d_state_out, B: int, L: int,
+                                     scale: float, dq, dk, dv, d_state_in, workspace, stream=None,
+                                     check: bool = True) -> int:
+    wp, wb = _ws(workspace)
+    rc = lib().swimba_linear_attention_backward(h.ptr, _ptr(log_decay), *_rows(q, B, L), *_rows(k, B, L),
+                                                *_rows(v, B, L), _ptr(state_in), _ptr(d_o), _ptr(d_state_out), B, L,
+                                                scale, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_state_in), wp, wb,
+                                                _stream(stream))
+    if check and rc != OK:
+        h._raise(rc)
+    return rc
+
+
+def swimba_linear_attention_step(h: Handle, log_decay, q, k, v, state_in, B: int, scale: float, o, state_out,
+                                 stream=None, check: bool = True) -> int:
+    rc = lib().swimba_linear_attention_step(h.ptr, _ptr(log_decay), *_rows(q, B, 1), *_rows(k, B, 1), *_rows(v, B, 1),
+                                            _ptr(state_in), B, scale, _ptr(o), _ptr(state_out), _stream(stream))
+    if check and rc != OK:
+        h._raise(rc)
+    return rc
+
+
+def swimba_layer_norm(h: Handle, x, weight, bias, rows: int, groups: int, width: int, eps: float, y, mean, rstd,
+                      stream=None, check: bool = True) -> int:
+    """x [rows, groups * width]; its rows may lie apart."""
+    assert x.dim() == 2 and (x.shape[1] == 1 or x.stride(1) == 1), "x must be rows of contiguous entries"
+    ldx = x.stride(0) if rows > 1 else groups * width
+    rc = lib().swimba_layer_norm(h.ptr, x.data_ptr(), ldx, _ptr(weight), _ptr(bias), rows, groups, width, eps, _ptr(y),
+                                 _ptr(mean), _ptr(rstd), _stream(stream))
+    if check and rc != OK:
+        h._raise(rc)
+    return rc
+
+
+def swimba_layer_norm_workspace_bytes(h: Handle, rows: int, groups: int, width: int) -> int:
+    return int(lib().swimba_layer_norm_workspace_bytes(h.ptr, rows, groups, width))
+
+
+def swimba_layer_norm_backward(h: Handle, dy, x, weight, mean, rstd, rows: int, groups: int, width: int, dx, dweight,
+                               dbias, workspace, stream=None, check: bool = True) -> int:
+    assert x.dim() == 2 and (x.shape[1] == 1 or x.stride(1) == 1), "x must be rows of contiguous entries"
+    ldx = x.stride(0) if rows > 1 else groups * width
+    wp, wb = _ws(workspace)
+    rc = lib().swimba_layer_norm_backward(h.ptr, _ptr(dy), x.data_ptr(), ldx, _ptr(weight), _ptr(mean), _ptr(rstd), rows,
+                                          groups, width, _ptr(dx), _ptr(dweight), _ptr(dbias), wp, wb, _stream(stream))
+    if check and rc != OK:
+        h._raise(rc)
+    return rc
+
+
+def swimba_balance_loss_workspace_bytes(h: Handle, T: int) -> int:
+    return int(lib().swimba_balance_loss_workspace_bytes(h.ptr, T))
+
+
+def swimba_balance_loss(h: Handle, w: swimba_weights, u, topk_idx, valid, T: int, coef: float, loss, counts, mean_prob,
+                        dW_router, du, workspace, accumulate: bool = False, stream=None, check: bool = True) -> int:
+    wp, wb = _ws(workspace)
+    rc = lib().swimba_balance_loss(h.ptr, ctypes.byref(w), _ptr(u), _ptr(topk_idx), _ptr(valid), T, coef, _ptr(loss),
+                                   _ptr(counts), _ptr(mean_prob), _ptr(dW_router), 1 if accumulate else 0, _ptr(du), wp,
+                                   wb, _stream(stream))
+    if check and rc != OK:
+        h._raise(rc)
+    return rc
+
+
 KERNEL_NAMES = {1: "router_topk", 4: "expert_gemm",
                 5: "mix_slots", 6: "project_mix_simt", 7: "ssd_sequential", 8: "decode_update",
                 9: "ssd_tiles", 10: "segment_scan", 11: "ssd_scalars", 12: "slot_streams",
                 13: "slot_sum", 14: "project_small", 15: "conv_silu", 16: "gated_rmsnorm",
                 17: "dt_columns", 18: "ssd_adjoint", 19: "clear", 20: "dpi_dg", 21: "dw_router",
-                22: "dw_expert", 23: "adjoint_states", 24: "ssd_state"}
+                22: "dw_expert", 23: "adjoint_states", 24: "ssd_state", 25: "la_steps", 26: "la_states", 27: "la_chain", 28: "la_tiles", 29: "la_head_sum",
+                30: "la_step", 31: "layer_norm", 32: "layer_norm_backward", 33: "layer_norm_sum", 34: "balance_count",
+                35: "balance_tokens", 36: "balance_dw", 37: "balance_sum"}
 
 
 def swimba_profile(h: Handle, enable: bool) -> None:

@@ -4,38 +4,9 @@
 #include <cstring>
 #include <new>
 
-#include "internal.h"
-#include "tc05.cuh"
-
-using namespace swimba;
-
-struct swimba_handle {
-    swimba_config cfg;
-    int device;
-    int sm_count;
-    int *d_status;          // device status word
-    cudaStream_t last_stream;
-    int last_launches;
-    Profiler prof;
-    TmapCache tmaps;        // tensor maps encoded so far (same buffers call after call: encoded once)
-    // host-buffer entry point: copy streams and events of its batch-slice pipeline
-    cudaStream_t s_in, s_out;
-    cudaEvent_t ev_start, ev_out, ev_in[32], ev_done[32];
-    char err[256];
-};
+#include "handle.h"
 
 namespace {
-
-constexpr size_t kAlign = 256;
-inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline size_t elt_size(int dtype) { return dtype == SWIMBA_DTYPE_FP32 ? 4 : 2; }
-
-int fail(swimba_handle *h, int code, const char *msg)
-{
-    if (h) snprintf(h->err, sizeof(h->err), "%s", msg);
-    return code;
-}
 
 // Workspace of the forward: [BC | idx | w], each 256-byte aligned.
 struct FwdLayout {
@@ -170,14 +141,6 @@ void destroy_host_pipeline(swimba_handle *h)
         if (h->ev_in[i]) cudaEventDestroy(h->ev_in[i]);
         if (h->ev_done[i]) cudaEventDestroy(h->ev_done[i]);
     }
-}
-
-int set_device(swimba_handle *h)
-{
-    int cur = -1;
-    if (cudaGetDevice(&cur) != cudaSuccess) return fail(h, SWIMBA_ERR_CUDA, "cudaGetDevice failed");
-    if (cur != h->device) return fail(h, SWIMBA_ERR_CUDA, "handle used on a different device than it was created on");
-    return SWIMBA_OK;
 }
 
 // Router + projection + mix into BC (dtype, or fp32 when bc_fp32).  scalars != NULL: the SSD step

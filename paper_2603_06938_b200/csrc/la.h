@@ -1,0 +1,76 @@
+// Linear attention with a decay for each head: the jobs its kernels work.
+//
+// One job is the map  (q, k, v, entry state) -> (o, exit state)  of
+//   forward in time   S_t = lambda S_{t-1} + a k_t v_t^T,          o_t = p-part + c-part = S_t^T q_t
+//   backward in time  R_t = lambda R_{t+1} + a k_t v_t^T,  with the entry state already at the last token
+//                     (R_L = E + a k_L v_L^T) and the exit state lambda R_1 in front of the first
+// with DK = entries of q and k, DV = entries of v and o, both of which a gradient call sets as it needs:
+//   forward    q, k, v -> o                    scores and carried part times scale, a = 1
+//   d query    q := do, k := v, v := k         the same with the state transposed
+//   d key      q := v, k := do, v := q         backward in time, entered by the final state's gradient,
+//   d value    q := k, k := q,  v := do        whose products do q^T carry the scale (a = scale), not the read
+#pragma once
+#include "internal.h"
+
+namespace swimba {
+
+struct LaJob {
+    const void *q, *k, *v;       // rows of token t of sequence b start at ((b L + t) ld)
+    int64_t ldq, ldk, ldv;       // elements from token to token
+    int rq, rk, rv;              // head h reads stream h / r
+    int dk, dv;
+    int reverse;                 // 1: backward in time
+    int transposed;              // states lie as [DK][DV] (0: as [DV][DK])
+    const float *s_in;           // [B, H, DV, DK] (or transposed); NULL: zeros
+    float *s_out;                // may be NULL
+    void *o;                     // [B, L, H, DV], rows ldo apart
+    int64_t ldo;
+    int o_f32;                   // o is float whatever the dtype
+    float scale_p, scale_c, scale_a;   // of the scores inside a tile, of the carried state's part, of what the state adds
+    float *seg;                  // [B, H, nseg] states in the layout of s_in, when sequences are cut
+};
+
+constexpr int LA_MAX_JOBS = 3;
+struct LaArgs {
+    LaJob job[LA_MAX_JOBS];
+    int njobs;
+    const float *log_decay;      // [H]
+    int B, L, H;
+    int seg_len, nseg;           // tokens per segment (the last may be shorter), segments per sequence
+};
+
+// log2 of the decay.  Held above -1e4, where one step underflows to nothing already, so that the zeroth
+// power of a decay of exp(-infinity) is 1 and not a NaN.
+__device__ __forceinline__ float la_log2_decay(float g)
+{
+    const float g2 = g * 1.4426950408889634f;
+    return g2 < -1.0e4f ? -1.0e4f : g2;
+}
+
+// Segments the kernels cut every sequence of a call into, and the bytes they keep for that.
+void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg);
+// (bytes of one job's segment states; grows with B and with L)
+size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count);
+// Runs the jobs: per-segment states, their chain, outputs; or outputs alone when nseg == 1.
+int launch_la(LaunchCtx &ctx, int dtype, LaArgs &a, int sm_count);
+// out[t, g, :] = sum over the r heads of group g of part[t, g r + i, :], in that order.
+int launch_la_head_sum(LaunchCtx &ctx, int dtype, const float *part, int64_t T, int G, int r, int N, void *out);
+int launch_la_step(LaunchCtx &ctx, int dtype, const float *log_decay, const void *q, int64_t ldq, const void *k,
+                   int64_t ldk, const void *v, int64_t ldv, const float *s_in, int B, int H, int G, int P, int N,
+                   float scale, int sm_count, void *o, float *s_out);
+
+// Layer norm over each of `groups` equal channel groups of a row (every group: width entries).
+int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
+                      int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd);
+size_t layer_norm_partial_bytes(int64_t rows, int groups, int width, int sm_count);
+int launch_layer_norm_backward(LaunchCtx &ctx, int dtype, const void *dy, const void *x, int64_t ldx, const float *w,
+                               const float *mean, const float *rstd, int64_t rows, int groups, int width, int sm_count,
+                               void *dx, float *dw, float *db, float *partial);
+
+// Balance loss of a router (see swimba_balance_loss).
+size_t balance_workspace_bytes(int dtype, int64_t T, int F, int E, int sm_count);
+int launch_balance(LaunchCtx &ctx, int dtype, const void *u, const void *W, const int32_t *idx, const uint8_t *valid,
+                   int64_t T, int F, int E, int k, float coef, int sm_count, float *loss, int32_t *counts,
+                   float *mean_prob, float *dW, bool add, void *du, void *workspace);
+
+}  // namespace swimba
