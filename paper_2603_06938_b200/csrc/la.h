@@ -36,7 +36,7 @@ struct LaArgs {
     int njobs;
     const float *log_decay;      // [H]
     int B, L, H;
-    int seg_len, nseg;           // tokens per segment (the last may be shorter), segments per sequence
+    int seg_len, nseg;           // tokens per segment (the last in the sequence may be shorter), segments per sequence
 };
 
 // log2 of the decay.  Held above -1e4, where one step underflows to nothing already, so that the zeroth
@@ -47,12 +47,28 @@ __device__ __forceinline__ float la_log2_decay(float g)
     return g2 < -1.0e4f ? -1.0e4f : g2;
 }
 
+// The decay as a sum of two floats: multiplied up over the tokens of a slow head's memory, the rounding of one would be the
+// largest error there is (256 tokens: 3e-6).
+struct LaDecay {
+    float hi, lo;
+};
+__device__ __forceinline__ LaDecay la_decay(float g)
+{
+    const double l = exp2((double)la_log2_decay(g));
+    return LaDecay{(float)l, (float)(l - (double)(float)l)};
+}
+
 // Segments the kernels cut every sequence of a call into, and the bytes they keep for that.
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg);
 // (bytes of one job's segment states; grows with B and with L)
 size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count);
+// The tensor-core kernel (la_tiles.cu): the head sizes it has, whether the rows are within its reach, its launches
+// (states: the pass that leaves every segment's end state).
+bool la_tiles_shape(int dtype, int N, int P);
+bool la_tiles_reach(const LaArgs &a);
+int launch_la_tiles(LaunchCtx &ctx, const LaArgs &a, bool states);
 // Runs the jobs: per-segment states, their chain, outputs; or outputs alone when nseg == 1.
-int launch_la(LaunchCtx &ctx, int dtype, LaArgs &a, int sm_count);
+int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a);
 // out[t, g, :] = sum over the r heads of group g of part[t, g r + i, :], in that order.
 int launch_la_head_sum(LaunchCtx &ctx, int dtype, const float *part, int64_t T, int G, int r, int N, void *out);
 int launch_la_step(LaunchCtx &ctx, int dtype, const float *log_decay, const void *q, int64_t ldq, const void *k,

@@ -1,0 +1,566 @@
+// Linear attention with a decay for each head on the tensor cores (bf16; 64 or 128 entries of keys and of values):
+// tiles of 128 tokens, the carried state on chip.  What a job is: la.h.  Per tile, with n tokens, r the place of a
+// token in the order of the walk, and the state S [DK, DV] entering it:
+//   QK   A = Q K^T                                            scores
+//        P_ij = scale_p lambda^|i-j| A_ij  for tokens j that i sees, else 0
+//   PV   O1 = P V,   QS  O2 = Q S,   o_i = O1_i + scale_c lambda^(r_i + first) O2_i
+//   KV   D = K^T (w V),  w_j = scale_a lambda^(n - r_j - first),   S <- lambda^n S + D
+// (first = 1 walking forward, 0 backward, where the decay follows the read of a token).
+//
+// Precision.  Sums are fp32 in tensor memory, the state stays fp32 in registers.  P and the state's copy for QS are
+// rounded to bf16 (a term of o, which is bf16 itself, passes one of the two).  w V is not: it goes into the state, an
+// fp32 result, and is taken as the sum of three bf16 parts (2^-24 of it), one product each.
+//
+// A token's bits reach nobody in front of it: scores are masked by selection, and entries of V that are infinite or NaN,
+// which a zero of P would turn into NaN, are zeros in PV; the epilogue adds them to the rows that see them.
+#include <algorithm>
+#include <cstddef>
+
+#include "la.h"
+#include "tc05.cuh"
+
+namespace swimba {
+
+namespace {
+
+constexpr int LT = 128;                      // tokens per tile
+constexpr int LDV = 64;                      // columns of v a CTA works (128 of them: two CTAs)
+constexpr int PARTS = 3;                     // bf16 parts of w V
+constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
+constexpr int THREADS = 512;
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2;
+// tensor memory columns: two score tiles (their masked bf16 form over their first half), O2, O1, two D
+constexpr uint32_t TM_QK = 0, TM_QS = 256, TM_PV = 320, TM_KV = 384, TM_COLS = 512;
+
+template <int DK> struct Sm {
+    static constexpr int NS = DK == 64 ? 3 : 2;           // stages of Q, K and V
+    static constexpr uint32_t QB = DK / 64 * SLAB;        // bytes of a Q or K tile
+    static constexpr uint32_t Q = 0, K = Q + NS * QB, V = K + NS * QB, VW = V + NS * SLAB, S = VW + PARTS * SLAB,
+                              SMALL = S + DK * 128;
+};
+struct Small {
+    uint64_t full_q[3], full_k[3], full_v[3], free_q[3], free_k[3], free_v[3];
+    uint64_t qk_full[2], p_full[2], kv_done[2], qs_done, pv_done, vw_full, s_full, o_free;
+    uint32_t tmem;
+    int abort_flag;
+    int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
+    alignas(16) float pow_col[32];           // factors of a score block's columns
+    float pow_diag[32];                      // lambda^m
+};
+
+static_assert(offsetof(Small, pow_col) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
+
+struct Maps {
+    CUtensorMap q[LA_MAX_JOBS], k[LA_MAX_JOBS], v[LA_MAX_JOBS];
+};
+
+__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b) { return tc::f32x2(__uint_as_float(a), __uint_as_float(b)); }
+
+// STATE_ONLY: from a zero state, and only the end state is kept (in seg).
+template <int DK, bool STATE_ONLY>
+__global__ void __launch_bounds__(THREADS, 1)
+la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs a, int *d_status)
+{
+    typedef Sm<DK> L;
+    constexpr int NS = L::NS;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Small *sm = (Small *)(smem + L::SMALL);
+    int *abort_flag = &sm->abort_flag;
+    if ((tc::smem_u32(smem) & 1023u) != 0) {       // the swizzled tiles need a 1024-byte aligned base
+        if (threadIdx.x == 0) atomicCAS(d_status, 0, SWIMBA_ERR_DEVICE_BOUNDS);
+        return;
+    }
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+
+    // slices of one head side by side, then the jobs on it: they read the same rows at about the same time
+    int64_t id = blockIdx.x;
+    const int slices = a.job[0].dv / LDV;
+    const int c0 = (int)(id % slices) * LDV;
+    id /= slices;
+    const int ji = (int)(id % a.njobs);
+    id /= a.njobs;
+    const int nrun = STATE_ONLY ? a.nseg - 1 : a.nseg;     // (the last segment's end state enters nothing)
+    const int seg = (int)(id % nrun);                      // in the order of the walk
+    id /= nrun;
+    const int h = (int)(id % a.H), b = (int)(id / a.H);
+    const LaJob &j = a.job[ji];
+    const bool rev = j.reverse != 0;
+    const int place = rev ? a.nseg - 1 - seg : seg;
+    const int t_begin = place * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    const int ntiles = (t_end - t_begin + LT - 1) / LT;
+    auto tile_at = [&](int t) { return t_begin + (rev ? ntiles - 1 - t : t) * LT; };       // first token of tile t
+    auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
+
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) {
+            tc::mbar_init(&sm->full_q[s], 1);
+            tc::mbar_init(&sm->full_k[s], 1);
+            tc::mbar_init(&sm->full_v[s], 1);
+            tc::mbar_init(&sm->free_q[s], 1);
+            tc::mbar_init(&sm->free_k[s], 1);
+            tc::mbar_init(&sm->free_v[s], 4);
+        }
+        for (int s = 0; s < 2; ++s) {
+            tc::mbar_init(&sm->qk_full[s], 1);
+            tc::mbar_init(&sm->p_full[s], 4);
+            tc::mbar_init(&sm->kv_done[s], 1);
+            sm->odd_tile[s] = 0;
+        }
+        tc::mbar_init(&sm->qs_done, 1);
+        tc::mbar_init(&sm->pv_done, 1);
+        tc::mbar_init(&sm->vw_full, 4);
+        tc::mbar_init(&sm->s_full, 4);
+        tc::mbar_init(&sm->o_free, 4);
+        *abort_flag = 0;
+        tc::fence_mbar_init();
+    }
+    if (warp == WARP_ALLOC) {
+        tc::tmem_alloc(&sm->tmem, TM_COLS);
+        tc::tmem_relinquish();
+    }
+    if (warp == WARP_TMA && lane == 0) {
+        if (!STATE_ONLY) tc::prefetch_tmap(&maps.q[ji]);
+        tc::prefetch_tmap(&maps.k[ji]);
+        tc::prefetch_tmap(&maps.v[ji]);
+    }
+    grid_dep_launch();
+    grid_dep_wait();
+    const float g2 = la_log2_decay(a.log_decay[h]);
+    if (warp == 3) {
+        sm->pow_diag[lane] = exp2f(lane * g2);
+        sm->pow_col[lane] = exp2f((rev ? lane : 31 - lane) * g2);
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = sm->tmem;
+
+    if (warp == WARP_TMA) {
+        // ------------------------------------------------------------------ loads, in the order in which room comes free
+        const bool leader = tc::elect_one();
+        for (int t = 0; t < ntiles; ++t) {
+            const int s = t % NS, at = tile_at(t);
+            const uint32_t ph = ((t / NS) & 1) ^ 1;
+            auto load = [&](uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int col, int stream) {
+                tc::mbar_wait(room, ph, abort_flag, d_status);
+                if (leader && !*(volatile int *)abort_flag) {
+                    tc::mbar_arrive_expect_tx(full, bytes);
+                    for (uint32_t o = 0; o < bytes; o += SLAB)
+                        tc::tma_load_4d(smem + dst + o, m, full, col + (int)(o / SLAB) * 64, stream, at, b);
+                }
+                __syncwarp();
+            };
+            load(&sm->full_k[s], &sm->free_k[s], L::K + s * L::QB, L::QB, &maps.k[ji], 0, h / j.rk);
+            if (!STATE_ONLY) load(&sm->full_q[s], &sm->free_q[s], L::Q + s * L::QB, L::QB, &maps.q[ji], 0, h / j.rq);
+            load(&sm->full_v[s], &sm->free_v[s], L::V + s * SLAB, SLAB, &maps.v[ji], c0, h / j.rv);
+        }
+        // No copy may be in flight when the CTA leaves: after an abort nobody else has waited for the last ones (those
+        // that were not issued any more never arrive, and these waits run out soon).
+        auto settle = [&](uint64_t *full, uint32_t ph) {
+            int quiet = 0;
+            if (*(volatile int *)abort_flag) tc::mbar_wait(full, ph, &quiet, d_status, 10000000ll);
+            else tc::mbar_wait(full, ph, abort_flag, d_status);
+        };
+        for (int t = max(0, ntiles - NS); t < ntiles; ++t) {
+            settle(&sm->full_k[t % NS], (t / NS) & 1);
+            if (!STATE_ONLY) settle(&sm->full_q[t % NS], (t / NS) & 1);
+            settle(&sm->full_v[t % NS], (t / NS) & 1);
+        }
+    } else if (warp == WARP_MMA) {
+        // ------------------------------------------------------------------ products
+        const bool leader = tc::elect_one();
+        constexpr uint32_t id_qk = tc::idesc_bf16(128, 128, 0, 0);      // Q (K-major) x K (K-major)
+        constexpr uint32_t id_qs = tc::idesc_bf16(128, LDV, 0, 1);      // Q (K-major) x S (MN-major); P (TMEM) x V (MN-major)
+        constexpr uint32_t id_kv = tc::idesc_bf16(128, LDV, 1, 1);      // K (MN-major) x wV (MN-major)
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t base = tc::smem_u32(smem);
+        const uint64_t dQ = tc::smem_desc_sw128(base + L::Q, 16, 1024), dK = tc::smem_desc_sw128(base + L::K, 16, 1024);
+        // (64 keys: both halves of the 128 rows of D are the same 64 keys)
+        const uint64_t dKt = tc::smem_desc_sw128(base + L::K, DK == 128 ? SLAB : 0, 1024);
+        const uint64_t dV = tc::smem_desc_sw128(base + L::V, SLAB, 1024), dW = tc::smem_desc_sw128(base + L::VW, SLAB, 1024);
+        const uint64_t dS = tc::smem_desc_sw128(base + L::S, SLAB, 1024);
+        auto scores = [&](int t) {
+            const int s = t % NS;
+            const uint32_t ph = (t / NS) & 1;
+            tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
+            tc::mbar_wait(&sm->full_q[s], ph, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB));
+                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dK, s * L::QB));
+#pragma unroll
+                for (int kk = 0; kk < DK / 16; ++kk) {
+                    const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
+                    tc::mma_ss(tm + TM_QK + (t & 1) * 128, tc::smem_desc_advance(q, o), tc::smem_desc_advance(k, o), id_qk, kk > 0);
+                }
+                tc::mma_commit(&sm->qk_full[t & 1]);
+            }
+            __syncwarp();
+        };
+        if (!STATE_ONLY && ntiles > 0) scores(0);
+        for (int t = 0; t < ntiles; ++t) {
+            const int s = t % NS;
+            const uint32_t ph = (t / NS) & 1;
+            // KV: the state's additions do not wait for the state
+            if (STATE_ONLY) {
+                tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
+                if (t > 0) tc::mbar_wait(&sm->s_full, (t - 1) & 1, abort_flag, d_status);     // (D of the tile in front has been read)
+            }
+            tc::mbar_wait(&sm->vw_full, t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, s * L::QB));
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    const uint64_t w = tc::smem_desc_fresh(tc::smem_desc_advance(dW, p * SLAB));
+#pragma unroll
+                    for (int kk = 0; kk < LT / 16; ++kk)
+                        tc::mma_ss(tm + TM_KV + (t & 1) * 64, tc::smem_desc_advance(k, kk * 2048),
+                                   tc::smem_desc_advance(w, kk * 2048), id_kv, p > 0 || kk > 0);
+                }
+                tc::mma_commit(&sm->kv_done[t & 1]);
+                tc::mma_commit(&sm->free_k[s]);
+            }
+            __syncwarp();
+            if (STATE_ONLY) continue;
+            // QS: the carried part, once the state is there and the epilogue has read the tile in front
+            tc::mbar_wait(&sm->s_full, t & 1, abort_flag, d_status);
+            if (t > 0) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB));
+                const uint64_t st = tc::smem_desc_fresh(dS);
+#pragma unroll
+                for (int kk = 0; kk < DK / 16; ++kk)
+                    tc::mma_ss(tm + TM_QS, tc::smem_desc_advance(q, (kk >> 2) * SLAB + (kk & 3) * 32),
+                               tc::smem_desc_advance(st, kk * 2048), id_qs, kk > 0);
+                tc::mma_commit(&sm->qs_done);
+                tc::mma_commit(&sm->free_q[s]);
+            }
+            __syncwarp();
+            if (t + 1 < ntiles) scores(t + 1);
+            // PV
+            tc::mbar_wait(&sm->full_v[s], ph, abort_flag, d_status);
+            tc::mbar_wait(&sm->p_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t v = tc::smem_desc_fresh(tc::smem_desc_advance(dV, s * SLAB));
+#pragma unroll
+                for (int kk = 0; kk < LT / 16; ++kk)
+                    tc::mma_ts(tm + TM_PV, tm + TM_QK + (t & 1) * 128 + kk * 8, tc::smem_desc_advance(v, kk * 2048), id_qs, kk > 0);
+                tc::mma_commit(&sm->pv_done);
+            }
+            __syncwarp();
+        }
+    } else if (warp >= 4 && warp < 8) {
+        // ------------------------------------------------------------------ masks: a row of the scores per thread
+        const int q4 = warp & 3, i = q4 * 32 + lane;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16);
+        float rho[4];
+#pragma unroll
+        for (int bl = 0; bl < 4; ++bl)         // the factor of a whole block of 32 tokens; its columns' are in pow_col
+            rho[bl] = rev ? (bl > q4 ? j.scale_p * exp2f((32 * bl - i) * g2) : 0.f)
+                          : (bl < q4 ? j.scale_p * exp2f((i - 32 * bl - 31) * g2) : 0.f);
+        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
+            tc::mbar_wait(&sm->qk_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            const uint32_t region = row + TM_QK + (t & 1) * 128;
+#pragma unroll
+            for (int bl = 0; bl < 4; ++bl) {
+                uint32_t o[16];
+                if (rev ? bl < q4 : bl > q4) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = 0u;
+                    tc::tmem_st16(region + bl * 16, o);
+                    continue;
+                }
+                uint32_t x[32];
+                tc::tmem_ld32(region + bl * 32, x);
+                tc::tmem_ld_wait();
+                if (bl != q4) {
+                    const uint64_t r2 = tc::f32x2(rho[bl], rho[bl]);
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        const float4 c = *reinterpret_cast<const float4 *>(&sm->pow_col[2 * e]);
+                        o[e] = tc::f32x2_bf16(tc::f32x2_mul(pair_of(x[2 * e], x[2 * e + 1]), tc::f32x2_mul(r2, tc::f32x2(c.x, c.y))));
+                        o[e + 1] = tc::f32x2_bf16(tc::f32x2_mul(pair_of(x[2 * e + 2], x[2 * e + 3]), tc::f32x2_mul(r2, tc::f32x2(c.z, c.w))));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int d = rev ? e - lane : lane - e;
+                        const float f = sm->pow_diag[d & 31] * j.scale_p * __uint_as_float(x[e]);
+                        x[e] = d >= 0 ? __float_as_uint(f) : 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = tc::pack_bf16x2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
+                }
+                tc::tmem_st16(region + bl * 16, o);
+            }
+            tc::tmem_st_wait();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->p_full[t & 1]);
+        }
+    } else if (warp >= 8 && warp < 12) {
+        // ------------------------------------------------------------------ w V, and the epilogue of the tile in front
+        const int q4 = warp & 3, r = q4 * 32 + lane, ltid = tid - 256;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16);
+        const uint64_t neg = tc::f32x2(-1.f, -1.f);
+        auto weigh = [&](int t) {
+            const int s = t % NS, n = tile_n(t);
+            tc::mbar_wait(&sm->full_v[s], (t / NS) & 1, abort_flag, d_status);
+            if (t > 0) tc::mbar_wait(&sm->kv_done[(t - 1) & 1], ((t - 1) >> 1) & 1, abort_flag, d_status);
+            uint8_t *src = smem + L::V + s * SLAB, *dst = smem + L::VW;
+            bool any_odd = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int rr = (ltid >> 3) + 16 * i;
+                const uint32_t off = tc::sw128_offset(rr, ltid & 7);
+                const uint4 v = *reinterpret_cast<const uint4 *>(src + off);
+                const int e = rev ? rr + 1 : n - 1 - rr;            // n - r - first
+                const float w = rr < n ? j.scale_a * exp2f(e * g2) : 0.f;
+                const uint64_t w2 = tc::f32x2(w, w);
+                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                uint32_t p[PARTS][4], even[4], odd = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    // (an exponent of all ones: infinity or NaN)
+                    const uint32_t lo = (in[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+                    const uint32_t hi = (in[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                    odd |= lo | hi;
+                    even[k] = in[k] & ~(lo | hi);
+                    uint64_t x = tc::f32x2_mul(w2, pair_of(in[k] << 16, in[k] & 0xffff0000u));
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) {
+                        p[q][k] = tc::f32x2_bf16(x);
+                        if (q + 1 < PARTS) x = tc::f32x2_fma(neg, pair_of(p[q][k] << 16, p[q][k] & 0xffff0000u), x);
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q)
+                    *reinterpret_cast<uint4 *>(dst + q * SLAB + off) = make_uint4(p[q][0], p[q][1], p[q][2], p[q][3]);
+                if (!STATE_ONLY && odd) {
+                    *reinterpret_cast<uint4 *>(src + off) = make_uint4(even[0], even[1], even[2], even[3]);
+                    any_odd = true;
+                }
+            }
+            if (any_odd) ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
+            tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tc::mbar_arrive(&sm->vw_full);
+                if (STATE_ONLY) tc::mbar_arrive(&sm->free_v[s]);
+            }
+            if (!STATE_ONLY) tc::named_bar_sync(1, 128);
+        };
+        auto finish = [&](int t) {
+            const int s = t % NS, n = tile_n(t), at = tile_at(t);
+            tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            const float w = r < n ? j.scale_c * exp2f((rev ? n - 1 - r : r + 1) * g2) : 0.f;
+            const uint64_t w2 = tc::f32x2(w, w);
+            const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
+            const int64_t pos = ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * j.dv + c0;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t x[32], y[32];
+                __syncwarp();
+                tc::tmem_ld32(row + TM_QS + half * 32, x);
+                tc::tmem_ld32(row + TM_PV + half * 32, y);
+                tc::tmem_ld_wait();
+                if (odd) {                       // what is not finite, for the rows that see it
+                    const __nv_bfloat16 *v = (const __nv_bfloat16 *)j.v + ((int64_t)b * a.L + at) * j.ldv +
+                                             (int64_t)(h / j.rv) * j.dv + c0 + half * 32;
+#pragma unroll 1
+                    for (int jb = 0; jb < 8; ++jb) {
+                        uint32_t p[8];
+                        tc::tmem_ld8(row + TM_QK + (t & 1) * 128 + jb * 8, p);
+                        tc::tmem_ld_wait();
+#pragma unroll 1
+                        for (int k = 0; k < 16; ++k) {
+                            const int jj = jb * 16 + k;
+                            uint32_t pw = 0;
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) pw = z == (k >> 1) ? p[z] : pw;
+                            const float pf = __uint_as_float(k & 1 ? pw & 0xffff0000u : pw << 16);
+                            if (jj < n && (rev ? jj >= r : jj <= r)) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) {
+                                    const float u = __bfloat162float(v[jj * j.ldv + e]);
+                                    if (!isfinite(u)) y[e] = __float_as_uint(fmaf(pf, u, __uint_as_float(y[e])));
+                                }
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (half == 1) {                 // everything of this tile has been read
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tc::mbar_arrive(&sm->o_free);
+                        tc::mbar_arrive(&sm->free_v[s]);
+                    }
+                }
+                if (r < n && j.o_f32) {
+                    float4 *p = reinterpret_cast<float4 *>((float *)j.o + pos + half * 32);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 u0 = tc::f32x2_get(tc::f32x2_fma(w2, pair_of(x[4 * e], x[4 * e + 1]), pair_of(y[4 * e], y[4 * e + 1])));
+                        const float2 u1 = tc::f32x2_get(tc::f32x2_fma(w2, pair_of(x[4 * e + 2], x[4 * e + 3]), pair_of(y[4 * e + 2], y[4 * e + 3])));
+                        p[e] = make_float4(u0.x, u0.y, u1.x, u1.y);
+                    }
+                } else if (r < n) {
+                    uint4 *p = reinterpret_cast<uint4 *>((__nv_bfloat16 *)j.o + pos + half * 32);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const int c = 8 * e + 2 * z;
+                            u[z] = tc::f32x2_bf16(tc::f32x2_fma(w2, pair_of(x[c], x[c + 1]), pair_of(y[c], y[c + 1])));
+                        }
+                        p[e] = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                }
+            }
+        };
+        for (int t = 0; t < ntiles; ++t) {
+            weigh(t);
+            if (!STATE_ONLY && t > 0) finish(t - 1);
+        }
+        if (!STATE_ONLY && ntiles > 0) finish(ntiles - 1);
+    } else if (warp >= 12) {
+        // ------------------------------------------------------------------ the state: a key per thread (64 of them: two
+        // threads, 32 columns each)
+        constexpr int NC = DK == 128 ? 64 : 32;
+        const int q4 = warp & 3, d = (q4 * 32 + lane) % DK, cc = DK == 128 ? 0 : (q4 >> 1) * 32;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16);
+        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * j.dv;
+        const float *from = STATE_ONLY ? nullptr
+                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
+                            : j.s_in   ? j.s_in + bh * ssize
+                                       : nullptr;
+        float st[NC];
+#pragma unroll
+        for (int e = 0; e < NC; ++e) {
+            const int64_t c = c0 + cc + e;
+            st[e] = !from ? 0.f : j.transposed ? from[(int64_t)d * j.dv + c] : from[c * DK + d];
+        }
+        auto publish = [&]() {                   // the bf16 copy that QS reads: row d, columns side by side
+#pragma unroll
+            for (int e = 0; e < NC; e += 8)
+                *reinterpret_cast<uint4 *>(smem + L::S + tc::sw128_offset(d, (cc + e) >> 3)) =
+                    make_uint4(tc::pack_bf16x2(st[e], st[e + 1]), tc::pack_bf16x2(st[e + 2], st[e + 3]),
+                               tc::pack_bf16x2(st[e + 4], st[e + 5]), tc::pack_bf16x2(st[e + 6], st[e + 7]));
+            tc::fence_proxy_async_smem();
+        };
+        if (!STATE_ONLY) {
+            publish();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->s_full);
+        }
+        const float full = (float)exp2((double)g2 * LT);
+        for (int t = 0; t < ntiles; ++t) {
+            const int n = tile_n(t);
+            const float dec = n == LT ? full : (float)exp2((double)g2 * n);
+            tc::mbar_wait(&sm->kv_done[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < NC; k += 32) {
+                uint32_t x[32];
+                tc::tmem_ld32(row + TM_KV + (t & 1) * 64 + cc + k, x);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) st[k + e] = fmaf(dec, st[k + e], __uint_as_float(x[e]));
+            }
+            if (!STATE_ONLY && t + 1 < ntiles) {
+                tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
+                publish();
+            }
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && (STATE_ONLY || t + 1 < ntiles)) tc::mbar_arrive(&sm->s_full);
+        }
+        float *to = STATE_ONLY ? j.seg + (bh * a.nseg + seg + 1) * ssize
+                    : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
+        if (to) {
+#pragma unroll
+            for (int e = 0; e < NC; ++e) {
+                const int64_t c = c0 + cc + e;
+                if (j.transposed) to[(int64_t)d * j.dv + c] = st[e];
+                else to[c * DK + d] = st[e];
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == WARP_ALLOC) tc::tmem_dealloc(tmem, TM_COLS);
+}
+
+// [B, L, streams, D] rows ld apart; a box is 128 tokens of 64 entries of one stream.  Rows behind the sequence read as zeros.
+bool stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int streams, int L, int B, int64_t ld)
+{
+    const uint64_t dims[4] = {(uint64_t)D, (uint64_t)streams, (uint64_t)L, (uint64_t)B};
+    const uint64_t strides[3] = {(uint64_t)D * 2, (uint64_t)ld * 2, (uint64_t)ld * L * 2};
+    const uint32_t box[4] = {64, 1, LT, 1};
+    return encode_tmap_bf16_cached(cache, m, p, 4, dims, strides, box);
+}
+
+template <int DK, bool STATE_ONLY>
+bool run_tiles(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
+{
+    const size_t smem = Sm<DK>::SMALL + sizeof(Small);
+    if (!ensure_dynamic_smem((const void *)la_tiles_kernel<DK, STATE_ONLY>, smem)) return false;
+    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? a.nseg - 1 : a.nseg) * (a.job[0].dv / LDV);
+    ctx.begin(STATE_ONLY ? STAGE_LA_STATES : STAGE_LA_TILES);
+    launch_kernel(la_tiles_kernel<DK, STATE_ONLY>, dim3((unsigned)n), dim3(THREADS), smem, ctx.stream, true, maps, a,
+                  ctx.d_status);
+    ctx.end();
+    return cudaGetLastError() == cudaSuccess;
+}
+
+}  // namespace
+
+bool la_tiles_shape(int dtype, int N, int P)
+{
+    return dtype == SWIMBA_DTYPE_BF16 && (N == 64 || N == 128) && (P == 64 || P == 128);
+}
+
+bool la_tiles_reach(const LaArgs &a)
+{
+    // (a tensor map's strides stay below 2^40 bytes)
+    for (int i = 0; i < a.njobs; ++i)
+        for (int64_t ld : {a.job[i].ldq, a.job[i].ldk, a.job[i].ldv})
+            if (ld * 2 * a.L >= (int64_t)1 << 40) return false;
+    return true;
+}
+
+int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states)
+{
+    // jobs of one head size go in one launch
+    for (int dk : {64, 128}) {
+        LaArgs a = all;
+        Maps maps;
+        a.njobs = 0;
+        for (int i = 0; i < all.njobs; ++i) {
+            const LaJob &j = all.job[i];
+            if (j.dk != dk) continue;
+            const int n = a.njobs++;
+            a.job[n] = j;
+            if (!stream_map(ctx.tmaps, &maps.q[n], j.q, j.dk, a.H / j.rq, a.L, a.B, j.ldq) ||
+                !stream_map(ctx.tmaps, &maps.k[n], j.k, j.dk, a.H / j.rk, a.L, a.B, j.ldk) ||
+                !stream_map(ctx.tmaps, &maps.v[n], j.v, j.dv, a.H / j.rv, a.L, a.B, j.ldv))
+                return SWIMBA_ERR_CUDA;
+        }
+        if (a.njobs == 0) continue;
+        const bool ok = dk == 64 ? (states ? run_tiles<64, true>(ctx, maps, a) : run_tiles<64, false>(ctx, maps, a))
+                                 : (states ? run_tiles<128, true>(ctx, maps, a) : run_tiles<128, false>(ctx, maps, a));
+        if (!ok) return SWIMBA_ERR_CUDA;
+    }
+    return SWIMBA_OK;
+}
+
+}  // namespace swimba

@@ -37,10 +37,10 @@ la_steps_kernel(const __grid_constant__ LaArgs a)
     if (c0 >= j.dv) return;
     const int tid = threadIdx.x, lane16 = tid & 15, col = (tid >> 4) * 4;   // four columns c0 + col ..
     const int dk = j.dk, dv = j.dv;
-    const float g2 = la_log2_decay(a.log_decay[h]);
-    const float lam = exp2f(g2);
-    // segments are numbered in the order in which they are walked
-    const int w0 = seg * a.seg_len, w1 = min(a.L, w0 + a.seg_len);
+    const LaDecay lam = la_decay(a.log_decay[h]);
+    // segments are numbered in the order of the walk; w counts its tokens
+    const int place = j.reverse ? a.nseg - 1 - seg : seg, first = place * a.seg_len, last = min(a.L, first + a.seg_len);
+    const int w0 = j.reverse ? a.L - last : first, w1 = w0 + (last - first);
     const T *q = (const T *)j.q + (int64_t)b * a.L * j.ldq + (int64_t)(h / j.rq) * dk;
     const T *k = (const T *)j.k + (int64_t)b * a.L * j.ldk + (int64_t)(h / j.rk) * dk;
     const T *v = (const T *)j.v + (int64_t)b * a.L * j.ldv + (int64_t)(h / j.rv) * dv;
@@ -86,9 +86,10 @@ la_steps_kernel(const __grid_constant__ LaArgs a)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     // the decay meets the state before the token (forward) or behind it (backward)
-                    float x = j.reverse ? fmaf(ka, vv[c], s[m][c]) : fmaf(lam, s[m][c], ka * vv[c]);
+                    const float y = s[m][c];
+                    const float x = j.reverse ? fmaf(ka, vv[c], y) : fmaf(lam.hi, y, fmaf(lam.lo, y, ka * vv[c]));
                     if (!STATE_ONLY) acc[c] = fmaf(x, qq, acc[c]);
-                    s[m][c] = j.reverse ? lam * x : x;
+                    s[m][c] = j.reverse ? fmaf(lam.hi, x, lam.lo * x) : x;
                 }
             }
             if (!STATE_ONLY) {
@@ -138,13 +139,16 @@ la_chain_kernel(const __grid_constant__ LaArgs a)
     const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
     if (i >= ssize) return;
     const int h = (int)(blockIdx.y % a.H);
-    const float lam = exp2f(la_log2_decay(a.log_decay[h]) * a.seg_len);   // (segments in front of the last are whole)
+    const double l2 = la_log2_decay(a.log_decay[h]);
+    // every segment but the sequence's last, the first of a walk backward, is whole
+    const float whole = (float)exp2(l2 * a.seg_len), first = j.reverse ? (float)exp2(l2 * (a.L - (a.nseg - 1) * a.seg_len)) : whole;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.s_in) s = *reinterpret_cast<const float4 *>(j.s_in + blockIdx.y * ssize + i);
     float *p = j.seg + (int64_t)blockIdx.y * a.nseg * ssize + i;
 #pragma unroll 4
     for (int g = 1; g < a.nseg; ++g) {
         const float4 l = *reinterpret_cast<const float4 *>(p + g * ssize);
+        const float lam = g == 1 ? first : whole;
         s.x = fmaf(lam, s.x, l.x);
         s.y = fmaf(lam, s.y, l.y);
         s.z = fmaf(lam, s.z, l.z);
@@ -248,7 +252,7 @@ la_step_kernel(const float *__restrict__ log_decay, const T *__restrict__ q, int
     const int h = (int)(bh % H);
     const int64_t b = bh / H;
     const int g = h / (H / G);
-    const float lam = exp2f(la_log2_decay(log_decay[h]));
+    const LaDecay lam = la_decay(log_decay[h]);
     const int64_t base = (bh * P + p0) * N;
     float acc[ST_ROWS], vv[ST_ROWS];
 #pragma unroll
@@ -265,10 +269,10 @@ la_step_kernel(const float *__restrict__ log_decay, const T *__restrict__ q, int
 #pragma unroll
         for (int r = 0; r < ST_ROWS; ++r) {
             if (p0 + r >= P) continue;
-            s[r].x = fmaf(lam, s[r].x, vv[r] * kk.x);
-            s[r].y = fmaf(lam, s[r].y, vv[r] * kk.y);
-            s[r].z = fmaf(lam, s[r].z, vv[r] * kk.z);
-            s[r].w = fmaf(lam, s[r].w, vv[r] * kk.w);
+            s[r].x = fmaf(lam.hi, s[r].x, fmaf(lam.lo, s[r].x, vv[r] * kk.x));
+            s[r].y = fmaf(lam.hi, s[r].y, fmaf(lam.lo, s[r].y, vv[r] * kk.y));
+            s[r].z = fmaf(lam.hi, s[r].z, fmaf(lam.lo, s[r].z, vv[r] * kk.z));
+            s[r].w = fmaf(lam.hi, s[r].w, fmaf(lam.lo, s[r].w, vv[r] * kk.w));
             acc[r] = fmaf(s[r].x, qq.x, fmaf(s[r].y, qq.y, fmaf(s[r].z, qq.z, fmaf(s[r].w, qq.w, acc[r]))));
             __stcs(reinterpret_cast<float4 *>(s_out + base + (int64_t)r * N + n), s[r]);
         }
@@ -311,9 +315,11 @@ void run_step_n(LaunchCtx &ctx, const float *log_decay, const void *q, int64_t l
 }  // namespace
 
 namespace {
-constexpr int LA_MIN_SEG = 64;      // tokens
-// Segments per sequence that give every SM two blocks.
-int la_want(int B, int H, int N, int P, int njobs, int sm_count)
+// What a segment's length is a multiple of: token-by-token segments have 64 tokens at least, tiles 128.
+constexpr int LA_STEP_SEG = 64, LA_TILE_SEG = 128;
+// The most segments a sequence is cut into: token by token, as many as give every SM two blocks; by tiles, as many
+// as fill two waves.
+int la_most(int B, int H, int N, int P, int njobs, int sm_count)
 {
     const int64_t blocks = (int64_t)njobs * B * H * ceil_div(std::max(N, P), LA_COLS);
     return (int)std::max<int64_t>(1, 2 * sm_count / blocks);
@@ -322,28 +328,54 @@ int la_want(int B, int H, int N, int P, int njobs, int sm_count)
 
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg)
 {
-    (void)dtype;
-    const int len = std::max(LA_MIN_SEG, ceil_div(ceil_div(L, la_want(B, H, N, P, njobs, sm_count)), 16) * 16);
-    *seg_len = std::min(len, L);
-    *nseg = ceil_div(L, *seg_len);
+    const bool tiles = la_tiles_shape(dtype, N, P);
+    const int most = la_most(B, H, N, P, njobs, sm_count);
+    if (!tiles) {
+        const int len = std::max(LA_STEP_SEG, ceil_div(ceil_div(L, most), 16) * 16);
+        *seg_len = std::min(len, L);
+        *nseg = ceil_div(L, *seg_len);
+        return;
+    }
+    // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states
+    // (about 0.6 of a tile each) with what two more launches take (about 6 tiles).
+    const int nt = ceil_div(L, LA_TILE_SEG);
+    const int64_t items = (int64_t)njobs * B * H * ceil_div(std::max(N, P), LA_COLS);
+    double best = 1e30;
+    for (int n = 1; n <= std::min(most, nt); ++n) {
+        const int len = ceil_div(nt, n), ns = ceil_div(nt, len);
+        const double cost = (double)ceil_div64(items * ns, sm_count) * len +
+                            (ns > 1 ? 0.6 * ceil_div64(items * (ns - 1), sm_count) * len + 6 : 0);
+        if (cost < best) {
+            best = cost;
+            *seg_len = len * LA_TILE_SEG;
+            *nseg = ns;
+        }
+    }
 }
 
 size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count)
 {
     // the most that a call of up to B sequences and L tokens is cut into; none where sequences stay whole
-    (void)dtype;
+    const bool tiles = la_tiles_shape(dtype, N, P);
     int64_t most = 0;
     for (int b = 1; b <= B; ++b) {
-        const int n = std::min(la_want(b, H, N, P, njobs, sm_count), ceil_div(L, LA_MIN_SEG));
+        const int n = std::min(la_most(b, H, N, P, njobs, sm_count), ceil_div(L, tiles ? LA_TILE_SEG : LA_STEP_SEG));
         if (n == 1) break;
         most = std::max<int64_t>(most, (int64_t)b * n);
     }
     return (size_t)most * H * N * P * sizeof(float);
 }
 
-int launch_la(LaunchCtx &ctx, int dtype, LaArgs &a, int sm_count)
+int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a)
 {
-    return dtype == SWIMBA_DTYPE_FP32 ? launch_steps<float>(ctx, a) : launch_steps<__nv_bfloat16>(ctx, a);
+    if (!la_tiles_shape(dtype, a.job[0].dk, a.job[0].dv) || !la_tiles_reach(a))
+        return dtype == SWIMBA_DTYPE_FP32 ? launch_steps<float>(ctx, a) : launch_steps<__nv_bfloat16>(ctx, a);
+    if (a.nseg > 1) {
+        int rc = launch_la_tiles(ctx, a, true);
+        if (rc == SWIMBA_OK) rc = launch_chain(ctx, a);
+        if (rc != SWIMBA_OK) return rc;
+    }
+    return launch_la_tiles(ctx, a, false);
 }
 
 int launch_la_head_sum(LaunchCtx &ctx, int dtype, const float *part, int64_t T, int G, int r, int N, void *out)

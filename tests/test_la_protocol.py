@@ -1,0 +1,161 @@
+"""The waits of the linear-attention tile kernel, on the CPU: its warps as coroutines over counted barriers, run in random
+orders.  Every wait ends, no barrier gets two phases ahead of a waiter (parities would alias), and no buffer is written while
+its last contents are still to be read."""
+import random
+
+import pytest
+
+
+class Bars:
+    def __init__(self, need):
+        self.need, self.got, self.done = need, {n: 0 for n in need}, {n: 0 for n in need}
+
+    def arrive(self, n):
+        self.got[n] += 1
+        if self.got[n] == self.need[n]:
+            self.got[n], self.done[n] = 0, self.done[n] + 1
+
+    def ready(self, n, phase):
+        assert self.done[n] <= phase + 1, f"{n}: phase {self.done[n]} with a waiter on {phase}"
+        return self.done[n] > phase
+
+
+class Buffers:
+    """name -> (version held, readers still to come)."""
+
+    def __init__(self):
+        self.v = {}
+
+    def write(self, name, version, readers):
+        old = self.v.get(name)
+        assert old is None or old[1] == 0, f"{name}: version {version} over {old}"
+        self.v[name] = [version, readers]
+
+    def read(self, name, version):
+        assert self.v[name][0] == version and self.v[name][1] > 0, f"{name}: {version} wanted, {self.v[name]} held"
+        self.v[name][1] -= 1
+
+
+def run(n, ns, state_only, rng):
+    need = {f"{k}_{x}{s}": 1 for s in range(ns) for k in ("full", "free") for x in "qkv"}
+    for s in range(ns):
+        need[f"free_v{s}"] = 1
+    need.update({f"{k}{p}": 1 for p in range(2) for k in ("qk_full", "p_full", "kv_done")})
+    need.update(qs_done=1, pv_done=1, vw_full=1, s_full=1, o_free=1)
+    bars, buf = Bars(need), Buffers()
+    async_ops = []                       # products and copies, each queue in order: callables
+
+    def tma():
+        for t in range(n):
+            s = t % ns
+            for x in "kv" if state_only else "kqv":
+                if t >= ns:
+                    yield f"free_{x}{s}", t // ns - 1
+                readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 3}[x]
+                async_ops.append([lambda x=x, s=s, t=t, r=readers: (buf.write(f"{x}{s}", t, r), bars.arrive(f"full_{x}{s}"))])
+
+    def mma():
+        queue = []
+        async_ops.append(queue)
+
+        def scores(t):
+            yield f"full_k{t % ns}", t // ns
+            yield f"full_q{t % ns}", t // ns
+            queue.append(lambda: (buf.read(f"k{t % ns}", t), buf.read(f"q{t % ns}", t), buf.write(f"a{t & 1}", t, 1),
+                                  bars.arrive(f"qk_full{t & 1}")))
+        if not state_only and n:
+            yield from scores(0)
+        for t in range(n):
+            s = t % ns
+            if state_only:
+                yield f"full_k{s}", t // ns
+                if t:
+                    yield "s_full", t - 1
+            yield "vw_full", t
+            queue.append(lambda t=t, s=s: (buf.read(f"k{s}", t), buf.read("vw", t), buf.write(f"d{t & 1}", t, 1),
+                                           bars.arrive(f"kv_done{t & 1}"), bars.arrive(f"free_k{s}")))
+            if state_only:
+                continue
+            yield "s_full", t
+            if t:
+                yield "o_free", t - 1
+            queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s", t), buf.write("qs", t, 1),
+                                           bars.arrive("qs_done"), bars.arrive(f"free_q{s}")))
+            if t + 1 < n:
+                yield from scores(t + 1)
+            yield f"full_v{s}", t // ns
+            yield f"p_full{t & 1}", t >> 1
+            queue.append(lambda t=t, s=s: (buf.read(f"v{s}", t), buf.read(f"p{t & 1}", t), buf.write("pv", t, 1),
+                                           bars.arrive("pv_done")))
+
+    def masks():
+        for t in range(n):
+            yield f"qk_full{t & 1}", t >> 1
+            buf.read(f"a{t & 1}", t)
+            buf.write(f"p{t & 1}", t, 2)                 # the product, and the epilogue of a tile that is not all finite
+            yield None
+            bars.arrive(f"p_full{t & 1}")
+
+    def values():
+        def finish(t):
+            yield "qs_done", t
+            yield "pv_done", t
+            buf.read("qs", t)
+            buf.read("pv", t)
+            buf.read(f"p{t & 1}", t)
+            buf.read(f"v{t % ns}", t)
+            yield None
+            bars.arrive("o_free")
+            bars.arrive(f"free_v{t % ns}")
+        for t in range(n):
+            yield f"full_v{t % ns}", t // ns
+            if t:
+                yield f"kv_done{(t - 1) & 1}", (t - 1) >> 1
+            buf.read(f"v{t % ns}", t)
+            buf.write("vw", t, 1)
+            yield None
+            bars.arrive("vw_full")
+            if state_only:
+                bars.arrive(f"free_v{t % ns}")
+            elif t:
+                yield from finish(t - 1)
+        if not state_only and n:
+            yield from finish(n - 1)
+
+    def state():
+        if not state_only:
+            buf.write("s", 0, 1)
+            bars.arrive("s_full")
+        for t in range(n):
+            yield f"kv_done{t & 1}", t >> 1
+            buf.read(f"d{t & 1}", t)
+            if not state_only and t + 1 < n:
+                yield "qs_done", t
+                buf.write("s", t + 1, 1)
+                yield None
+            if state_only or t + 1 < n:
+                bars.arrive("s_full")
+
+    live = [[g, next(g, "end")] for g in ([tma(), mma(), values(), state()] + ([] if state_only else [masks()]))]
+    live = [x for x in live if x[1] != "end"]
+    while live or any(async_ops):
+        steps = [x for x in live if x[1] is None or bars.ready(*x[1])]
+        queues = [q for q in async_ops if q]
+        assert steps or queues, [x[1] for x in live]
+        pick = rng.randrange(len(steps) + len(queues))
+        if pick < len(steps):
+            x = steps[pick]
+            x[1] = next(x[0], "end")
+            if x[1] == "end":
+                live.remove(x)
+        else:
+            queues[pick - len(steps)].pop(0)()
+
+
+@pytest.mark.parametrize("state_only", [False, True])
+@pytest.mark.parametrize("ns", [2, 3])
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 7, 20])
+def test_every_wait_ends_and_no_buffer_is_lost(n, ns, state_only):
+    rng = random.Random(n * 10 + ns)
+    for _ in range(60):
+        run(n, ns, state_only, rng)
