@@ -40,8 +40,8 @@ def run(n, ns, state_only, rng):
     need = {f"{k}_{x}{s}": 1 for s in range(ns) for k in ("full", "free") for x in "qkv"}
     for s in range(ns):
         need[f"free_v{s}"] = 1
-    need.update({f"{k}{p}": 1 for p in range(2) for k in ("qk_full", "p_full", "kv_done")})
-    need.update(qs_done=1, pv_done=1, vw_full=1, s_full=1, o_free=1)
+    need.update({f"{k}{p}": 1 for p in range(2) for k in ("qk_full", "p_full")})
+    need.update(qs_done=1, qs_read=1, pv_done=1, vw_full=1, kv_done=1, kv_read=1, s_full=1, o_free=1)
     bars, buf = Bars(need), Buffers()
     async_ops = []                       # products and copies, each queue in order: callables
 
@@ -51,7 +51,7 @@ def run(n, ns, state_only, rng):
             for x in "kv" if state_only else "kqv":
                 if t >= ns:
                     yield f"free_{x}{s}", t // ns - 1
-                readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 3}[x]
+                readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 2}[x]
                 async_ops.append([lambda x=x, s=s, t=t, r=readers: (buf.write(f"{x}{s}", t, r), bars.arrive(f"full_{x}{s}"))])
 
     def mma():
@@ -69,23 +69,24 @@ def run(n, ns, state_only, rng):
             s = t % ns
             if state_only:
                 yield f"full_k{s}", t // ns
-                if t:
-                    yield "s_full", t - 1
+            if t:
+                yield "kv_read", t - 1
             yield "vw_full", t
-            queue.append(lambda t=t, s=s: (buf.read(f"k{s}", t), buf.read("vw", t), buf.write(f"d{t & 1}", t, 1),
-                                           bars.arrive(f"kv_done{t & 1}"), bars.arrive(f"free_k{s}")))
+            queue.append(lambda t=t, s=s: (buf.read(f"k{s}", t), buf.read("vw", t), buf.write("d", t, 1),
+                                           bars.arrive("kv_done"), bars.arrive(f"free_k{s}")))
             if state_only:
                 continue
             yield "s_full", t
             if t:
                 yield "o_free", t - 1
-            queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s", t), buf.write("qs", t, 1),
+            queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s", t), buf.write("o", 2 * t, 1),
                                            bars.arrive("qs_done"), bars.arrive(f"free_q{s}")))
             if t + 1 < n:
                 yield from scores(t + 1)
             yield f"full_v{s}", t // ns
             yield f"p_full{t & 1}", t >> 1
-            queue.append(lambda t=t, s=s: (buf.read(f"v{s}", t), buf.read(f"p{t & 1}", t), buf.write("pv", t, 1),
+            yield "qs_read", t
+            queue.append(lambda t=t, s=s: (buf.read(f"v{s}", t), buf.read(f"p{t & 1}", t), buf.write("o", 2 * t + 1, 1),
                                            bars.arrive("pv_done")))
 
     def masks():
@@ -97,46 +98,47 @@ def run(n, ns, state_only, rng):
             bars.arrive(f"p_full{t & 1}")
 
     def values():
-        def finish(t):
-            yield "qs_done", t
-            yield "pv_done", t
-            buf.read("qs", t)
-            buf.read("pv", t)
-            buf.read(f"p{t & 1}", t)
-            buf.read(f"v{t % ns}", t)
-            yield None
-            bars.arrive("o_free")
-            bars.arrive(f"free_v{t % ns}")
         for t in range(n):
             yield f"full_v{t % ns}", t // ns
             if t:
-                yield f"kv_done{(t - 1) & 1}", (t - 1) >> 1
+                yield "kv_done", t - 1
             buf.read(f"v{t % ns}", t)
             buf.write("vw", t, 1)
             yield None
             bars.arrive("vw_full")
             if state_only:
                 bars.arrive(f"free_v{t % ns}")
-            elif t:
-                yield from finish(t - 1)
-        if not state_only and n:
-            yield from finish(n - 1)
+
+    def outputs():
+        for t in range(n):
+            yield "qs_done", t
+            buf.read("o", 2 * t)
+            yield None
+            bars.arrive("qs_read")
+            yield "pv_done", t
+            buf.read("o", 2 * t + 1)
+            buf.read(f"p{t & 1}", t)
+            yield None
+            bars.arrive("o_free")
+            buf.write(f"v{t % ns}", f"o{t}", 1)           # staged where V stood
+            yield None
+            buf.read(f"v{t % ns}", f"o{t}")               # the copy to memory
+            bars.arrive(f"free_v{t % ns}")
 
     def state():
-        if not state_only:
-            buf.write("s", 0, 1)
-            bars.arrive("s_full")
         for t in range(n):
-            yield f"kv_done{t & 1}", t >> 1
-            buf.read(f"d{t & 1}", t)
-            if not state_only and t + 1 < n:
-                yield "qs_done", t
-                buf.write("s", t + 1, 1)
+            if not state_only:
+                if t:
+                    yield "qs_done", t - 1
+                buf.write("s", t, 1)
                 yield None
-            if state_only or t + 1 < n:
                 bars.arrive("s_full")
+            yield "kv_done", t
+            buf.read("d", t)
+            yield None
+            bars.arrive("kv_read")
 
-    live = [[g, next(g, "end")] for g in ([tma(), mma(), values(), state()] + ([] if state_only else [masks()]))]
+    live = [[g, next(g, "end")] for g in ([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]))]
     live = [x for x in live if x[1] != "end"]
     while live or any(async_ops):
         steps = [x for x in live if x[1] is None or bars.ready(*x[1])]
