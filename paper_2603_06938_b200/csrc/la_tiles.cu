@@ -3,8 +3,7 @@
 // token in the order of the walk, and the state S [DK, DV] entering it:
 //   QK   A = Q K^T                                            scores
 //        P_ij = scale_p lambda^|i-j| A_ij  for tokens j that i sees, else 0
-//   QS   O = Q S, then O_i <- scale_c lambda^(r_i + first) O_i
-//   PV   O += P V
+//   PV   O1 = P V,   QS  O2 = Q S,   o_i = O1_i + scale_c lambda^(r_i + first) O2_i
 //   KV   D = K^T (w V),  w_j = scale_a lambda^(n - r_j - first),   S <- lambda^n S + D
 // (first = 1 walking forward, 0 backward, where the decay follows the read of a token).
 //
@@ -33,8 +32,9 @@ constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
 // fit waited for instructions most of the time (9000 cycles a tile).
 constexpr int THREADS = 1024;
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 28;
-// tensor memory columns: two score tiles (their masked bf16 form over them), O, a D for each part
-constexpr uint32_t TM_QK = 0, TM_O = 256, TM_KV = 320, TM_COLS = 512;
+constexpr int AHEAD = 4;                     // tiles whose rows are on their way to L2
+// tensor memory columns: scores, P (bf16), Q S, P V, a D for each part of w V
+constexpr uint32_t TM_QK = 0, TM_P = 128, TM_QS = 192, TM_PV = 256, TM_KV = 320, TM_COLS = 512;
 
 template <int DK> struct Sm {
     static constexpr int NS = DK == 64 ? 3 : 2;           // stages of Q, K and V
@@ -44,7 +44,7 @@ template <int DK> struct Sm {
 };
 struct Small {
     uint64_t full_q[3], full_k[3], full_v[3], free_q[3], free_k[3], free_v[3];
-    uint64_t qk_full[2], p_full[2], qs_done, qs_read, pv_done, vw_full, kv_done, kv_read, s_full, o_free;
+    uint64_t qk_full, qk_read, p_full, qs_done, pv_done, vw_full[2], kv_done[2], kv_read, s_full, o_free;
     uint32_t tmem;
     int abort_flag;
     int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
@@ -108,16 +108,16 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             tc::mbar_init(&sm->free_v[s], STATE_ONLY ? 8 : j.o_f32 ? 4 : 1);
         }
         for (int s = 0; s < 2; ++s) {
-            tc::mbar_init(&sm->qk_full[s], 1);
-            tc::mbar_init(&sm->p_full[s], 8);
+            tc::mbar_init(&sm->vw_full[s], 8);
+            tc::mbar_init(&sm->kv_done[s], 1);
             sm->odd_tile[s] = 0;
         }
+        tc::mbar_init(&sm->qk_full, 1);
+        tc::mbar_init(&sm->qk_read, 8);
+        tc::mbar_init(&sm->p_full, 8);
         tc::mbar_init(&sm->qs_done, 1);
-        tc::mbar_init(&sm->qs_read, 4);
-        tc::mbar_init(&sm->kv_done, 1);
-        tc::mbar_init(&sm->kv_read, 8);
         tc::mbar_init(&sm->pv_done, 1);
-        tc::mbar_init(&sm->vw_full, 8);
+        tc::mbar_init(&sm->kv_read, 8);
         tc::mbar_init(&sm->s_full, 8);
         tc::mbar_init(&sm->o_free, 4);
         *abort_flag = 0;
@@ -146,8 +146,19 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     if (warp == WARP_TMA) {
         // ------------------------------------------------------------------ loads, in the order in which room comes free
         const bool leader = tc::elect_one();
+        // (a load from L2 comes back in about half the time that one from HBM takes, and its room is taken that much shorter)
+        auto prefetch = [&](int t) {
+            if (t >= ntiles || !leader) return;
+            for (int o = 0; o < DK; o += 64) {
+                tc::tma_prefetch_4d(&maps.k[ji], o, h / j.rk, tile_at(t), b);
+                if (!STATE_ONLY) tc::tma_prefetch_4d(&maps.q[ji], o, h / j.rq, tile_at(t), b);
+            }
+            tc::tma_prefetch_4d(&maps.v[ji], c0, h / j.rv, tile_at(t), b);
+        };
+        for (int t = NS; t < AHEAD; ++t) prefetch(t);
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NS, at = tile_at(t);
+            prefetch(t + AHEAD);
             const uint32_t ph = ((t / NS) & 1) ^ 1;
             auto load = [&](uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int col, int stream) {
                 tc::mbar_wait(room, ph, abort_flag, d_status);
@@ -193,6 +204,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             const uint32_t ph = (t / NS) & 1;
             tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
             tc::mbar_wait(&sm->full_q[s], ph, abort_flag, d_status);
+            if (t > 0) tc::mbar_wait(&sm->qk_read, (t - 1) & 1, abort_flag, d_status);
             tc::tc_fence_after();
             if (leader) {
                 const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB));
@@ -200,9 +212,9 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
 #pragma unroll
                 for (int kk = 0; kk < DK / 16; ++kk) {
                     const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
-                    tc::mma_ss(tm + TM_QK + (t & 1) * 128, tc::smem_desc_advance(q, o), tc::smem_desc_advance(k, o), id_qk, kk > 0);
+                    tc::mma_ss(tm + TM_QK, tc::smem_desc_advance(q, o), tc::smem_desc_advance(k, o), id_qk, kk > 0);
                 }
-                tc::mma_commit(&sm->qk_full[t & 1]);
+                tc::mma_commit(&sm->qk_full);
             }
             __syncwarp();
         };
@@ -210,20 +222,25 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NS;
             const uint32_t ph = (t / NS) & 1;
-            // KV: the state's additions do not wait for the state
+            // KV, by halves of the tile: w V of one is made while the other is multiplied.  It does not wait for the state.
             if (STATE_ONLY) tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
             if (t > 0) tc::mbar_wait(&sm->kv_read, (t - 1) & 1, abort_flag, d_status);
-            tc::mbar_wait(&sm->vw_full, t & 1, abort_flag, d_status);
-            tc::tc_fence_after();
-            if (leader) {
-                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, s * L::QB)), w = tc::smem_desc_fresh(dW);
+#pragma unroll 1
+            for (int hf = 0; hf < 2; ++hf) {
+                tc::mbar_wait(&sm->vw_full[hf], t & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+                if (leader) {
+                    const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, s * L::QB + hf * 8192));
+                    const uint64_t w = tc::smem_desc_fresh(tc::smem_desc_advance(dW, hf * 8192));
 #pragma unroll
-                for (int kk = 0; kk < LT / 16; ++kk)
-                    tc::mma_ss(tm + TM_KV, tc::smem_desc_advance(k, kk * 2048), tc::smem_desc_advance(w, kk * 2048), id_kv, kk > 0);
-                tc::mma_commit(&sm->kv_done);
-                tc::mma_commit(&sm->free_k[s]);
+                    for (int kk = 0; kk < LT / 32; ++kk)
+                        tc::mma_ss(tm + TM_KV, tc::smem_desc_advance(k, kk * 2048), tc::smem_desc_advance(w, kk * 2048), id_kv,
+                                   hf + kk > 0);
+                    tc::mma_commit(&sm->kv_done[hf]);
+                    if (hf == 1) tc::mma_commit(&sm->free_k[s]);
+                }
+                __syncwarp();
             }
-            __syncwarp();
             if (STATE_ONLY) continue;
             // QS: the carried part, once the state is there and the epilogue has read the tile in front
             tc::mbar_wait(&sm->s_full, t & 1, abort_flag, d_status);
@@ -234,7 +251,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                 const uint64_t st = tc::smem_desc_fresh(dS);
 #pragma unroll
                 for (int kk = 0; kk < DK / 16; ++kk)
-                    tc::mma_ss(tm + TM_O, tc::smem_desc_advance(q, (kk >> 2) * SLAB + (kk & 3) * 32),
+                    tc::mma_ss(tm + TM_QS, tc::smem_desc_advance(q, (kk >> 2) * SLAB + (kk & 3) * 32),
                                tc::smem_desc_advance(st, kk * 2048), id_qs, kk > 0);
                 tc::mma_commit(&sm->qs_done);
                 tc::mma_commit(&sm->free_q[s]);
@@ -243,40 +260,48 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             if (t + 1 < ntiles) scores(t + 1);
             // PV
             tc::mbar_wait(&sm->full_v[s], ph, abort_flag, d_status);
-            tc::mbar_wait(&sm->p_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
-            tc::mbar_wait(&sm->qs_read, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->p_full, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
             if (leader) {
                 const uint64_t v = tc::smem_desc_fresh(tc::smem_desc_advance(dV, s * SLAB));
 #pragma unroll
                 for (int kk = 0; kk < LT / 16; ++kk)
-                    tc::mma_ts(tm + TM_O, tm + TM_QK + (t & 1) * 128 + (kk >> 2) * 64 + (kk & 3) * 8,
-                               tc::smem_desc_advance(v, kk * 2048), id_qs, 1);
+                    tc::mma_ts(tm + TM_PV, tm + TM_P + kk * 8, tc::smem_desc_advance(v, kk * 2048), id_qs, kk > 0);
                 tc::mma_commit(&sm->pv_done);
             }
             __syncwarp();
         }
     } else if (warp >= WARP_MASK && warp < WARP_W) {
-        // ------------------------------------------------------------------ masks: half a row of the scores per thread, its
-        // result over the first half of what it was made from
+        // ------------------------------------------------------------------ masks: half a row of the scores per thread
         const int q4 = warp & 3, half = (warp - WARP_MASK) >> 2, i = q4 * 32 + lane;
-        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_QK + half * 64;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16), from = row + TM_QK + half * 64, to = row + TM_P + half * 32;
         const float scale_p = j.scale_p;
         const uint32_t keep = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
-            tc::mbar_wait(&sm->qk_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            if (t > 0) {                         // (P has been read, by the epilogue too where V was not all finite)
+                tc::mbar_wait(&sm->pv_done, (t - 1) & 1, abort_flag, d_status);
+                if (((volatile int *)sm->odd_tile)[(t - 1) & 1] == t) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
+            }
+            tc::mbar_wait(&sm->qk_full, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            const uint32_t region = row + (t & 1) * 128;
 #pragma unroll 1
             for (int k = 0; k < 2; ++k) {
                 const int bl = half * 2 + k;
+                const bool seen = rev ? bl >= q4 : bl <= q4;
                 uint32_t x[32], o[16];
-                if (rev ? bl < q4 : bl > q4) {
+                if (seen) {
+                    tc::tmem_ld32(from + k * 32, x);
+                    tc::tmem_ld_wait();
+                }
+                if (k == 1) {
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&sm->qk_read);
+                }
+                if (!seen) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[e] = 0u;
                 } else {
-                    tc::tmem_ld32(region + k * 32, x);
-                    tc::tmem_ld_wait();
                     if (bl == q4) {
                         const float *f = &sm->pow_diag[31 + lane];
 #pragma unroll
@@ -297,12 +322,12 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                         }
                     }
                 }
-                tc::tmem_st16(region + k * 16, o);
+                tc::tmem_st16(to + k * 16, o);
             }
             tc::tmem_st_wait();
             tc::tc_fence_before();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sm->p_full[t & 1]);
+            if (lane == 0) tc::mbar_arrive(&sm->p_full);
         }
     } else if (warp >= WARP_W && warp < WARP_STATE) {
         // ------------------------------------------------------------------ w V: eight entries of two rows at a time
@@ -312,13 +337,14 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NS, n = tile_n(t);
             tc::mbar_wait(&sm->full_v[s], (t / NS) & 1, abort_flag, d_status);
-            if (t > 0) tc::mbar_wait(&sm->kv_done, (t - 1) & 1, abort_flag, d_status);
             const uint32_t off = tc::sw128_offset(r0, ltid & 7);           // (32 rows on: 4096 bytes, same swizzle)
             uint32_t odd = 0;
 #pragma unroll 1
-            for (int i = 0; i < 4; i += 2) {
+            for (int hf = 0; hf < 2; ++hf) {
+                const int i = hf * 2;
                 uint4 v[2];
                 uint64_t w2[2];
+                if (t > 0) tc::mbar_wait(&sm->kv_done[hf], (t - 1) & 1, abort_flag, d_status);
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const int rr = r0 + 32 * (i + z), e = rev ? rr + 1 : n - 1 - rr;      // n - r - first steps of decay
@@ -346,24 +372,22 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                     *reinterpret_cast<uint4 *>(dst + SLAB) = make_uint4(p[1][0], p[1][1], p[1][2], p[1][3]);
                     if (parts == 3) *reinterpret_cast<uint4 *>(dst + 2 * SLAB) = make_uint4(p[2][0], p[2][1], p[2][2], p[2][3]);
                 }
-            }
-            if (!STATE_ONLY && (odd & 0x80008000u)) {
+                if (!STATE_ONLY && (odd & 0x80008000u)) {
 #pragma unroll 1
-                for (int i = 0; i < 16; ++i) {
-                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + L::V + s * SLAB + off + (i >> 2) * 4096) + (i & 3);
-                    uint32_t in = *at;
-                    if ((in & 0x7f80u) == 0x7f80u) in &= 0xffff0000u;
-                    if ((in & 0x7f800000u) == 0x7f800000u) in &= 0xffffu;
-                    *at = in;
+                    for (int z = 0; z < 8; ++z) {
+                        uint32_t *at = reinterpret_cast<uint32_t *>(smem + L::V + s * SLAB + off + (i + (z >> 2)) * 4096) + (z & 3);
+                        uint32_t in = *at;
+                        if ((in & 0x7f80u) == 0x7f80u) in &= 0xffff0000u;
+                        if ((in & 0x7f800000u) == 0x7f800000u) in &= 0xffffu;
+                        *at = in;
+                    }
+                    ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
                 }
-                ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
+                tc::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm->vw_full[hf]);
             }
-            tc::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                tc::mbar_arrive(&sm->vw_full);
-                if (STATE_ONLY) tc::mbar_arrive(&sm->free_v[s]);
-            }
+            if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
         }
     } else if (warp >= WARP_STATE && warp < WARP_O) {
         // ------------------------------------------------------------------ the state: half a key's columns per thread (of
@@ -399,7 +423,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             }
             const float dec = sm->pow[tile_n(t)];
             const uint64_t dec2 = tc::f32x2(dec, dec);
-            tc::mbar_wait(&sm->kv_done, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->kv_done[1], t & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll
             for (int k = 0; k < NC; k += 16) {
@@ -434,38 +458,21 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     } else if (warp >= WARP_O) {
         // ------------------------------------------------------------------ o: a row per thread, staged where V stood
         const int q4 = warp & 3, r = q4 * 32 + lane;
-        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_O;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16);
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             const int s = t % NS, n = tile_n(t), at = tile_at(t);
             const float w = r < n ? j.scale_c * sm->pow[rev ? n - 1 - r : r + 1] : 0.f;
             const uint64_t w2 = tc::f32x2(w, w);
             tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
-            tc::tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < 64; c += 32) {   // the carried part, for PV to add to
-                uint32_t x[32];
-                tc::tmem_ld32(row + c, x);
-                tc::tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float2 v = tc::f32x2_get(tc::f32x2_mul(w2, pair_of(x[e], x[e + 1])));
-                    x[e] = __float_as_uint(v.x);
-                    x[e + 1] = __float_as_uint(v.y);
-                }
-                tc::tmem_st32(row + c, x);
-            }
-            tc::tmem_st_wait();
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sm->qs_read);
             tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
             const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
             uint8_t *stage = smem + L::V + s * SLAB;
 #pragma unroll 1
             for (int c = 0; c < 64; c += 16) {
-                uint32_t y[16];
-                tc::tmem_ld16(row + c, y);
+                uint32_t x[16], y[16];
+                tc::tmem_ld16(row + TM_QS + c, x);
+                tc::tmem_ld16(row + TM_PV + c, y);
                 tc::tmem_ld_wait();
                 if (odd) {                       // what is not finite, for the rows that see it
                     const __nv_bfloat16 *v = (const __nv_bfloat16 *)j.v + ((int64_t)b * a.L + at) * j.ldv +
@@ -473,7 +480,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
 #pragma unroll 1
                     for (int jb = 0; jb < 8; ++jb) {
                         uint32_t p[8];
-                        tc::tmem_ld8(row - TM_O + TM_QK + (t & 1) * 128 + (jb >> 2) * 64 + (jb & 3) * 8, p);
+                        tc::tmem_ld8(row + TM_P + jb * 8, p);
                         tc::tmem_ld_wait();
 #pragma unroll 1
                         for (int k = 0; k < 16; ++k) {
@@ -493,6 +500,17 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                         __syncwarp();
                     }
                 }
+                if (c == 48) {                   // everything in tensor memory has been read
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&sm->o_free);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float2 u = tc::f32x2_get(tc::f32x2_fma(w2, pair_of(x[e], x[e + 1]), pair_of(y[e], y[e + 1])));
+                    y[e] = __float_as_uint(u.x);
+                    y[e + 1] = __float_as_uint(u.y);
+                }
                 if (j.o_f32) {
                     if (r < n) {
                         uint4 *p = reinterpret_cast<uint4 *>((float *)j.o + ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * j.dv + c0 + c);
@@ -508,17 +526,14 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                                        tc::f32x2_bf16(pair_of(y[e + 4], y[e + 5])), tc::f32x2_bf16(pair_of(y[e + 6], y[e + 7])));
                 }
             }
-            tc::tc_fence_before();
-            if (!j.o_f32) {
-                tc::fence_proxy_async_smem();
-                tc::named_bar_sync(1, 128);
+            if (j.o_f32) {
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm->free_v[s]);
+                continue;
             }
-            __syncwarp();
-            if (lane == 0) {
-                tc::mbar_arrive(&sm->o_free);
-                if (j.o_f32) tc::mbar_arrive(&sm->free_v[s]);
-            }
-            if (!j.o_f32 && q4 == 0) {           // (rows behind the sequence are clipped by the tensor map)
+            tc::fence_proxy_async_smem();
+            tc::named_bar_sync(1, 128);
+            if (q4 == 0) {                       // (rows behind the sequence are clipped by the tensor map)
                 if (tc::elect_one()) {
                     tc::tma_store_4d(&maps.o[ji], stage, c0, h, at, b);
                     tc::bulk_commit_group();

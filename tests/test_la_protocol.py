@@ -40,9 +40,10 @@ def run(n, ns, state_only, rng):
     need = {f"{k}_{x}{s}": 1 for s in range(ns) for k in ("full", "free") for x in "qkv"}
     for s in range(ns):
         need[f"free_v{s}"] = 1
-    need.update({f"{k}{p}": 1 for p in range(2) for k in ("qk_full", "p_full")})
-    need.update(qs_done=1, qs_read=1, pv_done=1, vw_full=1, kv_done=1, kv_read=1, s_full=1, o_free=1)
+    need.update({n: 1 for n in ("qk_full", "qk_read", "p_full", "qs_done", "pv_done", "vw_full0", "vw_full1", "kv_done0",
+                                "kv_done1", "kv_read", "s_full", "o_free")})
     bars, buf = Bars(need), Buffers()
+    odd = lambda t: t % 3 == 1
     async_ops = []                       # products and copies, each queue in order: callables
 
     def tma():
@@ -61,8 +62,10 @@ def run(n, ns, state_only, rng):
         def scores(t):
             yield f"full_k{t % ns}", t // ns
             yield f"full_q{t % ns}", t // ns
-            queue.append(lambda: (buf.read(f"k{t % ns}", t), buf.read(f"q{t % ns}", t), buf.write(f"a{t & 1}", t, 1),
-                                  bars.arrive(f"qk_full{t & 1}")))
+            if t:
+                yield "qk_read", t - 1
+            queue.append(lambda: (buf.read(f"k{t % ns}", t), buf.read(f"q{t % ns}", t), buf.write("a", t, 1),
+                                  bars.arrive("qk_full")))
         if not state_only and n:
             yield from scores(0)
         for t in range(n):
@@ -71,53 +74,61 @@ def run(n, ns, state_only, rng):
                 yield f"full_k{s}", t // ns
             if t:
                 yield "kv_read", t - 1
-            yield "vw_full", t
-            queue.append(lambda t=t, s=s: (buf.read(f"k{s}", t), buf.read("vw", t), buf.write("d", t, 1),
-                                           bars.arrive("kv_done"), bars.arrive(f"free_k{s}")))
+            yield "vw_full0", t
+            queue.append(lambda t=t: (buf.read("vw0", t), buf.write("d", t, 1), bars.arrive("kv_done0")))
+            yield "vw_full1", t
+            queue.append(lambda t=t, s=s: (buf.read(f"k{s}", t), buf.read("vw1", t), bars.arrive("kv_done1"),
+                                           bars.arrive(f"free_k{s}")))
             if state_only:
                 continue
             yield "s_full", t
             if t:
                 yield "o_free", t - 1
-            queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s", t), buf.write("o", 2 * t, 1),
+            queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s", t), buf.write("qs", t, 1),
                                            bars.arrive("qs_done"), bars.arrive(f"free_q{s}")))
             if t + 1 < n:
                 yield from scores(t + 1)
             yield f"full_v{s}", t // ns
-            yield f"p_full{t & 1}", t >> 1
-            yield "qs_read", t
-            queue.append(lambda t=t, s=s: (buf.read(f"v{s}", t), buf.read(f"p{t & 1}", t), buf.write("o", 2 * t + 1, 1),
+            yield "p_full", t
+            queue.append(lambda t=t, s=s: (buf.read(f"v{s}", t), buf.read("p", t), buf.write("pv", t, 1),
                                            bars.arrive("pv_done")))
 
     def masks():
         for t in range(n):
-            yield f"qk_full{t & 1}", t >> 1
-            buf.read(f"a{t & 1}", t)
-            buf.write(f"p{t & 1}", t, 2)                 # the product, and the epilogue of a tile that is not all finite
+            if t:
+                yield "pv_done", t - 1
+                if odd(t - 1):
+                    yield "o_free", t - 1
+            yield "qk_full", t
+            buf.read("a", t)
             yield None
-            bars.arrive(f"p_full{t & 1}")
+            bars.arrive("qk_read")
+            buf.write("p", t, 1 + odd(t))                # the product, and the epilogue where V was not all finite
+            yield None
+            bars.arrive("p_full")
 
     def values():
         for t in range(n):
             yield f"full_v{t % ns}", t // ns
-            if t:
-                yield "kv_done", t - 1
             buf.read(f"v{t % ns}", t)
-            buf.write("vw", t, 1)
-            yield None
-            bars.arrive("vw_full")
+            for half in (0, 1):
+                if t:
+                    yield f"kv_done{half}", t - 1
+                buf.write(f"vw{half}", t, 1)
+                yield None
+                bars.arrive(f"vw_full{half}")
             if state_only:
                 bars.arrive(f"free_v{t % ns}")
 
     def outputs():
         for t in range(n):
             yield "qs_done", t
-            buf.read("o", 2 * t)
-            yield None
-            bars.arrive("qs_read")
             yield "pv_done", t
-            buf.read("o", 2 * t + 1)
-            buf.read(f"p{t & 1}", t)
+            buf.read("qs", t)
+            buf.read("pv", t)
+            yield None
+            if odd(t):
+                buf.read("p", t)
             yield None
             bars.arrive("o_free")
             buf.write(f"v{t % ns}", f"o{t}", 1)           # staged where V stood
@@ -133,7 +144,7 @@ def run(n, ns, state_only, rng):
                 buf.write("s", t, 1)
                 yield None
                 bars.arrive("s_full")
-            yield "kv_done", t
+            yield "kv_done1", t
             buf.read("d", t)
             yield None
             bars.arrive("kv_read")
