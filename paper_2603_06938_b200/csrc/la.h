@@ -11,6 +11,7 @@
 //   d value    q := k, k := q,  v := do        whose products do q^T carry the scale (a = scale), not the read
 #pragma once
 #include "internal.h"
+#include "tc05.cuh"
 
 namespace swimba {
 
@@ -62,11 +63,15 @@ __device__ __forceinline__ LaDecay la_decay(float g)
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg);
 // (bytes of one job's segment states; grows with B and with L)
 size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count);
+// Tensor map of [B, L, streams, D], rows ld apart, for boxes of 128 tokens of 64 entries of one stream.  Rows behind
+// the sequence read as zeros and are not written.
+bool la_stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int streams, int L, int B, int64_t ld);
 // The tensor-core kernel (la_tiles.cu): the head sizes it has, whether the rows are within its reach, its launches
 // (states: the pass that leaves every segment's end state).
 bool la_tiles_shape(int dtype, int N, int P);
 bool la_tiles_reach(const LaArgs &a);
 int launch_la_tiles(LaunchCtx &ctx, const LaArgs &a, bool states);
+int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states);      // its jobs of 128 values (la_wide.cu)
 // Runs the jobs: per-segment states, their chain, outputs; or outputs alone when nseg == 1.
 int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a);
 // out[t, g, :] = sum over the r heads of group g of part[t, g r + i, :], in that order.

@@ -32,7 +32,6 @@ constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
 // fit waited for instructions most of the time (9000 cycles a tile).
 constexpr int THREADS = 1024;
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 28;
-constexpr int AHEAD = 4;                     // tiles whose rows are on their way to L2
 // tensor memory columns: scores, P (bf16), Q S, P V, a D for each part of w V
 constexpr uint32_t TM_QK = 0, TM_P = 128, TM_QS = 192, TM_PV = 256, TM_KV = 320, TM_COLS = 512;
 
@@ -146,19 +145,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     if (warp == WARP_TMA) {
         // ------------------------------------------------------------------ loads, in the order in which room comes free
         const bool leader = tc::elect_one();
-        // (a load from L2 comes back in about half the time that one from HBM takes, and its room is taken that much shorter)
-        auto prefetch = [&](int t) {
-            if (t >= ntiles || !leader) return;
-            for (int o = 0; o < DK; o += 64) {
-                tc::tma_prefetch_4d(&maps.k[ji], o, h / j.rk, tile_at(t), b);
-                if (!STATE_ONLY) tc::tma_prefetch_4d(&maps.q[ji], o, h / j.rq, tile_at(t), b);
-            }
-            tc::tma_prefetch_4d(&maps.v[ji], c0, h / j.rv, tile_at(t), b);
-        };
-        for (int t = NS; t < AHEAD; ++t) prefetch(t);
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NS, at = tile_at(t);
-            prefetch(t + AHEAD);
             const uint32_t ph = ((t / NS) & 1) ^ 1;
             auto load = [&](uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int col, int stream) {
                 tc::mbar_wait(room, ph, abort_flag, d_status);
@@ -549,15 +537,6 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     if (warp == WARP_ALLOC) tc::tmem_dealloc(tmem, TM_COLS);
 }
 
-// [B, L, streams, D] rows ld apart; a box is 128 tokens of 64 entries of one stream.  Rows behind the sequence read as zeros.
-bool stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int streams, int L, int B, int64_t ld)
-{
-    const uint64_t dims[4] = {(uint64_t)D, (uint64_t)streams, (uint64_t)L, (uint64_t)B};
-    const uint64_t strides[3] = {(uint64_t)D * 2, (uint64_t)ld * 2, (uint64_t)ld * L * 2};
-    const uint32_t box[4] = {64, 1, LT, 1};
-    return encode_tmap_bf16_cached(cache, m, p, 4, dims, strides, box);
-}
-
 template <int DK, bool STATE_ONLY>
 bool run_tiles(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 {
@@ -572,6 +551,14 @@ bool run_tiles(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 }
 
 }  // namespace
+
+bool la_stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int streams, int L, int B, int64_t ld)
+{
+    const uint64_t dims[4] = {(uint64_t)D, (uint64_t)streams, (uint64_t)L, (uint64_t)B};
+    const uint64_t strides[3] = {(uint64_t)D * 2, (uint64_t)ld * 2, (uint64_t)ld * L * 2};
+    const uint32_t box[4] = {64, 1, LT, 1};
+    return encode_tmap_bf16_cached(cache, m, p, 4, dims, strides, box);
+}
 
 bool la_tiles_shape(int dtype, int N, int P)
 {
@@ -589,27 +576,32 @@ bool la_tiles_reach(const LaArgs &a)
 
 int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states)
 {
-    // jobs of one head size go in one launch
-    for (int dk : {64, 128}) {
-        LaArgs a = all;
-        Maps maps;
-        a.njobs = 0;
-        for (int i = 0; i < all.njobs; ++i) {
-            const LaJob &j = all.job[i];
-            if (j.dk != dk) continue;
-            const int n = a.njobs++;
-            a.job[n] = j;
-            if (!stream_map(ctx.tmaps, &maps.q[n], j.q, j.dk, a.H / j.rq, a.L, a.B, j.ldq) ||
-                !stream_map(ctx.tmaps, &maps.k[n], j.k, j.dk, a.H / j.rk, a.L, a.B, j.ldk) ||
-                !stream_map(ctx.tmaps, &maps.v[n], j.v, j.dv, a.H / j.rv, a.L, a.B, j.ldv) ||
-                (!states && !j.o_f32 && !stream_map(ctx.tmaps, &maps.o[n], j.o, j.dv, a.H, a.L, a.B, j.ldo)))
-                return SWIMBA_ERR_CUDA;
+    // jobs of one pair of head sizes go in one launch
+    for (int dk : {64, 128})
+        for (int dv : {64, 128}) {
+            LaArgs a = all;
+            a.njobs = 0;
+            for (int i = 0; i < all.njobs; ++i)
+                if (all.job[i].dk == dk && all.job[i].dv == dv) a.job[a.njobs++] = all.job[i];
+            if (a.njobs == 0) continue;
+            if (dv == 128) {
+                const int rc = launch_la_wide(ctx, a, states);
+                if (rc != SWIMBA_OK) return rc;
+                continue;
+            }
+            Maps maps;
+            for (int i = 0; i < a.njobs; ++i) {
+                const LaJob &j = a.job[i];
+                if (!la_stream_map(ctx.tmaps, &maps.q[i], j.q, j.dk, a.H / j.rq, a.L, a.B, j.ldq) ||
+                    !la_stream_map(ctx.tmaps, &maps.k[i], j.k, j.dk, a.H / j.rk, a.L, a.B, j.ldk) ||
+                    !la_stream_map(ctx.tmaps, &maps.v[i], j.v, j.dv, a.H / j.rv, a.L, a.B, j.ldv) ||
+                    (!states && !j.o_f32 && !la_stream_map(ctx.tmaps, &maps.o[i], j.o, j.dv, a.H, a.L, a.B, j.ldo)))
+                    return SWIMBA_ERR_CUDA;
+            }
+            const bool ok = dk == 64 ? (states ? run_tiles<64, true>(ctx, maps, a) : run_tiles<64, false>(ctx, maps, a))
+                                     : (states ? run_tiles<128, true>(ctx, maps, a) : run_tiles<128, false>(ctx, maps, a));
+            if (!ok) return SWIMBA_ERR_CUDA;
         }
-        if (a.njobs == 0) continue;
-        const bool ok = dk == 64 ? (states ? run_tiles<64, true>(ctx, maps, a) : run_tiles<64, false>(ctx, maps, a))
-                                 : (states ? run_tiles<128, true>(ctx, maps, a) : run_tiles<128, false>(ctx, maps, a));
-        if (!ok) return SWIMBA_ERR_CUDA;
-    }
     return SWIMBA_OK;
 }
 

@@ -1,0 +1,581 @@
+// Linear attention with a decay for each head on the tensor cores, heads of 128 values (bf16; 64 or 128 keys): the
+// same five steps per tile of 128 tokens as in la_tiles.cu, with all values of a head in one CTA, so that scores and masks
+// are made once.  What makes room for that in shared memory (two or three stages of Q, K and V, the bf16 state):
+//   w V   is made transposed, [DV, tokens], straight into tensor memory, half a tile's three parts at a time, and is the A
+//         operand of KV:  D = (w V)^T K
+//   S     lies in tensor memory in fp32, [DV, DK]; between two tiles it is read, rounded for QS and scaled by lambda^n,
+//         and KV adds to it
+//   O     one region: Q S^T, scaled row by row in place, then P V on top
+// Shared memory is what bounds such a tile: 7860 cycles of reads and writes for two CTAs of 64 values each against 3900 here.
+#include <algorithm>
+#include <cstddef>
+
+#include "la.h"
+#include "tc05.cuh"
+
+namespace swimba {
+
+namespace {
+
+constexpr int LT = 128;                      // tokens per tile
+constexpr int DV = 128;
+constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
+constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
+// warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 4 for the state, 8 for o
+constexpr int THREADS = 1024;
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 24;
+// tensor memory columns: scores and over them P (bf16), O, S, the parts of half a tile's w V
+constexpr uint32_t TM_QK = 0, TM_O = 128, TM_S = 256, TM_VW = 384, TM_COLS = 512;
+
+template <int DK> struct Sm {
+    static constexpr int NS = DK == 64 ? 3 : 2;           // stages of Q, K and V
+    static constexpr uint32_t QB = DK / 64 * SLAB;        // bytes of a Q or K tile
+    static constexpr uint32_t Q = 0, K = Q + NS * QB, V = K + NS * QB, S = V + NS * VB, SMALL = S + QB;
+};
+struct Small {
+    uint64_t full_q[3], full_k[3], full_v[3], free_q[3], free_k[3], free_v[3];
+    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, kv_done, vw_full, vw_done, v_read;
+    uint32_t tmem;
+    int abort_flag;
+    int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
+    alignas(16) float pow_col[32];           // factors of a score block's columns
+    float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
+    float pow[LT + 1];                       // lambda^m
+    float weight[LT];                        // of a whole tile's tokens in w V
+};
+static_assert(offsetof(Small, pow_col) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
+
+struct Maps {
+    CUtensorMap q[LA_MAX_JOBS], k[LA_MAX_JOBS], v[LA_MAX_JOBS], o[LA_MAX_JOBS];
+};
+
+__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b) { return tc::f32x2(__uint_as_float(a), __uint_as_float(b)); }
+
+// STATE_ONLY: from a zero state, and only the end state is kept (in seg).
+template <int DK, bool STATE_ONLY>
+__global__ void __launch_bounds__(THREADS, 1)
+la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs a, int *d_status)
+{
+    typedef Sm<DK> L;
+    constexpr int NS = L::NS;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Small *sm = (Small *)(smem + L::SMALL);
+    int *abort_flag = &sm->abort_flag;
+    if ((tc::smem_u32(smem) & 1023u) != 0) {       // the swizzled tiles need a 1024-byte aligned base
+        if (threadIdx.x == 0) atomicCAS(d_status, 0, SWIMBA_ERR_DEVICE_BOUNDS);
+        return;
+    }
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+
+    // the jobs on one head side by side: they read the same rows at about the same time
+    int64_t id = blockIdx.x;
+    const int ji = (int)(id % a.njobs);
+    id /= a.njobs;
+    const int nrun = STATE_ONLY ? a.nseg - 1 : a.nseg;     // (the last segment's end state enters nothing)
+    const int seg = (int)(id % nrun);                      // in the order of the walk
+    id /= nrun;
+    const int h = (int)(id % a.H), b = (int)(id / a.H);
+    const LaJob &j = a.job[ji];
+    const bool rev = j.reverse != 0;
+    // three parts where the state is a result; two (2^-16) where only the read of it is, whose copy is rounded to bf16
+    const int parts = j.s_out ? 3 : 2;
+    const int place = rev ? a.nseg - 1 - seg : seg;
+    const int t_begin = place * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    const int ntiles = (t_end - t_begin + LT - 1) / LT;
+    auto tile_at = [&](int t) { return t_begin + (rev ? ntiles - 1 - t : t) * LT; };       // first token of tile t
+    auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
+
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) {
+            tc::mbar_init(&sm->full_q[s], 1);
+            tc::mbar_init(&sm->full_k[s], 1);
+            tc::mbar_init(&sm->full_v[s], 1);
+            tc::mbar_init(&sm->free_q[s], 1);
+            tc::mbar_init(&sm->free_k[s], 1);
+            tc::mbar_init(&sm->free_v[s], STATE_ONLY || j.o_f32 ? 8 : 2);
+        }
+        sm->odd_tile[0] = sm->odd_tile[1] = 0;
+        tc::mbar_init(&sm->qk_full, 1);
+        tc::mbar_init(&sm->p_full, 8);
+        tc::mbar_init(&sm->qs_done, 1);
+        tc::mbar_init(&sm->o_scaled, 8);
+        tc::mbar_init(&sm->pv_done, 1);
+        tc::mbar_init(&sm->o_free, 8);
+        tc::mbar_init(&sm->s_full, 4);
+        tc::mbar_init(&sm->kv_done, 1);
+        tc::mbar_init(&sm->vw_full, 8);
+        tc::mbar_init(&sm->vw_done, 1);
+        tc::mbar_init(&sm->v_read, 8);
+        *abort_flag = 0;
+        tc::fence_mbar_init();
+    }
+    if (warp == WARP_ALLOC) {
+        tc::tmem_alloc(&sm->tmem, TM_COLS);
+        tc::tmem_relinquish();
+    }
+    if (warp == WARP_TMA && lane == 0) {
+        if (!STATE_ONLY) tc::prefetch_tmap(&maps.q[ji]);
+        tc::prefetch_tmap(&maps.k[ji]);
+        tc::prefetch_tmap(&maps.v[ji]);
+    }
+    grid_dep_launch();
+    grid_dep_wait();
+    const float g2 = la_log2_decay(a.log_decay[h]);
+    if (tid <= LT) sm->pow[tid] = exp2f(tid * g2);
+    else if (tid >= 256 && tid < 288) sm->pow_col[tid - 256] = exp2f((rev ? tid - 256 : 287 - tid) * g2);
+    else if (tid >= 320 && tid < 383) sm->pow_diag[tid - 320] = j.scale_p * exp2f(abs(tid - 351) * g2);
+    else if (tid >= 512 && tid < 640) sm->weight[tid - 512] = j.scale_a * exp2f((rev ? tid - 511 : 639 - tid) * g2);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = sm->tmem;
+
+    if (warp == WARP_TMA) {
+        // ------------------------------------------------------------------ loads, in the order in which room comes free
+        const bool leader = tc::elect_one();
+        for (int t = 0; t < ntiles; ++t) {
+            const int s = t % NS, at = tile_at(t);
+            const uint32_t ph = ((t / NS) & 1) ^ 1;
+            auto load = [&](uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int stream) {
+                tc::mbar_wait(room, ph, abort_flag, d_status);
+                if (leader && !*(volatile int *)abort_flag) {
+                    tc::mbar_arrive_expect_tx(full, bytes);
+                    for (uint32_t o = 0; o < bytes; o += SLAB)
+                        tc::tma_load_4d(smem + dst + o, m, full, (int)(o / SLAB) * 64, stream, at, b);
+                }
+                __syncwarp();
+            };
+            if (!STATE_ONLY) load(&sm->full_q[s], &sm->free_q[s], L::Q + s * L::QB, L::QB, &maps.q[ji], h / j.rq);
+            load(&sm->full_k[s], &sm->free_k[s], L::K + s * L::QB, L::QB, &maps.k[ji], h / j.rk);
+            load(&sm->full_v[s], &sm->free_v[s], L::V + s * VB, VB, &maps.v[ji], h / j.rv);
+        }
+        // No copy may be in flight when the CTA leaves: after an abort nobody else has waited for the last ones (those
+        // that were not issued any more never arrive, and these waits run out soon).
+        auto settle = [&](uint64_t *full, uint32_t ph) {
+            int quiet = 0;
+            if (*(volatile int *)abort_flag) tc::mbar_wait(full, ph, &quiet, d_status, 10000000ll);
+            else tc::mbar_wait(full, ph, abort_flag, d_status);
+        };
+        for (int t = max(0, ntiles - NS); t < ntiles; ++t) {
+            settle(&sm->full_k[t % NS], (t / NS) & 1);
+            if (!STATE_ONLY) settle(&sm->full_q[t % NS], (t / NS) & 1);
+            settle(&sm->full_v[t % NS], (t / NS) & 1);
+        }
+    } else if (warp == WARP_MMA) {
+        // ------------------------------------------------------------------ products
+        const bool leader = tc::elect_one();
+        constexpr uint32_t id_qk = tc::idesc_bf16(128, 128, 0, 0);      // Q x K, Q x S (all K-major)
+        constexpr uint32_t id_pv = tc::idesc_bf16(128, DV, 0, 1);       // P (TMEM) x V (MN-major)
+        constexpr uint32_t id_kv = tc::idesc_bf16(128, DK, 0, 1);       // (w V)^T (TMEM) x K (MN-major)
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t base = tc::smem_u32(smem);
+        const uint64_t dQ = tc::smem_desc_sw128(base + L::Q, 16, 1024), dK = tc::smem_desc_sw128(base + L::K, 16, 1024);
+        const uint64_t dKt = tc::smem_desc_sw128(base + L::K, SLAB, 1024), dV = tc::smem_desc_sw128(base + L::V, SLAB, 1024);
+        const uint64_t dS = tc::smem_desc_sw128(base + L::S, 16, 1024);
+        auto scores = [&](int t) {
+            const int s = t % NS;
+            const uint32_t ph = (t / NS) & 1;
+            tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
+            tc::mbar_wait(&sm->full_q[s], ph, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB));
+                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dK, s * L::QB));
+#pragma unroll
+                for (int kk = 0; kk < DK / 16; ++kk) {
+                    const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
+                    tc::mma_ss(tm + TM_QK, tc::smem_desc_advance(q, o), tc::smem_desc_advance(k, o), id_qk, kk > 0);
+                }
+                tc::mma_commit(&sm->qk_full);
+            }
+            __syncwarp();
+        };
+        auto add_half = [&](int t, int hf) {
+            const int s = t % NS;
+            tc::mbar_wait(&sm->vw_full, hf, abort_flag, d_status);        // (two phases a tile)
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, s * L::QB + hf * 8192));
+#pragma unroll 1
+                for (int p = 0; p < parts; ++p)
+#pragma unroll
+                    for (int kk = 0; kk < LT / 32; ++kk)
+                        tc::mma_ts(tm + TM_S, tm + TM_VW + p * 32 + kk * 8, tc::smem_desc_advance(k, kk * 2048), id_kv, 1);
+                tc::mma_commit(&sm->vw_done);
+                if (hf == 1) {
+                    tc::mma_commit(&sm->kv_done);
+                    tc::mma_commit(&sm->free_k[s]);
+                }
+            }
+            __syncwarp();
+        };
+        if (!STATE_ONLY && ntiles > 0) scores(0);
+        for (int t = 0; t < ntiles; ++t) {
+            const int s = t % NS;
+            const uint32_t ph = (t / NS) & 1;
+            if (STATE_ONLY) tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
+            // QS: the carried part, once the state is there and the epilogue has read the tile in front
+            tc::mbar_wait(&sm->s_full, t & 1, abort_flag, d_status);
+            if (!STATE_ONLY) {
+                if (t > 0) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+                if (leader) {
+                    const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB)), st = tc::smem_desc_fresh(dS);
+#pragma unroll
+                    for (int kk = 0; kk < DK / 16; ++kk) {
+                        const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
+                        tc::mma_ss(tm + TM_O, tc::smem_desc_advance(q, o), tc::smem_desc_advance(st, o), id_qk, kk > 0);
+                    }
+                    tc::mma_commit(&sm->qs_done);
+                    tc::mma_commit(&sm->free_q[s]);
+                }
+                __syncwarp();
+            }
+            add_half(t, 0);
+            const bool odd = !STATE_ONLY && ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
+            if (odd) add_half(t, 1);
+            if (!STATE_ONLY) {
+                // PV, on top of the scaled carried part
+                tc::mbar_wait(&sm->full_v[s], ph, abort_flag, d_status);
+                tc::mbar_wait(&sm->p_full, t & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->o_scaled, t & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+                if (leader) {
+                    const uint64_t v = tc::smem_desc_fresh(tc::smem_desc_advance(dV, s * VB));
+#pragma unroll
+                    for (int kk = 0; kk < LT / 16; ++kk)
+                        tc::mma_ts(tm + TM_O, tm + TM_QK + (kk >> 2) * 64 + (kk & 3) * 8, tc::smem_desc_advance(v, kk * 2048), id_pv, 1);
+                    tc::mma_commit(&sm->pv_done);
+                }
+                __syncwarp();
+            }
+            if (!odd) add_half(t, 1);
+            if (!STATE_ONLY && t + 1 < ntiles) {
+                // the next scores go where P stands, which the epilogue reads too if V was not all finite
+                tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
+                if (odd) tc::mbar_wait(&sm->o_free, t & 1, abort_flag, d_status);
+                scores(t + 1);
+            }
+        }
+    } else if (warp >= WARP_MASK && warp < WARP_W) {
+        // ------------------------------------------------------------------ masks: half a row of the scores per thread, its
+        // result over the first half of what it was made from
+        const int q4 = warp & 3, half = (warp - WARP_MASK) >> 2, i = q4 * 32 + lane;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_QK + half * 64;
+        const float scale_p = j.scale_p;
+        const uint32_t keep = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
+            tc::mbar_wait(&sm->qk_full, t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+#pragma unroll 1
+            for (int k = 0; k < 2; ++k) {
+                const int bl = half * 2 + k;
+                uint32_t x[32], o[16];
+                if (rev ? bl < q4 : bl > q4) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = 0u;
+                } else {
+                    tc::tmem_ld32(row + k * 32, x);
+                    tc::tmem_ld_wait();
+                    if (bl == q4) {
+                        const float *f = &sm->pow_diag[31 + lane];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float v = f[-e] * __uint_as_float(x[e]);
+                            x[e] = keep >> e & 1u ? __float_as_uint(v) : 0u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = tc::pack_bf16x2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
+                    } else {                     // a factor for the row's place before the block, one for each column's in it
+                        const float rho = scale_p * sm->pow[rev ? 32 * bl - i : i - 32 * bl - 31];
+                        const uint64_t r2 = tc::f32x2(rho, rho);
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            const float4 c = *reinterpret_cast<const float4 *>(&sm->pow_col[2 * e]);
+                            o[e] = tc::f32x2_bf16(tc::f32x2_mul(pair_of(x[2 * e], x[2 * e + 1]), tc::f32x2_mul(r2, tc::f32x2(c.x, c.y))));
+                            o[e + 1] = tc::f32x2_bf16(tc::f32x2_mul(pair_of(x[2 * e + 2], x[2 * e + 3]), tc::f32x2_mul(r2, tc::f32x2(c.z, c.w))));
+                        }
+                    }
+                }
+                tc::tmem_st16(row + k * 16, o);
+            }
+            tc::tmem_st_wait();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->p_full);
+        }
+    } else if (warp >= WARP_W && warp < WARP_STATE) {
+        // ------------------------------------------------------------------ (w V)^T: 32 values and 32 tokens of half a tile,
+        // 16 values at a time, transposed on the way from shared memory
+        const int q4 = warp & 3, tk = (warp - WARP_W) >> 2;
+        const uint64_t neg = tc::f32x2(-1.f, -1.f);
+        // this lane's row of the 8 x 8 blocks: (token octet, value octet) = (lane / 16, lane / 8 % 2), token lane % 8
+        const int tok = tk * 32 + (lane >> 4) * 8 + (lane & 7);
+        const uint32_t slab = L::V + (q4 >> 1) * SLAB, ch0 = (q4 & 1) * 4 + ((lane >> 3) & 1);
+        const uint32_t to = tmem + TM_VW + tk * 16;
+        const uint32_t base = tc::smem_u32(smem);
+        for (int t = 0; t < ntiles; ++t) {
+            const int s = t % NS, n = tile_n(t), shift = rev ? 0 : LT - n;
+            tc::mbar_wait(&sm->full_v[s], (t / NS) & 1, abort_flag, d_status);
+            const uint32_t src = base + slab + s * VB;
+            uint32_t odd = 0;
+#pragma unroll 1
+            for (int hf = 0; hf < 2; ++hf) {
+                if (2 * t + hf > 0) tc::mbar_wait(&sm->vw_done, (hf + 1) & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+                uint64_t w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int jj = hf * 64 + tk * 32 + c * 8 + (lane & 3) * 2;
+                    w[c] = tc::f32x2(jj < n ? sm->weight[jj + shift] : 0.f, jj + 1 < n ? sm->weight[jj + 1 + shift] : 0.f);
+                }
+#pragma unroll 1
+                for (int lg = 0; lg < 2; ++lg) {
+                    uint32_t r[8], p[3][8];
+                    const uint32_t at = src + tc::sw128_offset(hf * 64 + tok, ch0 + lg * 2);
+                    tc::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]);
+                    tc::ldmatrix_x4_trans(at + 16 * 128, r[4], r[5], r[6], r[7]);      // (16 tokens on: same swizzle)
+                    if (!STATE_ONLY && hf == 0) {      // the other half too: PV must find no infinity and no NaN in V
+                        uint32_t u[8];
+                        tc::ldmatrix_x4_trans(at + 64 * 128, u[0], u[1], u[2], u[3]);
+                        tc::ldmatrix_x4_trans(at + 80 * 128, u[4], u[5], u[6], u[7]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)    // (an exponent of all ones carries into the sign's place)
+                            odd |= ((r[e] & 0x7f807f80u) + 0x00800080u) | ((u[e] & 0x7f807f80u) + 0x00800080u);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        uint64_t x = tc::f32x2_mul(w[e >> 1], pair_of(r[e] << 16, r[e] & 0xffff0000u));
+                        p[0][e] = tc::f32x2_bf16(x);
+                        x = tc::f32x2_fma(neg, pair_of(p[0][e] << 16, p[0][e] & 0xffff0000u), x);
+                        p[1][e] = tc::f32x2_bf16(x);
+                        x = tc::f32x2_fma(neg, pair_of(p[1][e] << 16, p[1][e] & 0xffff0000u), x);
+                        p[2][e] = tc::f32x2_bf16(x);
+                    }
+                    const uint32_t dst = to + ((uint32_t)(q4 * 32 + lg * 16) << 16);
+                    tc::tmem_st_16x128b_x4(dst, p[0]);
+                    tc::tmem_st_16x128b_x4(dst + 32, p[1]);
+                    if (parts == 3) tc::tmem_st_16x128b_x4(dst + 64, p[2]);
+                }
+                tc::tmem_st_wait();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (!STATE_ONLY && __any_sync(0xffffffffu, (odd & 0x80008000u) != 0)) {
+                    // seen with the first half; what is not finite gives way to zeros once both halves have been read, and
+                    // PV waits for that
+                    if (hf == 0) ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
+                    else {
+#pragma unroll 1
+                        for (int i = 0; i < 64; ++i) {
+                            unsigned short *e = reinterpret_cast<unsigned short *>(
+                                smem + slab + s * VB + tc::sw128_offset((i >> 5) * 64 + tk * 32 + (i & 31), (q4 & 1) * 4 + (lane >> 3))) + (lane & 7);
+                            if ((*e & 0x7f80) == 0x7f80) *e = 0;
+                        }
+                        tc::fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                }
+                if (lane == 0) tc::mbar_arrive(&sm->vw_full);
+            }
+            if (lane == 0) tc::mbar_arrive(STATE_ONLY ? &sm->free_v[s] : &sm->v_read);
+        }
+    } else if (warp >= WARP_STATE && warp < WARP_O) {
+        // ------------------------------------------------------------------ the state, a value's row per thread: between two
+        // tiles its bf16 copy for QS goes to shared memory and it is scaled where it stands
+        const int q4 = warp & 3, d = q4 * 32 + lane;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_S;
+        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * DV;
+        const int64_t at0 = j.transposed ? d : (int64_t)d * DK, step = j.transposed ? DV : 1;
+        const float *from = STATE_ONLY ? nullptr
+                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
+                            : j.s_in   ? j.s_in + bh * ssize
+                                       : nullptr;
+        for (int t = 0; t < ntiles; ++t) {
+            const float dec = sm->pow[tile_n(t)];
+            const uint64_t dec2 = tc::f32x2(dec, dec);
+            if (t > 0) {
+                tc::mbar_wait(&sm->kv_done, (t - 1) & 1, abort_flag, d_status);
+                if (!STATE_ONLY) tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+            }
+#pragma unroll 1
+            for (int c = 0; c < DK; c += 32) {
+                uint32_t x[32];
+                if (t > 0) {
+                    tc::tmem_ld32(row + c, x);
+                    tc::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
+                }
+                if (!STATE_ONLY) {
+                    uint8_t *dst = smem + L::S + (c >> 6) * SLAB;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        *reinterpret_cast<uint4 *>(dst + tc::sw128_offset(d, ((c & 63) + e) >> 3)) =
+                            make_uint4(tc::f32x2_bf16(pair_of(x[e], x[e + 1])), tc::f32x2_bf16(pair_of(x[e + 2], x[e + 3])),
+                                       tc::f32x2_bf16(pair_of(x[e + 4], x[e + 5])), tc::f32x2_bf16(pair_of(x[e + 6], x[e + 7])));
+                }
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const float2 v = tc::f32x2_get(tc::f32x2_mul(dec2, pair_of(x[e], x[e + 1])));
+                    x[e] = __float_as_uint(v.x);
+                    x[e + 1] = __float_as_uint(v.y);
+                }
+                __syncwarp();
+                tc::tmem_st32(row + c, x);
+            }
+            tc::tmem_st_wait();
+            tc::fence_proxy_async_smem();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->s_full);
+        }
+        float *to = STATE_ONLY ? j.seg + (bh * a.nseg + seg + 1) * ssize
+                    : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
+        if (to && ntiles > 0) {
+            tc::mbar_wait(&sm->kv_done, (ntiles - 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < DK; c += 32) {
+                uint32_t x[32];
+                __syncwarp();
+                tc::tmem_ld32(row + c, x);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) to[at0 + (c + e) * step] = __uint_as_float(x[e]);
+            }
+        }
+    } else if (warp >= WARP_O) {
+        // ------------------------------------------------------------------ o: half a row per thread, staged where V stood
+        const int q4 = warp & 3, half = (warp - WARP_O) >> 2, r = q4 * 32 + lane;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16), mine = row + TM_O + half * 64;
+        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
+            const int s = t % NS, n = tile_n(t), at = tile_at(t);
+            const float w = r < n ? j.scale_c * sm->pow[rev ? n - 1 - r : r + 1] : 0.f;
+            const uint64_t w2 = tc::f32x2(w, w);
+            tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 32) {   // the carried part, for PV to add to
+                uint32_t x[32];
+                tc::tmem_ld32(mine + c, x);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const float2 v = tc::f32x2_get(tc::f32x2_mul(w2, pair_of(x[e], x[e + 1])));
+                    x[e] = __float_as_uint(v.x);
+                    x[e + 1] = __float_as_uint(v.y);
+                }
+                tc::tmem_st32(mine + c, x);
+            }
+            tc::tmem_st_wait();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->o_scaled);
+            tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            tc::mbar_wait(&sm->v_read, t & 1, abort_flag, d_status);      // (w V has been made of all of V)
+            const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
+            uint8_t *stage = smem + L::V + s * VB + half * SLAB;
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t y[32];
+                __syncwarp();
+                tc::tmem_ld32(mine + c, y);
+                tc::tmem_ld_wait();
+                if (odd) {                       // what is not finite, for the rows that see it
+                    const __nv_bfloat16 *v = (const __nv_bfloat16 *)j.v + ((int64_t)b * a.L + at) * j.ldv +
+                                             (int64_t)(h / j.rv) * DV + half * 64 + c;
+#pragma unroll 1
+                    for (int jj = 0; jj < n; ++jj) {
+                        uint32_t p[8], pw = 0;   // (the eight columns that hold token jj)
+                        __syncwarp();
+                        tc::tmem_ld8(row + TM_QK + (jj >> 6) * 64 + (jj >> 4 & 3) * 8, p);
+                        tc::tmem_ld_wait();
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) pw = z == (jj >> 1 & 7) ? p[z] : pw;
+                        const float pf = __uint_as_float(jj & 1 ? pw & 0xffff0000u : pw << 16);
+                        if (rev ? jj >= r : jj <= r) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const float u = __bfloat162float(v[jj * j.ldv + e]);
+                                if (!isfinite(u)) y[e] = __float_as_uint(fmaf(pf, u, __uint_as_float(y[e])));
+                            }
+                        }
+                    }
+                }
+                if (c == 32) {                   // everything in tensor memory has been read
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&sm->o_free);
+                }
+                if (j.o_f32) {
+                    if (r < n) {
+                        uint4 *p = reinterpret_cast<uint4 *>((float *)j.o + ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * DV + half * 64 + c);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        *reinterpret_cast<uint4 *>(stage + tc::sw128_offset(r, (c + e) >> 3)) =
+                            make_uint4(tc::f32x2_bf16(pair_of(y[e], y[e + 1])), tc::f32x2_bf16(pair_of(y[e + 2], y[e + 3])),
+                                       tc::f32x2_bf16(pair_of(y[e + 4], y[e + 5])), tc::f32x2_bf16(pair_of(y[e + 6], y[e + 7])));
+                }
+            }
+            if (j.o_f32) {
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm->free_v[s]);
+                continue;
+            }
+            tc::fence_proxy_async_smem();
+            tc::named_bar_sync(1 + half, 128);
+            if (q4 == 0) {                       // (rows behind the sequence are clipped by the tensor map)
+                if (tc::elect_one()) {
+                    tc::tma_store_4d(&maps.o[ji], stage, half * 64, h, at, b);
+                    tc::bulk_commit_group();
+                    tc::bulk_wait_read_all();
+                    tc::mbar_arrive(&sm->free_v[s]);
+                }
+                __syncwarp();
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == WARP_ALLOC) tc::tmem_dealloc(tmem, TM_COLS);
+}
+
+template <int DK, bool STATE_ONLY>
+bool run_wide(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
+{
+    const size_t smem = Sm<DK>::SMALL + sizeof(Small);
+    if (!ensure_dynamic_smem((const void *)la_wide_kernel<DK, STATE_ONLY>, smem)) return false;
+    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? a.nseg - 1 : a.nseg);
+    ctx.begin(STATE_ONLY ? STAGE_LA_STATES : STAGE_LA_TILES);
+    launch_kernel(la_wide_kernel<DK, STATE_ONLY>, dim3((unsigned)n), dim3(THREADS), smem, ctx.stream, true, maps, a,
+                  ctx.d_status);
+    ctx.end();
+    return cudaGetLastError() == cudaSuccess;
+}
+
+}  // namespace
+
+int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states)
+{
+    Maps maps;
+    for (int i = 0; i < a.njobs; ++i) {
+        const LaJob &j = a.job[i];
+        if (!la_stream_map(ctx.tmaps, &maps.q[i], j.q, j.dk, a.H / j.rq, a.L, a.B, j.ldq) ||
+            !la_stream_map(ctx.tmaps, &maps.k[i], j.k, j.dk, a.H / j.rk, a.L, a.B, j.ldk) ||
+            !la_stream_map(ctx.tmaps, &maps.v[i], j.v, j.dv, a.H / j.rv, a.L, a.B, j.ldv) ||
+            (!states && !j.o_f32 && !la_stream_map(ctx.tmaps, &maps.o[i], j.o, j.dv, a.H, a.L, a.B, j.ldo)))
+            return SWIMBA_ERR_CUDA;
+    }
+    const bool ok = a.job[0].dk == 64 ? (states ? run_wide<64, true>(ctx, maps, a) : run_wide<64, false>(ctx, maps, a))
+                                      : (states ? run_wide<128, true>(ctx, maps, a) : run_wide<128, false>(ctx, maps, a));
+    return ok ? SWIMBA_OK : SWIMBA_ERR_CUDA;
+}
+
+}  // namespace swimba

@@ -319,9 +319,9 @@ namespace {
 constexpr int LA_STEP_SEG = 64, LA_TILE_SEG = 128;
 // The most segments a sequence is cut into: token by token, as many as give every SM two blocks; by tiles, as many
 // as fill two waves.
-int la_most(int B, int H, int N, int P, int njobs, int sm_count)
+int la_most(bool tiles, int B, int H, int N, int P, int njobs, int sm_count)
 {
-    const int64_t blocks = (int64_t)njobs * B * H * ceil_div(std::max(N, P), LA_COLS);
+    const int64_t blocks = (int64_t)njobs * B * H * (tiles ? 1 : ceil_div(std::max(N, P), LA_COLS));
     return (int)std::max<int64_t>(1, 2 * sm_count / blocks);
 }
 }  // namespace
@@ -329,7 +329,7 @@ int la_most(int B, int H, int N, int P, int njobs, int sm_count)
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg)
 {
     const bool tiles = la_tiles_shape(dtype, N, P);
-    const int most = la_most(B, H, N, P, njobs, sm_count);
+    const int most = la_most(tiles, B, H, N, P, njobs, sm_count);
     if (!tiles) {
         const int len = std::max(LA_STEP_SEG, ceil_div(ceil_div(L, most), 16) * 16);
         *seg_len = std::min(len, L);
@@ -339,7 +339,7 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
     // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states
     // (about 0.6 of a tile each) with what two more launches take (about 6 tiles).
     const int nt = ceil_div(L, LA_TILE_SEG);
-    const int64_t items = (int64_t)njobs * B * H * ceil_div(std::max(N, P), LA_COLS);
+    const int64_t items = (int64_t)njobs * B * H;
     double best = 1e30;
     for (int n = 1; n <= std::min(most, nt); ++n) {
         const int len = ceil_div(nt, n), ns = ceil_div(nt, len);
@@ -359,7 +359,7 @@ size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs,
     const bool tiles = la_tiles_shape(dtype, N, P);
     int64_t most = 0;
     for (int b = 1; b <= B; ++b) {
-        const int n = std::min(la_most(b, H, N, P, njobs, sm_count), ceil_div(L, tiles ? LA_TILE_SEG : LA_STEP_SEG));
+        const int n = std::min(la_most(tiles, b, H, N, P, njobs, sm_count), ceil_div(L, tiles ? LA_TILE_SEG : LA_STEP_SEG));
         if (n == 1) break;
         most = std::max<int64_t>(most, (int64_t)b * n);
     }

@@ -1,4 +1,4 @@
-"""The waits of the linear-attention tile kernel, on the CPU: its warps as coroutines over counted barriers, run in random
+"""The waits of the linear-attention tile kernels, on the CPU: their warps as coroutines over counted barriers, run in random
 orders.  Every wait ends, no barrier gets two phases ahead of a waiter (parities would alias), and no buffer is written while
 its last contents are still to be read."""
 import random
@@ -149,7 +149,137 @@ def run(n, ns, state_only, rng):
             yield None
             bars.arrive("kv_read")
 
-    live = [[g, next(g, "end")] for g in ([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]))]
+    drive([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]), bars, async_ops, rng)
+
+
+def run_wide(n, ns, state_only, rng):
+    need = {f"{k}_{x}{s}": 1 for s in range(ns) for k in ("full", "free") for x in "qkv"}
+    need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "kv_done", "vw_full",
+                                "vw_done", "v_read")})
+    bars, buf = Bars(need), Buffers()
+    odd = lambda t: not state_only and t % 3 == 1
+    async_ops = []
+
+    def tma():
+        for t in range(n):
+            s = t % ns
+            for x in "kv" if state_only else "qkv":
+                if t >= ns:
+                    yield f"free_{x}{s}", t // ns - 1
+                readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 2}[x]
+                async_ops.append([lambda x=x, s=s, t=t, r=readers: (buf.write(f"{x}{s}", t, r), bars.arrive(f"full_{x}{s}"))])
+
+    def mma():
+        queue = []
+        async_ops.append(queue)
+
+        def scores(t):
+            yield f"full_k{t % ns}", t // ns
+            yield f"full_q{t % ns}", t // ns
+            queue.append(lambda: (buf.read(f"k{t % ns}", t), buf.read(f"q{t % ns}", t), buf.write("qk", ("a", t), 1),
+                                  bars.arrive("qk_full")))
+
+        def half(t, hf):
+            yield "vw_full", 2 * t + hf
+            if hf:
+                queue.append(lambda: (buf.read("vw", 2 * t + 1), buf.read(f"k{t % ns}", t), buf.read("s_scaled", t),
+                                      buf.write("s", t + 1, 1), bars.arrive("vw_done"), bars.arrive("kv_done"),
+                                      bars.arrive(f"free_k{t % ns}")))
+            else:
+                queue.append(lambda: (buf.read("vw", 2 * t), bars.arrive("vw_done")))
+        if not state_only and n:
+            yield from scores(0)
+        for t in range(n):
+            s = t % ns
+            if state_only:
+                yield f"full_k{s}", t // ns
+            yield "s_full", t
+            if not state_only:
+                if t:
+                    yield "o_free", t - 1
+                queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s16", t), buf.write("o", ("s", t), 1),
+                                               bars.arrive("qs_done"), bars.arrive(f"free_q{s}")))
+            yield from half(t, 0)
+            if odd(t):
+                yield from half(t, 1)
+            if not state_only:
+                yield f"full_v{s}", t // ns
+                yield "p_full", t
+                yield "o_scaled", t
+                queue.append(lambda t=t, s=s: (buf.read(f"v{s}", ("z", t) if odd(t) else t), buf.read("qk", ("p", t)),
+                                               buf.read("o", ("w", t)), buf.write("o", ("o", t), 1), bars.arrive("pv_done")))
+            if not odd(t):
+                yield from half(t, 1)
+            if not state_only and t + 1 < n:
+                yield "pv_done", t
+                if odd(t):
+                    yield "o_free", t
+                yield from scores(t + 1)
+
+    def masks():
+        for t in range(n):
+            yield "qk_full", t
+            buf.read("qk", ("a", t))
+            buf.write("qk", ("p", t), 1 + odd(t))
+            yield None
+            bars.arrive("p_full")
+
+    def values():
+        for t in range(n):
+            yield f"full_v{t % ns}", t // ns
+            for hf in (0, 1):
+                if 2 * t + hf:
+                    yield "vw_done", 2 * t + hf - 1
+                assert buf.v[f"v{t % ns}"][0] == t, "w V from what replaced V"
+                buf.write("vw", 2 * t + hf, 1)
+                yield None
+                if hf:
+                    if odd(t):                            # what is not finite gives way to zeros
+                        buf.read(f"v{t % ns}", t)
+                        assert buf.v[f"v{t % ns}"][1] == 1
+                        buf.v[f"v{t % ns}"] = [("z", t), 1]
+                    else:
+                        buf.read(f"v{t % ns}", t)
+                bars.arrive("vw_full")
+            bars.arrive(f"free_v{t % ns}" if state_only else "v_read")
+
+    def outputs():
+        for t in range(n):
+            yield "qs_done", t
+            buf.read("o", ("s", t))
+            buf.write("o", ("w", t), 1)
+            yield None
+            bars.arrive("o_scaled")
+            yield "pv_done", t
+            yield "v_read", t
+            buf.read("o", ("o", t))
+            yield None
+            if odd(t):
+                buf.read("qk", ("p", t))
+            bars.arrive("o_free")
+            buf.write(f"v{t % ns}", f"o{t}", 1)
+            yield None
+            buf.read(f"v{t % ns}", f"o{t}")
+            bars.arrive(f"free_v{t % ns}")
+
+    def state():
+        for t in range(n):
+            if t:
+                yield "kv_done", t - 1
+                buf.read("s", t)
+                if not state_only:
+                    yield "qs_done", t - 1
+            buf.write("s_scaled", t, 1)
+            if not state_only:
+                buf.write("s16", t, 1)
+            yield None
+            bars.arrive("s_full")
+
+    drive([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]), bars, async_ops, rng)
+
+
+def drive(roles, bars, async_ops, rng):
+    live = [[g, next(g, "end")] for g in roles]
     live = [x for x in live if x[1] != "end"]
     while live or any(async_ops):
         steps = [x for x in live if x[1] is None or bars.ready(*x[1])]
@@ -172,3 +302,4 @@ def test_every_wait_ends_and_no_buffer_is_lost(n, ns, state_only):
     rng = random.Random(n * 10 + ns)
     for _ in range(60):
         run(n, ns, state_only, rng)
+        run_wide(n, ns, state_only, rng)
