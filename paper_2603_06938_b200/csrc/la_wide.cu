@@ -24,17 +24,18 @@ constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
 // warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 4 for the state, 8 for o
 constexpr int THREADS = 1024;
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 24;
-// tensor memory columns: scores and over them P (bf16), O, S, the parts of half a tile's w V
+// tensor memory columns: scores and over them P (bf16), O, S, a ring of four parts of half a tile's w V
 constexpr uint32_t TM_QK = 0, TM_O = 128, TM_S = 256, TM_VW = 384, TM_COLS = 512;
 
 template <int DK> struct Sm {
-    static constexpr int NS = DK == 64 ? 3 : 2;           // stages of Q, K and V
+    // stages: a Q tile is free early in its step, a K tile half way, a V tile when o, staged in its place, is on its way
+    static constexpr int NQ = DK == 64 ? 2 : 1, NK = DK == 64 ? 3 : 2, NV = 3;
     static constexpr uint32_t QB = DK / 64 * SLAB;        // bytes of a Q or K tile
-    static constexpr uint32_t Q = 0, K = Q + NS * QB, V = K + NS * QB, S = V + NS * VB, SMALL = S + QB;
+    static constexpr uint32_t Q = 0, K = Q + NQ * QB, V = K + NK * QB, S = V + NV * VB, SMALL = S + QB;
 };
 struct Small {
-    uint64_t full_q[3], full_k[3], full_v[3], free_q[3], free_k[3], free_v[3];
-    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, kv_done, vw_full, vw_done, v_read;
+    uint64_t full_q[2], full_k[3], full_v[3], free_q[2], free_k[3], free_v[3];
+    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, kv_done, vw_full[2], vw_done[4];
     uint32_t tmem;
     int abort_flag;
     int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
@@ -57,7 +58,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs a, int *d_status)
 {
     typedef Sm<DK> L;
-    constexpr int NS = L::NS;
+    constexpr int NQ = L::NQ, NK = L::NK, NV = L::NV;
     extern __shared__ __align__(1024) uint8_t smem[];
     Small *sm = (Small *)(smem + L::SMALL);
     int *abort_flag = &sm->abort_flag;
@@ -86,14 +87,19 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
 
     if (tid == 0) {
-        for (int s = 0; s < NS; ++s) {
+        for (int s = 0; s < NQ; ++s) {
             tc::mbar_init(&sm->full_q[s], 1);
-            tc::mbar_init(&sm->full_k[s], 1);
-            tc::mbar_init(&sm->full_v[s], 1);
             tc::mbar_init(&sm->free_q[s], 1);
+        }
+        for (int s = 0; s < NK; ++s) {
+            tc::mbar_init(&sm->full_k[s], 1);
             tc::mbar_init(&sm->free_k[s], 1);
+        }
+        for (int s = 0; s < NV; ++s) {
+            tc::mbar_init(&sm->full_v[s], 1);
             tc::mbar_init(&sm->free_v[s], STATE_ONLY || j.o_f32 ? 8 : 2);
         }
+        for (int s = 0; s < 4; ++s) tc::mbar_init(&sm->vw_done[s], 1);
         sm->odd_tile[0] = sm->odd_tile[1] = 0;
         tc::mbar_init(&sm->qk_full, 1);
         tc::mbar_init(&sm->p_full, 8);
@@ -103,9 +109,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         tc::mbar_init(&sm->o_free, 8);
         tc::mbar_init(&sm->s_full, 4);
         tc::mbar_init(&sm->kv_done, 1);
-        tc::mbar_init(&sm->vw_full, 8);
-        tc::mbar_init(&sm->vw_done, 1);
-        tc::mbar_init(&sm->v_read, 8);
+        tc::mbar_init(&sm->vw_full[0], 8);
+        tc::mbar_init(&sm->vw_full[1], 8);
         *abort_flag = 0;
         tc::fence_mbar_init();
     }
@@ -133,21 +138,24 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     if (warp == WARP_TMA) {
         // ------------------------------------------------------------------ loads, in the order in which room comes free
         const bool leader = tc::elect_one();
-        for (int t = 0; t < ntiles; ++t) {
-            const int s = t % NS, at = tile_at(t);
-            const uint32_t ph = ((t / NS) & 1) ^ 1;
-            auto load = [&](uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int stream) {
-                tc::mbar_wait(room, ph, abort_flag, d_status);
-                if (leader && !*(volatile int *)abort_flag) {
-                    tc::mbar_arrive_expect_tx(full, bytes);
-                    for (uint32_t o = 0; o < bytes; o += SLAB)
-                        tc::tma_load_4d(smem + dst + o, m, full, (int)(o / SLAB) * 64, stream, at, b);
-                }
-                __syncwarp();
-            };
-            if (!STATE_ONLY) load(&sm->full_q[s], &sm->free_q[s], L::Q + s * L::QB, L::QB, &maps.q[ji], h / j.rq);
-            load(&sm->full_k[s], &sm->free_k[s], L::K + s * L::QB, L::QB, &maps.k[ji], h / j.rk);
-            load(&sm->full_v[s], &sm->free_v[s], L::V + s * VB, VB, &maps.v[ji], h / j.rv);
+        auto load = [&](int t, int ns, uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int stream) {
+            if (t >= ntiles) return;
+            const int st = t % ns;
+            tc::mbar_wait(&room[st], ((t / ns) & 1) ^ 1, abort_flag, d_status);
+            if (leader && !*(volatile int *)abort_flag) {
+                tc::mbar_arrive_expect_tx(&full[st], bytes);
+                for (uint32_t o = 0; o < bytes; o += SLAB)
+                    tc::tma_load_4d(smem + dst + st * bytes + o, m, &full[st], (int)(o / SLAB) * 64, stream, tile_at(t), b);
+            }
+            __syncwarp();
+        };
+        auto load_q = [&](int t) { if (!STATE_ONLY) load(t, NQ, sm->full_q, sm->free_q, L::Q, L::QB, &maps.q[ji], h / j.rq); };
+        auto load_k = [&](int t) { load(t, NK, sm->full_k, sm->free_k, L::K, L::QB, &maps.k[ji], h / j.rk); };
+        auto load_v = [&](int t) { load(t, NV, sm->full_v, sm->free_v, L::V, VB, &maps.v[ji], h / j.rv); };
+        for (int t = -NV; t < ntiles; ++t) {
+            if (t + NQ >= 0) load_q(t + NQ);
+            if (t + NK >= 0) load_k(t + NK);
+            load_v(t + NV);
         }
         // No copy may be in flight when the CTA leaves: after an abort nobody else has waited for the last ones (those
         // that were not issued any more never arrive, and these waits run out soon).
@@ -156,11 +164,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             if (*(volatile int *)abort_flag) tc::mbar_wait(full, ph, &quiet, d_status, 10000000ll);
             else tc::mbar_wait(full, ph, abort_flag, d_status);
         };
-        for (int t = max(0, ntiles - NS); t < ntiles; ++t) {
-            settle(&sm->full_k[t % NS], (t / NS) & 1);
-            if (!STATE_ONLY) settle(&sm->full_q[t % NS], (t / NS) & 1);
-            settle(&sm->full_v[t % NS], (t / NS) & 1);
-        }
+        if (!STATE_ONLY)
+            for (int t = max(0, ntiles - NQ); t < ntiles; ++t) settle(&sm->full_q[t % NQ], (t / NQ) & 1);
+        for (int t = max(0, ntiles - NK); t < ntiles; ++t) settle(&sm->full_k[t % NK], (t / NK) & 1);
+        for (int t = max(0, ntiles - NV); t < ntiles; ++t) settle(&sm->full_v[t % NV], (t / NV) & 1);
     } else if (warp == WARP_MMA) {
         // ------------------------------------------------------------------ products
         const bool leader = tc::elect_one();
@@ -173,14 +180,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const uint64_t dKt = tc::smem_desc_sw128(base + L::K, SLAB, 1024), dV = tc::smem_desc_sw128(base + L::V, SLAB, 1024);
         const uint64_t dS = tc::smem_desc_sw128(base + L::S, 16, 1024);
         auto scores = [&](int t) {
-            const int s = t % NS;
-            const uint32_t ph = (t / NS) & 1;
-            tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
-            tc::mbar_wait(&sm->full_q[s], ph, abort_flag, d_status);
+            tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->full_q[t % NQ], (t / NQ) & 1, abort_flag, d_status);
             tc::tc_fence_after();
             if (leader) {
-                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB));
-                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dK, s * L::QB));
+                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, t % NQ * L::QB));
+                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dK, t % NK * L::QB));
 #pragma unroll
                 for (int kk = 0; kk < DK / 16; ++kk) {
                     const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
@@ -190,70 +195,68 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             __syncwarp();
         };
-        auto add_half = [&](int t, int hf) {
-            const int s = t % NS;
-            tc::mbar_wait(&sm->vw_full, hf, abort_flag, d_status);        // (two phases a tile)
-            tc::tc_fence_after();
-            if (leader) {
-                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, s * L::QB + hf * 8192));
-#pragma unroll 1
-                for (int p = 0; p < parts; ++p)
-#pragma unroll
-                    for (int kk = 0; kk < LT / 32; ++kk)
-                        tc::mma_ts(tm + TM_S, tm + TM_VW + p * 32 + kk * 8, tc::smem_desc_advance(k, kk * 2048), id_kv, 1);
-                tc::mma_commit(&sm->vw_done);
-                if (hf == 1) {
-                    tc::mma_commit(&sm->kv_done);
-                    tc::mma_commit(&sm->free_k[s]);
-                }
-            }
-            __syncwarp();
-        };
         if (!STATE_ONLY && ntiles > 0) scores(0);
+        int unit = 0;                            // parts of half tiles multiplied so far
         for (int t = 0; t < ntiles; ++t) {
-            const int s = t % NS;
-            const uint32_t ph = (t / NS) & 1;
-            if (STATE_ONLY) tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
-            // QS: the carried part, once the state is there and the epilogue has read the tile in front
-            tc::mbar_wait(&sm->s_full, t & 1, abort_flag, d_status);
-            if (!STATE_ONLY) {
+            if (STATE_ONLY) {
+                tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
+            } else {
+                // QS: the carried part, once the state is there and the epilogue has read the tile in front
+                tc::mbar_wait(&sm->s_full, t & 1, abort_flag, d_status);
                 if (t > 0) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 if (leader) {
-                    const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, s * L::QB)), st = tc::smem_desc_fresh(dS);
+                    const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, t % NQ * L::QB)), st = tc::smem_desc_fresh(dS);
 #pragma unroll
                     for (int kk = 0; kk < DK / 16; ++kk) {
                         const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
                         tc::mma_ss(tm + TM_O, tc::smem_desc_advance(q, o), tc::smem_desc_advance(st, o), id_qk, kk > 0);
                     }
                     tc::mma_commit(&sm->qs_done);
-                    tc::mma_commit(&sm->free_q[s]);
+                    tc::mma_commit(&sm->free_q[t % NQ]);
                 }
                 __syncwarp();
             }
-            add_half(t, 0);
-            const bool odd = !STATE_ONLY && ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
-            if (odd) add_half(t, 1);
-            if (!STATE_ONLY) {
-                // PV, on top of the scaled carried part
-                tc::mbar_wait(&sm->full_v[s], ph, abort_flag, d_status);
-                tc::mbar_wait(&sm->p_full, t & 1, abort_flag, d_status);
-                tc::mbar_wait(&sm->o_scaled, t & 1, abort_flag, d_status);
+            // KV, by halves of the tile and their parts
+#pragma unroll 1
+            for (int hf = 0; hf < 2; ++hf) {
+                tc::mbar_wait(&sm->vw_full[hf], t & 1, abort_flag, d_status);
                 tc::tc_fence_after();
-                if (leader) {
-                    const uint64_t v = tc::smem_desc_fresh(tc::smem_desc_advance(dV, s * VB));
+                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + hf * 8192));
+#pragma unroll 1
+                for (int p = 0; p < parts; ++p, ++unit) {
+                    if (leader) {
 #pragma unroll
-                    for (int kk = 0; kk < LT / 16; ++kk)
-                        tc::mma_ts(tm + TM_O, tm + TM_QK + (kk >> 2) * 64 + (kk & 3) * 8, tc::smem_desc_advance(v, kk * 2048), id_pv, 1);
-                    tc::mma_commit(&sm->pv_done);
+                        for (int kk = 0; kk < LT / 32; ++kk)
+                            tc::mma_ts(tm + TM_S, tm + TM_VW + (unit & 3) * 32 + kk * 8, tc::smem_desc_advance(k, kk * 2048), id_kv,
+                                       !STATE_ONLY || t + hf + p + kk > 0);
+                        tc::mma_commit(&sm->vw_done[unit & 3]);
+                    }
+                }
+                if (leader && hf == 1) {
+                    if (!STATE_ONLY || t == ntiles - 1) tc::mma_commit(&sm->kv_done);
+                    tc::mma_commit(&sm->free_k[t % NK]);
                 }
                 __syncwarp();
             }
-            if (!odd) add_half(t, 1);
-            if (!STATE_ONLY && t + 1 < ntiles) {
+            if (STATE_ONLY) continue;
+            // PV, on top of the scaled carried part (and behind KV: by then w V has been made of all of V, where o is staged)
+            tc::mbar_wait(&sm->full_v[t % NV], (t / NV) & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->p_full, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->o_scaled, t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t v = tc::smem_desc_fresh(tc::smem_desc_advance(dV, t % NV * VB));
+#pragma unroll
+                for (int kk = 0; kk < LT / 16; ++kk)
+                    tc::mma_ts(tm + TM_O, tm + TM_QK + (kk >> 2) * 64 + (kk & 3) * 8, tc::smem_desc_advance(v, kk * 2048), id_pv, 1);
+                tc::mma_commit(&sm->pv_done);
+            }
+            __syncwarp();
+            if (t + 1 < ntiles) {
                 // the next scores go where P stands, which the epilogue reads too if V was not all finite
                 tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
-                if (odd) tc::mbar_wait(&sm->o_free, t & 1, abort_flag, d_status);
+                if (((volatile int *)sm->odd_tile)[t & 1] == t + 1) tc::mbar_wait(&sm->o_free, t & 1, abort_flag, d_status);
                 scores(t + 1);
             }
         }
@@ -314,20 +317,21 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const uint32_t slab = L::V + (q4 >> 1) * SLAB, ch0 = (q4 & 1) * 4 + ((lane >> 3) & 1);
         const uint32_t to = tmem + TM_VW + tk * 16;
         const uint32_t base = tc::smem_u32(smem);
+        int unit = 0;                            // parts of half tiles made so far
         for (int t = 0; t < ntiles; ++t) {
-            const int s = t % NS, n = tile_n(t), shift = rev ? 0 : LT - n;
-            tc::mbar_wait(&sm->full_v[s], (t / NS) & 1, abort_flag, d_status);
+            const int s = t % NV, n = tile_n(t), shift = rev ? 0 : LT - n;
+            // (states alone: every tile's additions as they are at the end of the walk)
+            const float tail = STATE_ONLY ? exp2f((rev ? tile_at(t) - t_begin : t_end - tile_at(t) - n) * g2) : 1.f;
+            tc::mbar_wait(&sm->full_v[s], (t / NV) & 1, abort_flag, d_status);
             const uint32_t src = base + slab + s * VB;
             uint32_t odd = 0;
 #pragma unroll 1
             for (int hf = 0; hf < 2; ++hf) {
-                if (2 * t + hf > 0) tc::mbar_wait(&sm->vw_done, (hf + 1) & 1, abort_flag, d_status);
-                tc::tc_fence_after();
                 uint64_t w[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int jj = hf * 64 + tk * 32 + c * 8 + (lane & 3) * 2;
-                    w[c] = tc::f32x2(jj < n ? sm->weight[jj + shift] : 0.f, jj + 1 < n ? sm->weight[jj + 1 + shift] : 0.f);
+                    w[c] = tc::f32x2(jj < n ? tail * sm->weight[jj + shift] : 0.f, jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f);
                 }
 #pragma unroll 1
                 for (int lg = 0; lg < 2; ++lg) {
@@ -353,9 +357,16 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                         p[2][e] = tc::f32x2_bf16(x);
                     }
                     const uint32_t dst = to + ((uint32_t)(q4 * 32 + lg * 16) << 16);
-                    tc::tmem_st_16x128b_x4(dst, p[0]);
-                    tc::tmem_st_16x128b_x4(dst + 32, p[1]);
-                    if (parts == 3) tc::tmem_st_16x128b_x4(dst + 64, p[2]);
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) {
+                        if (q == 2 && parts == 2) break;
+                        const int u = unit + q;
+                        if (lg == 0 && u >= 4) {           // (the part that stood there has been multiplied)
+                            tc::mbar_wait(&sm->vw_done[u & 3], ((u >> 2) & 1) ^ 1, abort_flag, d_status);
+                            tc::tc_fence_after();
+                        }
+                        tc::tmem_st_16x128b_x4(dst + (u & 3) * 32, p[q]);
+                    }
                 }
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
@@ -375,9 +386,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                         __syncwarp();
                     }
                 }
-                if (lane == 0) tc::mbar_arrive(&sm->vw_full);
+                if (lane == 0) tc::mbar_arrive(&sm->vw_full[hf]);
+                unit += parts;
             }
-            if (lane == 0) tc::mbar_arrive(STATE_ONLY ? &sm->free_v[s] : &sm->v_read);
+            if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
         }
     } else if (warp >= WARP_STATE && warp < WARP_O) {
         // ------------------------------------------------------------------ the state, a value's row per thread: between two
@@ -390,40 +402,44 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                             : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
                             : j.s_in   ? j.s_in + bh * ssize
                                        : nullptr;
-        for (int t = 0; t < ntiles; ++t) {
+        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             const float dec = sm->pow[tile_n(t)];
             const uint64_t dec2 = tc::f32x2(dec, dec);
+            uint32_t x[2][16];
+            auto fetch = [&](int c, uint32_t (&r)[16]) {
+                if (t > 0) tc::tmem_ld16(row + c, r);
+                else
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) r[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
+            };
             if (t > 0) {
                 tc::mbar_wait(&sm->kv_done, (t - 1) & 1, abort_flag, d_status);
-                if (!STATE_ONLY) tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
             }
+            fetch(0, x[0]);
 #pragma unroll 1
             for (int c = 0; c < DK; c += 32) {
-                uint32_t x[32];
-                if (t > 0) {
-                    tc::tmem_ld32(row + c, x);
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const int cz = c + z * 16;
+                    uint32_t (&r)[16] = x[z];
                     tc::tmem_ld_wait();
-                } else {
+                    if (cz + 16 < DK) fetch(cz + 16, x[z ^ 1]);
+                    uint8_t *dst = smem + L::S + (cz >> 6) * SLAB;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
-                }
-                if (!STATE_ONLY) {
-                    uint8_t *dst = smem + L::S + (c >> 6) * SLAB;
+                    for (int e = 0; e < 16; e += 8)
+                        *reinterpret_cast<uint4 *>(dst + tc::sw128_offset(d, ((cz & 63) + e) >> 3)) =
+                            make_uint4(tc::f32x2_bf16(pair_of(r[e], r[e + 1])), tc::f32x2_bf16(pair_of(r[e + 2], r[e + 3])),
+                                       tc::f32x2_bf16(pair_of(r[e + 4], r[e + 5])), tc::f32x2_bf16(pair_of(r[e + 6], r[e + 7])));
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        *reinterpret_cast<uint4 *>(dst + tc::sw128_offset(d, ((c & 63) + e) >> 3)) =
-                            make_uint4(tc::f32x2_bf16(pair_of(x[e], x[e + 1])), tc::f32x2_bf16(pair_of(x[e + 2], x[e + 3])),
-                                       tc::f32x2_bf16(pair_of(x[e + 4], x[e + 5])), tc::f32x2_bf16(pair_of(x[e + 6], x[e + 7])));
+                    for (int e = 0; e < 16; e += 2) {
+                        const float2 v = tc::f32x2_get(tc::f32x2_mul(dec2, pair_of(r[e], r[e + 1])));
+                        r[e] = __float_as_uint(v.x);
+                        r[e + 1] = __float_as_uint(v.y);
+                    }
+                    tc::tmem_st16(row + cz, r);
                 }
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float2 v = tc::f32x2_get(tc::f32x2_mul(dec2, pair_of(x[e], x[e + 1])));
-                    x[e] = __float_as_uint(v.x);
-                    x[e + 1] = __float_as_uint(v.y);
-                }
-                __syncwarp();
-                tc::tmem_st32(row + c, x);
             }
             tc::tmem_st_wait();
             tc::fence_proxy_async_smem();
@@ -434,7 +450,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         float *to = STATE_ONLY ? j.seg + (bh * a.nseg + seg + 1) * ssize
                     : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
         if (to && ntiles > 0) {
-            tc::mbar_wait(&sm->kv_done, (ntiles - 1) & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - 1) & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < DK; c += 32) {
@@ -451,7 +467,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const int q4 = warp & 3, half = (warp - WARP_O) >> 2, r = q4 * 32 + lane;
         const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16), mine = row + TM_O + half * 64;
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
-            const int s = t % NS, n = tile_n(t), at = tile_at(t);
+            const int s = t % NV, n = tile_n(t), at = tile_at(t);
             const float w = r < n ? j.scale_c * sm->pow[rev ? n - 1 - r : r + 1] : 0.f;
             const uint64_t w2 = tc::f32x2(w, w);
             tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
@@ -475,7 +491,6 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             if (lane == 0) tc::mbar_arrive(&sm->o_scaled);
             tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            tc::mbar_wait(&sm->v_read, t & 1, abort_flag, d_status);      // (w V has been made of all of V)
             const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
             uint8_t *stage = smem + L::V + s * VB + half * SLAB;
 #pragma unroll 1

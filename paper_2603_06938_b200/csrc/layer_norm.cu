@@ -4,9 +4,13 @@
 //   z = w dy:  dx = rstd (z - mean(z) - xh mean(z xh)),  dw = sum over rows of dy xh,  db = sum over rows of dy
 // A row is read once: its entries stay in registers between the sums and the results, eight of them in each of
 // NV places a thread; the statistics are fp32 and in two passes over the registers (mean, then squares around it).
+// Instruction issue bounds these kernels as soon as it can (2048 entries a row by 256 threads: 77 us forward, 154
+// backward of 32768 rows; a copy of the same bytes takes 45): few threads a row, so that the sums across threads are
+// shared by many entries, and arithmetic on pairs.
 #include <algorithm>
 
 #include "la.h"
+#include "tc05.cuh"
 
 namespace swimba {
 
@@ -14,20 +18,38 @@ namespace {
 
 constexpr int LN_THREADS = 256;
 
-__device__ __forceinline__ void put8(float *p, const float (&v)[8])
+// Eight entries as four pairs.
+__device__ __forceinline__ void pairs8(const Raw8h &r, uint64_t (&v)[4])
 {
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void put8(__nv_bfloat16 *p, const float (&v)[8])
-{
-    uint32_t o[4];
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 q = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        o[i] = *reinterpret_cast<const uint32_t *>(&q);
-    }
-    *reinterpret_cast<uint4 *>(p) = make_uint4(o[0], o[1], o[2], o[3]);
+    for (int i = 0; i < 4; ++i) v[i] = tc::f32x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void pairs8(const Raw8f &r, uint64_t (&v)[4])
+{
+    v[0] = tc::f32x2(r.a.x, r.a.y); v[1] = tc::f32x2(r.a.z, r.a.w);
+    v[2] = tc::f32x2(r.b.x, r.b.y); v[3] = tc::f32x2(r.b.z, r.b.w);
+}
+__device__ __forceinline__ void load_pairs(const float *p, uint64_t (&v)[4])
+{
+    Raw8f r;
+    load_raw8(p, r);
+    pairs8(r, v);
+}
+__device__ __forceinline__ void put8(float *p, const uint64_t (&v)[4])
+{
+    const float2 a = tc::f32x2_get(v[0]), b = tc::f32x2_get(v[1]), c = tc::f32x2_get(v[2]), d = tc::f32x2_get(v[3]);
+    *reinterpret_cast<float4 *>(p) = make_float4(a.x, a.y, b.x, b.y);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(c.x, c.y, d.x, d.y);
+}
+__device__ __forceinline__ void put8(__nv_bfloat16 *p, const uint64_t (&v)[4])
+{
+    *reinterpret_cast<uint4 *>(p) = make_uint4(tc::f32x2_bf16(v[0]), tc::f32x2_bf16(v[1]), tc::f32x2_bf16(v[2]), tc::f32x2_bf16(v[3]));
+}
+__device__ __forceinline__ float both(uint64_t v)
+{
+    const float2 f = tc::f32x2_get(v);
+    return f.x + f.y;
 }
 
 // How a block of 256 threads lies over rows: `team` threads (a power of two) per group, gpb groups of a row and rpb rows
@@ -35,187 +57,239 @@ __device__ __forceinline__ void put8(__nv_bfloat16 *p, const float (&v)[8])
 struct LnShape {
     int team, nv, gpb, rpb, ychunks;
 };
-inline LnShape ln_shape(int groups, int width)
+// most: places a thread at most while a warp or part of one has a row (wider rows take more warps first, then more places).
+inline LnShape ln_shape(int groups, int width, int most)
 {
     LnShape s;
     const int chunks = width / 8;
-    s.nv = chunks <= 256 ? 1 : chunks <= 512 ? 2 : chunks <= 1024 ? 4 : 8;
+    s.nv = 1;
     s.team = 1;
-    while (s.team * s.nv < chunks) s.team *= 2;
+    while (s.team < 32 && s.team < chunks) s.team *= 2;
+    while (s.nv < most && s.team * s.nv < chunks) s.nv *= 2;
+    while (s.team < LN_THREADS && s.team * s.nv < chunks) s.team *= 2;
+    while (s.team * s.nv < chunks) s.nv *= 2;
     s.gpb = std::min(groups, LN_THREADS / s.team);
     s.ychunks = ceil_div(groups, s.gpb);
     s.gpb = ceil_div(groups, s.ychunks);
     s.rpb = LN_THREADS / (s.team * s.gpb);
     return s;
 }
+constexpr int LN_FORWARD_PLACES = 8, LN_BACKWARD_PLACES = 4;
 
-// Sum over the threads of a team; `red` has one float per warp and is used when a team is wider than a warp.
-template <int K> __device__ __forceinline__ void team_sum(float (&v)[K], int team, float *red)
+// Sums over the threads of a team.  A team wider than a warp meets in `red` (8 floats per sum), of which there are two,
+// taken in turn, so that one barrier a call is enough; every thread of the block calls it.
+template <int K> __device__ __forceinline__ void team_sum(float (&v)[K], int team, float *red, int &turn)
 {
-    const int width = min(team, 32);
-    for (int o = width >> 1; o > 0; o >>= 1)
+    if (team >= 32) {
 #pragma unroll
-        for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    } else {
+        for (int o = team >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
     if (team > 32) {
         const int warp = threadIdx.x >> 5, per = team >> 5, first = warp / per * per;
-        __syncthreads();
+        float *r = red + turn * K * 8;
+        turn ^= 1;
         if ((threadIdx.x & 31) == 0)
 #pragma unroll
-            for (int i = 0; i < K; ++i) red[i * 8 + warp] = v[i];
+            for (int i = 0; i < K; ++i) r[i * 8 + warp] = v[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            v[i] = 0.f;
-            for (int w = 0; w < per; ++w) v[i] += red[i * 8 + first + w];
+            if (per == 8) {
+                const float4 x = *reinterpret_cast<const float4 *>(r + i * 8), y = *reinterpret_cast<const float4 *>(r + i * 8 + 4);
+                v[i] = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+            } else {
+                v[i] = 0.f;
+                for (int w = 0; w < per; ++w) v[i] += r[i * 8 + first + w];
+            }
         }
     }
 }
 
-template <typename T, int NV>
+// R rows (or sets of rpb rows) at a time: their loads are in flight together and one barrier serves their sums.
+template <typename T, int NV, int R>
 __global__ void __launch_bounds__(LN_THREADS)
 layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict__ wt, const float *__restrict__ bias,
                   int64_t rows, int groups, int width, float eps, int team, int gpb, int rpb, T *__restrict__ y,
                   float *__restrict__ mean, float *__restrict__ rstd)
 {
-    __shared__ float red[8];
+    __shared__ __align__(16) float red[2 * R * 8];
     grid_dep_launch();
     const int tid = threadIdx.x, t = tid % team, slot = tid / team;
     const int g = blockIdx.y * gpb + slot % gpb, rslot = slot / gpb;
     const bool mine = rslot < rpb && g < groups;
-    float w[NV][8], b[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * team) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { w[i][e] = 1.f; b[i][e] = 0.f; }
-        (void)c;
-    }
     grid_dep_wait();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * team) * 8;
-        if (mine && c < width) {
-            if (wt) load8(wt + (int64_t)g * width + c, w[i]);
-            if (bias) load8(bias + (int64_t)g * width + c, b[i]);
-        }
-    }
-    const int64_t D = (int64_t)groups * width;
+    const int64_t D = (int64_t)groups * width, step = (int64_t)gridDim.x * rpb;
     const float inv = 1.f / width;
-    for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += (int64_t)gridDim.x * rpb) {
-        const int64_t r = r0 + rslot;
-        const bool live = mine && r < rows;
-        float v[NV][8], s[1] = {0.f};
+    const float *wg = wt + (int64_t)g * width, *bg = bias + (int64_t)g * width;
+    // few entries a thread: their weights stay in registers; more: they come from the L1 cache with every row
+    uint64_t w[NV > 2 ? 1 : NV][4], b[NV > 2 ? 1 : NV][4];
+    auto weights = [&](int c, uint64_t (&wv)[4], uint64_t (&bv)[4]) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
-            if (live && c < width) load8(x + r * ldx + (int64_t)g * width + c, v[i]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[0] += v[i][e];
+        for (int e = 0; e < 4; ++e) { wv[e] = tc::f32x2(1.f, 1.f); bv[e] = 0ull; }
+        if (mine && c < width) {
+            if (wt) load_pairs(wg + c, wv);
+            if (bias) load_pairs(bg + c, bv);
         }
-        team_sum(s, team, red);
-        const float mu = s[0] * inv;
-        s[0] = 0.f;
+    };
+    if constexpr (NV <= 2)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
+        for (int i = 0; i < NV; ++i) weights((t + i * team) * 8, w[i], b[i]);
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += R * step) {
+        uint64_t v[R][NV][4];
+        float s[R];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[i][e] -= mu;
-                if (c < width) s[0] = fmaf(v[i][e], v[i][e], s[0]);
+        for (int k = 0; k < R; ++k)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int64_t r = r0 + k * step + rslot;
+                const int c = (t + i * team) * 8;
+                typename Raw8<T>::type raw = {};
+                if (mine && r < rows && c < width) load_raw8(x + r * ldx + (int64_t)g * width + c, raw);
+                pairs8(raw, v[k][i]);
             }
-        }
-        team_sum(s, team, red);
-        const float rs = rsqrtf(s[0] * inv + eps);
-        if (!live) continue;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
-            if (c >= width) continue;
-            float o[8];
+        for (int k = 0; k < R; ++k) {
+            uint64_t a2[2] = {0ull, 0ull};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(v[i][e] * rs, w[i][e], b[i][e]);
-            put8(y + r * D + (int64_t)g * width + c, o);
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a2[e & 1] = tc::f32x2_add(a2[e & 1], v[k][i][e]);
+            s[k] = both(tc::f32x2_add(a2[0], a2[1]));
         }
-        if (t == 0) {
-            if (mean) mean[r * groups + g] = mu;
-            if (rstd) rstd[r * groups + g] = rs;
+        team_sum(s, team, red, turn);
+        float mu[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            mu[k] = s[k] * inv;
+            const uint64_t m2 = tc::f32x2(-mu[k], -mu[k]);
+            uint64_t a2[2] = {0ull, 0ull};
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((t + i * team) * 8 < width)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[k][i][e] = tc::f32x2_add(v[k][i][e], m2);
+                        a2[e & 1] = tc::f32x2_fma(v[k][i][e], v[k][i][e], a2[e & 1]);
+                    }
+            s[k] = both(tc::f32x2_add(a2[0], a2[1]));
+        }
+        team_sum(s, team, red, turn);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int64_t r = r0 + k * step + rslot;
+            const float rs = rsqrtf(s[k] * inv + eps);
+            const uint64_t rs2 = tc::f32x2(rs, rs);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * team) * 8;
+                uint64_t wv[4], bv[4], o[4];
+                if constexpr (NV > 2) weights(c, wv, bv);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[e] = NV > 2 ? tc::f32x2_fma(tc::f32x2_mul(v[k][i][e], rs2), wv[e], bv[e])
+                                  : tc::f32x2_fma(tc::f32x2_mul(v[k][i][e], rs2), w[NV > 2 ? 0 : i][e], b[NV > 2 ? 0 : i][e]);
+                if (mine && r < rows && c < width) put8(y + r * D + (int64_t)g * width + c, o);
+            }
+            if (mine && r < rows && t == 0) {
+                if (mean) mean[r * groups + g] = mu[k];
+                if (rstd) rstd[r * groups + g] = rs;
+            }
         }
     }
 }
 
 // dx, and each block's sums of dy xh and dy over the rows that it met: partial[block][0 dw | 1 db][D].
-template <typename T, int NV>
+template <typename T, int NV, int R>
 __global__ void __launch_bounds__(LN_THREADS)
 layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, int64_t ldx, const float *__restrict__ wt,
                            const float *__restrict__ mean, const float *__restrict__ rstd, int64_t rows, int groups,
                            int width, int team, int gpb, int rpb, T *__restrict__ dx, float *__restrict__ partial)
 {
-    __shared__ float red[16];
+    __shared__ __align__(16) float red[2 * 2 * R * 8];
     __shared__ float sums[LN_THREADS * 8];
     grid_dep_launch();
     grid_dep_wait();
     const int tid = threadIdx.x, t = tid % team, slot = tid / team;
     const int g = blockIdx.y * gpb + slot % gpb, rslot = slot / gpb;
     const bool mine = rslot < rpb && g < groups;
-    float w[NV][8], aw[NV][8], ab[NV][8];
+    uint64_t w[NV][4], aw[NV][4], ab[NV][4];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (t + i * team) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { w[i][e] = 1.f; aw[i][e] = 0.f; ab[i][e] = 0.f; }
-        if (wt && mine && c < width) load8(wt + (int64_t)g * width + c, w[i]);
+        for (int e = 0; e < 4; ++e) { w[i][e] = tc::f32x2(1.f, 1.f); aw[i][e] = 0ull; ab[i][e] = 0ull; }
+        if (wt && mine && c < width) load_pairs(wt + (int64_t)g * width + c, w[i]);
     }
-    const int64_t D = (int64_t)groups * width;
+    const int64_t D = (int64_t)groups * width, step = (int64_t)gridDim.x * rpb;
     const float inv = 1.f / width;
-    for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += (int64_t)gridDim.x * rpb) {
-        const int64_t r = r0 + rslot;
-        const bool live = mine && r < rows;
-        typename Raw8<T>::type rx[NV], rd[NV];
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += R * step) {
+        typename Raw8<T>::type rx[R][NV], rd[R][NV];
+        float rs[R], mr[R], s[2 * R];               // rstd, - mean rstd
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
-            if (live && c < width) {
-                load_raw8(x + r * ldx + (int64_t)g * width + c, rx[i]);
-                load_raw8(dy + r * D + (int64_t)g * width + c, rd[i]);
+        for (int k = 0; k < R; ++k) {
+            const int64_t r = r0 + k * step + rslot;
+            const bool live = mine && r < rows;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * team) * 8;
+                rx[k][i] = {};
+                rd[k][i] = {};
+                if (live && c < width) {
+                    load_raw8(x + r * ldx + (int64_t)g * width + c, rx[k][i]);
+                    load_raw8(dy + r * D + (int64_t)g * width + c, rd[k][i]);
+                }
             }
+            rs[k] = live ? rstd[r * groups + g] : 0.f;
+            mr[k] = live ? -mean[r * groups + g] * rs[k] : 0.f;
         }
-        const float mu = live ? mean[r * groups + g] : 0.f, rs = live ? rstd[r * groups + g] : 0.f;
-        float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
-            if (!(live && c < width)) continue;
-            float xv[8], dv[8];
-            unpack8(rx[i], xv);
-            unpack8(rd[i], dv);
+        for (int k = 0; k < R; ++k) {
+            const uint64_t rs2 = tc::f32x2(rs[k], rs[k]), mr2 = tc::f32x2(mr[k], mr[k]);
+            uint64_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float xh = (xv[e] - mu) * rs, z = dv[e] * w[i][e];
-                s[0] += z;
-                s[1] = fmaf(z, xh, s[1]);
-                aw[i][e] = fmaf(dv[e], xh, aw[i][e]);
-                ab[i][e] += dv[e];
+            for (int i = 0; i < NV; ++i) {
+                uint64_t xv[4], dv[4];
+                pairs8(rx[k][i], xv);
+                pairs8(rd[k][i], dv);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t xh = tc::f32x2_fma(xv[e], rs2, mr2), z = tc::f32x2_mul(dv[e], w[i][e]);
+                    s0 = tc::f32x2_add(s0, z);
+                    s1 = tc::f32x2_fma(z, xh, s1);
+                    aw[i][e] = tc::f32x2_fma(dv[e], xh, aw[i][e]);
+                    ab[i][e] = tc::f32x2_add(ab[i][e], dv[e]);
+                }
             }
+            s[2 * k] = both(s0);
+            s[2 * k + 1] = both(s1);
         }
-        team_sum(s, team, red);
-        if (!live) continue;
-        const float m0 = s[0] * inv, m1 = s[1] * inv;
+        team_sum(s, team, red, turn);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
-            if (c >= width) continue;
-            float xv[8], dv[8], o[8];
-            unpack8(rx[i], xv);
-            unpack8(rd[i], dv);
+        for (int k = 0; k < R; ++k) {
+            const int64_t r = r0 + k * step + rslot;
+            // rs (z - m0 - xh m1)
+            const float c0 = -rs[k] * s[2 * k] * inv, c1 = -rs[k] * s[2 * k + 1] * inv;
+            const uint64_t rs2 = tc::f32x2(rs[k], rs[k]), mr2 = tc::f32x2(mr[k], mr[k]), c02 = tc::f32x2(c0, c0), c12 = tc::f32x2(c1, c1);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float xh = (xv[e] - mu) * rs;
-                o[e] = rs * (dv[e] * w[i][e] - m0 - xh * m1);
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * team) * 8;
+                uint64_t xv[4], dv[4], o[4];
+                pairs8(rx[k][i], xv);
+                pairs8(rd[k][i], dv);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[e] = tc::f32x2_fma(tc::f32x2_mul(dv[e], w[i][e]), rs2,
+                                         tc::f32x2_fma(tc::f32x2_fma(xv[e], rs2, mr2), c12, c02));
+                if (mine && r < rows && c < width) put8(dx + r * D + (int64_t)g * width + c, o);
             }
-            put8(dx + r * D + (int64_t)g * width + c, o);
         }
     }
     if (!partial) return;
@@ -227,7 +301,11 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, in
             const int c = (t + i * team) * 8;
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sums[e * LN_THREADS + tid] = k == 0 ? aw[i][e] : ab[i][e];
+            for (int e = 0; e < 4; ++e) {
+                const float2 f = tc::f32x2_get(k == 0 ? aw[i][e] : ab[i][e]);
+                sums[2 * e * LN_THREADS + tid] = f.x;
+                sums[(2 * e + 1) * LN_THREADS + tid] = f.y;
+            }
             __syncthreads();
             if (rslot == 0 && mine && c < width) {
                 float o[8];
@@ -236,7 +314,9 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, in
                     o[e] = 0.f;
                     for (int q = 0; q < rpb; ++q) o[e] += sums[e * LN_THREADS + tid + q * gpb * team];
                 }
-                put8(partial + ((int64_t)blockIdx.x * 2 + k) * D + (int64_t)g * width + c, o);
+                float4 *p = reinterpret_cast<float4 *>(partial + ((int64_t)blockIdx.x * 2 + k) * D + (int64_t)g * width + c);
+                p[0] = make_float4(o[0], o[1], o[2], o[3]);
+                p[1] = make_float4(o[4], o[5], o[6], o[7]);
             }
         }
 }
@@ -269,44 +349,57 @@ layer_norm_sum_kernel(const float *__restrict__ partial, int nblk, int64_t D, fl
     }
 }
 
+// Blocks over the rows: as many as are resident together (a block walks the rows from there on).
+template <typename K> int ln_resident(K kern)
+{
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, LN_THREADS, 0) != cudaSuccess || n < 1) n = 1;
+    return n;
+}
 int ln_blocks(const LnShape &s, int64_t rows, int sm_count, int per_sm)
 {
     const int64_t need = ceil_div64(rows, s.rpb);
     return (int)std::min<int64_t>(need, std::max(1, per_sm * sm_count / s.ychunks));
 }
+constexpr int LN_GRAD_BLOCKS = 3;          // per SM: each leaves D partial sums twice
 
-template <typename T, int NV>
+template <typename T, int NV, int R>
 int run_norm(LaunchCtx &ctx, const LnShape &s, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
              int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd)
 {
+    static const int resident = ln_resident(layer_norm_kernel<T, NV, R>);
     ctx.begin(STAGE_LAYER_NORM);
-    launch_kernel(layer_norm_kernel<T, NV>, dim3(ln_blocks(s, rows, sm_count, 8), s.ychunks), dim3(LN_THREADS), 0,
-                  ctx.stream, true, (const T *)x, ldx, w, b, rows, groups, width, eps, s.team, s.gpb, s.rpb, (T *)y,
+    launch_kernel(layer_norm_kernel<T, NV, R>, dim3(ln_blocks(s, rows, sm_count, resident), s.ychunks), dim3(LN_THREADS),
+                  0, ctx.stream, true, (const T *)x, ldx, w, b, rows, groups, width, eps, s.team, s.gpb, s.rpb, (T *)y,
                   mean, rstd);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
 
-template <typename T, int NV>
+template <typename T, int NV, int R>
 int run_backward(LaunchCtx &ctx, const LnShape &s, const void *dy, const void *x, int64_t ldx, const float *w,
                  const float *mean, const float *rstd, int64_t rows, int groups, int width, int sm_count, void *dx,
                  float *partial)
 {
     ctx.begin(STAGE_LAYER_NORM_BACKWARD);
-    launch_kernel(layer_norm_backward_kernel<T, NV>, dim3(ln_blocks(s, rows, sm_count, 2), s.ychunks), dim3(LN_THREADS),
-                  0, ctx.stream, true, (const T *)dy, (const T *)x, ldx, w, mean, rstd, rows, groups, width, s.team,
-                  s.gpb, s.rpb, (T *)dx, partial);
+    launch_kernel(layer_norm_backward_kernel<T, NV, R>, dim3(ln_blocks(s, rows, sm_count, LN_GRAD_BLOCKS), s.ychunks),
+                  dim3(LN_THREADS), 0, ctx.stream, true, (const T *)dy, (const T *)x, ldx, w, mean, rstd, rows, groups,
+                  width, s.team, s.gpb, s.rpb, (T *)dx, partial);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
 
 }  // namespace
 
+// Rows (or sets of rpb rows) a thread takes at a time: enough bytes in flight without spilling.
+constexpr int ln_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+constexpr int ln_rows_backward(int nv) { return nv == 1 ? 2 : 1; }
+
 int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
                       int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd)
 {
-    const LnShape s = ln_shape(groups, width);
-#define LN_RUN(T, NV) run_norm<T, NV>(ctx, s, x, ldx, w, b, rows, groups, width, eps, sm_count, y, mean, rstd)
+    const LnShape s = ln_shape(groups, width, LN_FORWARD_PLACES);
+#define LN_RUN(T, NV) run_norm<T, NV, ln_rows(NV)>(ctx, s, x, ldx, w, b, rows, groups, width, eps, sm_count, y, mean, rstd)
     if (dtype == SWIMBA_DTYPE_FP32)
         return s.nv == 1 ? LN_RUN(float, 1) : s.nv == 2 ? LN_RUN(float, 2) : s.nv == 4 ? LN_RUN(float, 4) : LN_RUN(float, 8);
     return s.nv == 1 ? LN_RUN(__nv_bfloat16, 1) : s.nv == 2 ? LN_RUN(__nv_bfloat16, 2)
@@ -316,16 +409,16 @@ int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, con
 
 size_t layer_norm_partial_bytes(int64_t rows, int groups, int width, int sm_count)
 {
-    const LnShape s = ln_shape(groups, width);
-    return (size_t)ln_blocks(s, rows, sm_count, 2) * 2 * groups * width * sizeof(float);
+    const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES);
+    return (size_t)ln_blocks(s, rows, sm_count, LN_GRAD_BLOCKS) * 2 * groups * width * sizeof(float);
 }
 
 int launch_layer_norm_backward(LaunchCtx &ctx, int dtype, const void *dy, const void *x, int64_t ldx, const float *w,
                                const float *mean, const float *rstd, int64_t rows, int groups, int width, int sm_count,
                                void *dx, float *dw, float *db, float *partial)
 {
-    const LnShape s = ln_shape(groups, width);
-#define LN_RUN(T, NV) run_backward<T, NV>(ctx, s, dy, x, ldx, w, mean, rstd, rows, groups, width, sm_count, dx, partial)
+    const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES);
+#define LN_RUN(T, NV) run_backward<T, NV, ln_rows_backward(NV)>(ctx, s, dy, x, ldx, w, mean, rstd, rows, groups, width, sm_count, dx, partial)
     int rc;
     if (dtype == SWIMBA_DTYPE_FP32)
         rc = s.nv == 1 ? LN_RUN(float, 1) : s.nv == 2 ? LN_RUN(float, 2) : s.nv == 4 ? LN_RUN(float, 4) : LN_RUN(float, 8);
@@ -337,7 +430,7 @@ int launch_layer_norm_backward(LaunchCtx &ctx, int dtype, const void *dy, const 
     const int64_t D = (int64_t)groups * width;
     ctx.begin(STAGE_LAYER_NORM_SUM);
     launch_kernel(layer_norm_sum_kernel, dim3((unsigned)ceil_div64(2 * D, 32)), dim3(256), 0, ctx.stream, true, partial,
-                  ln_blocks(s, rows, sm_count, 2), D, dw, db);
+                  ln_blocks(s, rows, sm_count, LN_GRAD_BLOCKS), D, dw, db);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }

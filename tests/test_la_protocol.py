@@ -152,65 +152,77 @@ def run(n, ns, state_only, rng):
     drive([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]), bars, async_ops, rng)
 
 
-def run_wide(n, ns, state_only, rng):
-    need = {f"{k}_{x}{s}": 1 for s in range(ns) for k in ("full", "free") for x in "qkv"}
-    need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "kv_done", "vw_full",
-                                "vw_done", "v_read")})
+def run_wide(n, nq, state_only, rng):
+    ns = {"q": nq, "k": nq + 1, "v": 3}
+    parts = rng.choice([2, 3])
+    need = {f"{k}_{x}{s}": 1 for x in "qkv" for s in range(ns[x]) for k in ("full", "free")}
+    need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "kv_done", "vw_full0",
+                                "vw_full1", "vw_done0", "vw_done1", "vw_done2", "vw_done3")})
     bars, buf = Bars(need), Buffers()
     odd = lambda t: not state_only and t % 3 == 1
     async_ops = []
+    slot = lambda x, t: f"{x}{t % ns[x]}"
 
     def tma():
-        for t in range(n):
-            s = t % ns
-            for x in "kv" if state_only else "qkv":
-                if t >= ns:
-                    yield f"free_{x}{s}", t // ns - 1
-                readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 2}[x]
-                async_ops.append([lambda x=x, s=s, t=t, r=readers: (buf.write(f"{x}{s}", t, r), bars.arrive(f"full_{x}{s}"))])
+        def load(x, t):
+            if t < 0 or t >= n or (state_only and x == "q"):
+                return
+            if t >= ns[x]:
+                yield f"free_{slot(x, t)}", t // ns[x] - 1
+            readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 2}[x]
+            async_ops.append([lambda: (buf.write(slot(x, t), t, readers), bars.arrive(f"full_{slot(x, t)}"))])
+        for t in range(-3, n):
+            for x in "qkv":
+                yield from load(x, t + ns[x])
 
     def mma():
         queue = []
         async_ops.append(queue)
 
         def scores(t):
-            yield f"full_k{t % ns}", t // ns
-            yield f"full_q{t % ns}", t // ns
-            queue.append(lambda: (buf.read(f"k{t % ns}", t), buf.read(f"q{t % ns}", t), buf.write("qk", ("a", t), 1),
+            yield f"full_{slot('k', t)}", t // ns["k"]
+            yield f"full_{slot('q', t)}", t // ns["q"]
+            queue.append(lambda: (buf.read(slot("k", t), t), buf.read(slot("q", t), t), buf.write("qk", ("a", t), 1),
                                   bars.arrive("qk_full")))
 
-        def half(t, hf):
-            yield "vw_full", 2 * t + hf
-            if hf:
-                queue.append(lambda: (buf.read("vw", 2 * t + 1), buf.read(f"k{t % ns}", t), buf.read("s_scaled", t),
-                                      buf.write("s", t + 1, 1), bars.arrive("vw_done"), bars.arrive("kv_done"),
-                                      bars.arrive(f"free_k{t % ns}")))
-            else:
-                queue.append(lambda: (buf.read("vw", 2 * t), bars.arrive("vw_done")))
+        def half(t, hf, p, u):
+            def done():
+                buf.read(f"vw{u & 3}", u)
+                bars.arrive(f"vw_done{u & 3}")
+                if hf == 1 and p == parts - 1:
+                    buf.read(slot("k", t), t)
+                    if not state_only:
+                        buf.read("s_scaled", t)
+                        buf.write("s", t + 1, 1)
+                    if not state_only or t == n - 1:
+                        bars.arrive("kv_done")
+                    bars.arrive(f"free_{slot('k', t)}")
+            queue.append(done)
         if not state_only and n:
             yield from scores(0)
+        u = 0
         for t in range(n):
-            s = t % ns
             if state_only:
-                yield f"full_k{s}", t // ns
-            yield "s_full", t
-            if not state_only:
+                yield f"full_{slot('k', t)}", t // ns["k"]
+            else:
+                yield "s_full", t
                 if t:
                     yield "o_free", t - 1
-                queue.append(lambda t=t, s=s: (buf.read(f"q{s}", t), buf.read("s16", t), buf.write("o", ("s", t), 1),
-                                               bars.arrive("qs_done"), bars.arrive(f"free_q{s}")))
-            yield from half(t, 0)
-            if odd(t):
-                yield from half(t, 1)
-            if not state_only:
-                yield f"full_v{s}", t // ns
-                yield "p_full", t
-                yield "o_scaled", t
-                queue.append(lambda t=t, s=s: (buf.read(f"v{s}", ("z", t) if odd(t) else t), buf.read("qk", ("p", t)),
-                                               buf.read("o", ("w", t)), buf.write("o", ("o", t), 1), bars.arrive("pv_done")))
-            if not odd(t):
-                yield from half(t, 1)
-            if not state_only and t + 1 < n:
+                queue.append(lambda t=t: (buf.read(slot("q", t), t), buf.read("s16", t), buf.write("o", ("s", t), 1),
+                                          bars.arrive("qs_done"), bars.arrive(f"free_{slot('q', t)}")))
+            for hf in (0, 1):
+                yield f"vw_full{hf}", t
+                for p in range(parts):
+                    half(t, hf, p, u)
+                    u += 1
+            if state_only:
+                continue
+            yield f"full_{slot('v', t)}", t // ns["v"]
+            yield "p_full", t
+            yield "o_scaled", t
+            queue.append(lambda t=t: (buf.read(slot("v", t), ("z", t) if odd(t) else t), buf.read("qk", ("p", t)),
+                                      buf.read("o", ("w", t)), buf.write("o", ("o", t), 1), bars.arrive("pv_done")))
+            if t + 1 < n:
                 yield "pv_done", t
                 if odd(t):
                     yield "o_free", t
@@ -225,55 +237,58 @@ def run_wide(n, ns, state_only, rng):
             bars.arrive("p_full")
 
     def values():
+        u = 0
         for t in range(n):
-            yield f"full_v{t % ns}", t // ns
+            v = slot("v", t)
+            yield f"full_{v}", t // ns["v"]
             for hf in (0, 1):
-                if 2 * t + hf:
-                    yield "vw_done", 2 * t + hf - 1
-                assert buf.v[f"v{t % ns}"][0] == t, "w V from what replaced V"
-                buf.write("vw", 2 * t + hf, 1)
+                for p in range(parts):
+                    if u >= 4:
+                        yield f"vw_done{u & 3}", (u >> 2) - 1
+                    assert buf.v[v][0] == t, "w V from what replaced V"
+                    buf.write(f"vw{u & 3}", u, 1)
+                    u += 1
                 yield None
                 if hf:
+                    buf.read(v, t)
                     if odd(t):                            # what is not finite gives way to zeros
-                        buf.read(f"v{t % ns}", t)
-                        assert buf.v[f"v{t % ns}"][1] == 1
-                        buf.v[f"v{t % ns}"] = [("z", t), 1]
-                    else:
-                        buf.read(f"v{t % ns}", t)
-                bars.arrive("vw_full")
-            bars.arrive(f"free_v{t % ns}" if state_only else "v_read")
+                        assert buf.v[v][1] == 1
+                        buf.v[v] = [("z", t), 1]
+                bars.arrive(f"vw_full{hf}")
+            if state_only:
+                bars.arrive(f"free_{v}")
 
     def outputs():
         for t in range(n):
+            v = slot("v", t)
             yield "qs_done", t
             buf.read("o", ("s", t))
             buf.write("o", ("w", t), 1)
             yield None
             bars.arrive("o_scaled")
             yield "pv_done", t
-            yield "v_read", t
             buf.read("o", ("o", t))
             yield None
             if odd(t):
                 buf.read("qk", ("p", t))
             bars.arrive("o_free")
-            buf.write(f"v{t % ns}", f"o{t}", 1)
+            buf.write(v, f"o{t}", 1)
             yield None
-            buf.read(f"v{t % ns}", f"o{t}")
-            bars.arrive(f"free_v{t % ns}")
+            buf.read(v, f"o{t}")
+            bars.arrive(f"free_{v}")
 
     def state():
-        for t in range(n):
+        for t in range(0 if state_only else n):
             if t:
                 yield "kv_done", t - 1
                 buf.read("s", t)
-                if not state_only:
-                    yield "qs_done", t - 1
+                yield "qs_done", t - 1
             buf.write("s_scaled", t, 1)
-            if not state_only:
-                buf.write("s16", t, 1)
+            buf.write("s16", t, 1)
             yield None
             bars.arrive("s_full")
+        if state_only and n:
+            yield "kv_done", 0
 
     drive([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]), bars, async_ops, rng)
 
@@ -302,4 +317,4 @@ def test_every_wait_ends_and_no_buffer_is_lost(n, ns, state_only):
     rng = random.Random(n * 10 + ns)
     for _ in range(60):
         run(n, ns, state_only, rng)
-        run_wide(n, ns, state_only, rng)
+        run_wide(n, ns - 1, state_only, rng)
