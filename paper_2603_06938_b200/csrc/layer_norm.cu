@@ -30,9 +30,9 @@ __device__ __forceinline__ void pairs8(const Raw8f &r, uint64_t (&v)[4])
     v[0] = tc::f32x2(r.a.x, r.a.y); v[1] = tc::f32x2(r.a.z, r.a.w);
     v[2] = tc::f32x2(r.b.x, r.b.y); v[3] = tc::f32x2(r.b.z, r.b.w);
 }
-__device__ __forceinline__ void load_pairs(const float *p, uint64_t (&v)[4])
+template <typename T> __device__ __forceinline__ void load_pairs(const T *p, uint64_t (&v)[4])
 {
-    Raw8f r;
+    typename Raw8<T>::type r;
     load_raw8(p, r);
     pairs8(r, v);
 }
@@ -77,7 +77,7 @@ inline LnShape ln_shape(int groups, int width, int most)
 constexpr int LN_FORWARD_PLACES = 8, LN_BACKWARD_PLACES = 4;
 
 // Sums over the threads of a team.  A team wider than a warp meets in `red` (8 floats per sum), of which there are two,
-// taken in turn, so that one barrier a call is enough; every thread of the block calls it.
+// taken in turn, so that one barrier of the team a call is enough; every thread of the team calls it.
 template <int K> __device__ __forceinline__ void team_sum(float (&v)[K], int team, float *red, int &turn)
 {
     if (team >= 32) {
@@ -97,7 +97,7 @@ template <int K> __device__ __forceinline__ void team_sum(float (&v)[K], int tea
         if ((threadIdx.x & 31) == 0)
 #pragma unroll
             for (int i = 0; i < K; ++i) r[i * 8 + warp] = v[i];
-        __syncthreads();
+        tc::named_bar_sync(1 + threadIdx.x / team, team);
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             if (per == 8) {
@@ -206,99 +206,145 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict_
 }
 
 // dx, and each block's sums of dy xh and dy over the rows that it met: partial[block][0 dw | 1 db][D].
-template <typename T, int NV, int R>
-__global__ void __launch_bounds__(LN_THREADS)
-layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, int64_t ldx, const float *__restrict__ wt,
-                           const float *__restrict__ mean, const float *__restrict__ rstd, int64_t rows, int groups,
-                           int width, int team, int gpb, int rpb, T *__restrict__ dx, float *__restrict__ partial)
+// The rows come through a ring of stages in shared memory, rpb rows of x and dy each, filled by bulk copies ahead of their
+// use, and are read from there twice (sums, then dx): what a thread keeps in registers is the sums over rows, and
+// with rows and weights beside them no second block would fit an SM (154 us for 32768 x 2048 that way).
+constexpr int LN_STAGES = 4;
+struct LnRows {
+    int64_t rows, ldx, D;
+    int groups, width, team, gpb, rpb, sets, stages;     // sets: of rpb rows, in a stage
+};
+template <typename T, int NV>
+__global__ void __launch_bounds__(LN_THREADS, NV <= 4 ? 2 : 1)
+layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ wt,
+                           const float *__restrict__ mean, const float *__restrict__ rstd, const LnRows a,
+                           T *__restrict__ dx, float *__restrict__ partial, int *d_status)
 {
-    __shared__ __align__(16) float red[2 * 2 * R * 8];
-    __shared__ float sums[LN_THREADS * 8];
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ __align__(16) float red[2 * 2 * 8];
+    __shared__ uint64_t full[LN_STAGES], empty[LN_STAGES];
+    __shared__ int abort_flag;
+    const int tid = threadIdx.x, t = tid % a.team, slot = tid / a.team, lane = tid & 31;
+    const int g0 = blockIdx.y * a.gpb, ng = min(a.gpb, a.groups - g0), gl = slot % a.gpb, rslot = slot / a.gpb;
+    const bool mine = rslot < a.rpb && gl < ng;
+    const int seg = ng * a.width;                   // entries of a row that this block works
+    float *sw = reinterpret_cast<float *>(smem);    // the weights, then the stages: x rows, dy rows
+    T *ring = reinterpret_cast<T *>(sw + a.gpb * a.width);
+    const int per = a.rpb * a.sets;                 // rows of a stage
+    const int64_t stage = (int64_t)2 * per * a.gpb * a.width;
+    if (tid == 0) {
+        for (int i = 0; i < LN_STAGES; ++i) {
+            tc::mbar_init(&full[i], 1);
+            tc::mbar_init(&empty[i], LN_THREADS / 32);
+        }
+        abort_flag = 0;
+        tc::fence_mbar_init();
+    }
     grid_dep_launch();
     grid_dep_wait();
-    const int tid = threadIdx.x, t = tid % team, slot = tid / team;
-    const int g = blockIdx.y * gpb + slot % gpb, rslot = slot / gpb;
-    const bool mine = rslot < rpb && g < groups;
-    uint64_t w[NV][4], aw[NV][4], ab[NV][4];
+    for (int i = tid; i < seg; i += LN_THREADS) sw[i] = wt ? wt[(int64_t)g0 * a.width + i] : 1.f;
+    __syncthreads();
+    const int64_t nchunks = (a.rows + per - 1) / per;
+    // (warp 0) chunk number i of this block into its stage, if there is one
+    auto fill = [&](int64_t i) {
+        const int64_t ch = blockIdx.x + i * gridDim.x;
+        if (ch >= nchunks) return;
+        const int s = (int)(i % a.stages);
+        tc::mbar_wait(&empty[s], (uint32_t)((i / a.stages) & 1) ^ 1, &abort_flag, d_status);
+        const int64_t r0 = ch * per;
+        const int n = (int)min((int64_t)per, a.rows - r0);
+        const uint32_t bytes = (uint32_t)(seg * sizeof(T));
+        if (lane == 0) tc::mbar_arrive_expect_tx(&full[s], 2 * n * bytes);
+        __syncwarp();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * team) * 8;
+        for (int k = 0; k < 2; ++k) {
+            const int64_t ld = k == 0 ? a.ldx : a.D;
+            const T *src = (k == 0 ? x : dy) + r0 * ld + (int64_t)g0 * a.width;
+            T *dst = ring + s * stage + (int64_t)k * per * seg;
+            if (ld == seg) {                        // rows back to back
+                if (lane == 0) tc::bulk_load(dst, src, n * bytes, &full[s]);
+            } else {
+                for (int r = lane; r < n; r += 32) tc::bulk_load(dst + (int64_t)r * seg, src + r * ld, bytes, &full[s]);
+            }
+        }
+    };
+    if (tid < 32)
+        for (int i = 0; i < a.stages; ++i) fill(i);
+    uint64_t aw[NV][4], ab[NV][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { w[i][e] = tc::f32x2(1.f, 1.f); aw[i][e] = 0ull; ab[i][e] = 0ull; }
-        if (wt && mine && c < width) load_pairs(wt + (int64_t)g * width + c, w[i]);
-    }
-    const int64_t D = (int64_t)groups * width, step = (int64_t)gridDim.x * rpb;
-    const float inv = 1.f / width;
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) aw[i][e] = ab[i][e] = 0ull;
+    const float inv = 1.f / a.width;
     int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += R * step) {
-        typename Raw8<T>::type rx[R][NV], rd[R][NV];
-        float rs[R], mr[R], s[2 * R];               // rstd, - mean rstd
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int64_t r = r0 + k * step + rslot;
-            const bool live = mine && r < rows;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * team) * 8;
-                rx[k][i] = {};
-                rd[k][i] = {};
-                if (live && c < width) {
-                    load_raw8(x + r * ldx + (int64_t)g * width + c, rx[k][i]);
-                    load_raw8(dy + r * D + (int64_t)g * width + c, rd[k][i]);
-                }
-            }
-            rs[k] = live ? rstd[r * groups + g] : 0.f;
-            mr[k] = live ? -mean[r * groups + g] * rs[k] : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const uint64_t rs2 = tc::f32x2(rs[k], rs[k]), mr2 = tc::f32x2(mr[k], mr[k]);
+    int64_t it = 0;
+    for (int64_t ch = blockIdx.x; ch < nchunks; ch += gridDim.x, ++it) {
+        if (tid < 32 && it > 0) fill(it - 1 + a.stages);
+        const int st = (int)(it % a.stages);
+        const float *pw = sw + gl * a.width;
+        tc::mbar_wait(&full[st], (uint32_t)((it / a.stages) & 1), &abort_flag, d_status);
+#pragma unroll 2
+        for (int q = 0; q < a.sets; ++q) {
+            const int lr = q * a.rpb + rslot;
+            const int64_t r = ch * per + lr;
+            const bool live = mine && r < a.rows;
+            const float rs = live ? rstd[r * a.groups + g0 + gl] : 0.f, mr = live ? -mean[r * a.groups + g0 + gl] * rs : 0.f;
+            const T *px = ring + st * stage + (int64_t)lr * seg + gl * a.width, *pd = px + (int64_t)per * seg;
+            const uint64_t rs2 = tc::f32x2(rs, rs), mr2 = tc::f32x2(mr, mr);
             uint64_t s0 = 0ull, s1 = 0ull;
+            if (live) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                uint64_t xv[4], dv[4];
-                pairs8(rx[k][i], xv);
-                pairs8(rd[k][i], dv);
+                for (int i = 0; i < NV; ++i) {
+                    const int c = (t + i * a.team) * 8;
+                    if (c >= a.width) continue;
+                    uint64_t xv[4], dv[4], w[4];
+                    load_pairs(px + c, xv);
+                    load_pairs(pd + c, dv);
+                    load_pairs(pw + c, w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint64_t xh = tc::f32x2_fma(xv[e], rs2, mr2), z = tc::f32x2_mul(dv[e], w[i][e]);
-                    s0 = tc::f32x2_add(s0, z);
-                    s1 = tc::f32x2_fma(z, xh, s1);
-                    aw[i][e] = tc::f32x2_fma(dv[e], xh, aw[i][e]);
-                    ab[i][e] = tc::f32x2_add(ab[i][e], dv[e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const uint64_t xh = tc::f32x2_fma(xv[e], rs2, mr2), z = tc::f32x2_mul(dv[e], w[e]);
+                        s0 = tc::f32x2_add(s0, z);
+                        s1 = tc::f32x2_fma(z, xh, s1);
+                        aw[i][e] = tc::f32x2_fma(dv[e], xh, aw[i][e]);
+                        ab[i][e] = tc::f32x2_add(ab[i][e], dv[e]);
+                    }
                 }
             }
-            s[2 * k] = both(s0);
-            s[2 * k + 1] = both(s1);
-        }
-        team_sum(s, team, red, turn);
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int64_t r = r0 + k * step + rslot;
+            float s[2] = {both(s0), both(s1)};
+            __syncwarp();
+            team_sum(s, a.team, red, turn);
             // rs (z - m0 - xh m1)
-            const float c0 = -rs[k] * s[2 * k] * inv, c1 = -rs[k] * s[2 * k + 1] * inv;
-            const uint64_t rs2 = tc::f32x2(rs[k], rs[k]), mr2 = tc::f32x2(mr[k], mr[k]), c02 = tc::f32x2(c0, c0), c12 = tc::f32x2(c1, c1);
+            const float c0 = -rs * s[0] * inv, c1 = -rs * s[1] * inv;
+            const uint64_t c02 = tc::f32x2(c0, c0), c12 = tc::f32x2(c1, c1);
+            if (live) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * team) * 8;
-                uint64_t xv[4], dv[4], o[4];
-                pairs8(rx[k][i], xv);
-                pairs8(rd[k][i], dv);
+                for (int i = 0; i < NV; ++i) {
+                    const int c = (t + i * a.team) * 8;
+                    if (c >= a.width) continue;
+                    uint64_t xv[4], dv[4], w[4], o[4];
+                    load_pairs(px + c, xv);
+                    load_pairs(pd + c, dv);
+                    load_pairs(pw + c, w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    o[e] = tc::f32x2_fma(tc::f32x2_mul(dv[e], w[i][e]), rs2,
-                                         tc::f32x2_fma(tc::f32x2_fma(xv[e], rs2, mr2), c12, c02));
-                if (mine && r < rows && c < width) put8(dx + r * D + (int64_t)g * width + c, o);
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = tc::f32x2_fma(tc::f32x2_mul(dv[e], w[e]), rs2, tc::f32x2_fma(tc::f32x2_fma(xv[e], rs2, mr2), c12, c02));
+                    put8(dx + r * a.D + (int64_t)(g0 + gl) * a.width + c, o);
+                }
             }
         }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&empty[st]);
     }
     if (!partial) return;
-    // the rows of a block side by side: their sums meet in shared memory, in order
+    // the rows of a block side by side: their sums meet in shared memory, in order (every stage that was filled has been
+    // taken; what is left of the ring is room enough)
+    float *sums = reinterpret_cast<float *>(smem);
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * team) * 8;
+            const int c = (t + i * a.team) * 8;
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -307,14 +353,14 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, in
                 sums[(2 * e + 1) * LN_THREADS + tid] = f.y;
             }
             __syncthreads();
-            if (rslot == 0 && mine && c < width) {
+            if (rslot == 0 && mine && c < a.width) {
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     o[e] = 0.f;
-                    for (int q = 0; q < rpb; ++q) o[e] += sums[e * LN_THREADS + tid + q * gpb * team];
+                    for (int q = 0; q < a.rpb; ++q) o[e] += sums[e * LN_THREADS + tid + q * a.gpb * a.team];
                 }
-                float4 *p = reinterpret_cast<float4 *>(partial + ((int64_t)blockIdx.x * 2 + k) * D + (int64_t)g * width + c);
+                float4 *p = reinterpret_cast<float4 *>(partial + ((int64_t)blockIdx.x * 2 + k) * a.D + (int64_t)(g0 + gl) * a.width + c);
                 p[0] = make_float4(o[0], o[1], o[2], o[3]);
                 p[1] = make_float4(o[4], o[5], o[6], o[7]);
             }
@@ -361,7 +407,8 @@ int ln_blocks(const LnShape &s, int64_t rows, int sm_count, int per_sm)
     const int64_t need = ceil_div64(rows, s.rpb);
     return (int)std::min<int64_t>(need, std::max(1, per_sm * sm_count / s.ychunks));
 }
-constexpr int LN_GRAD_BLOCKS = 3;          // per SM: each leaves D partial sums twice
+constexpr int LN_GRAD_BLOCKS = 2;          // per SM, resident together: each leaves D partial sums twice
+constexpr size_t LN_GRAD_ROOM = 100 * 1024;  // of shared memory for one of them, where its rows are short enough
 
 template <typename T, int NV, int R>
 int run_norm(LaunchCtx &ctx, const LnShape &s, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
@@ -376,15 +423,29 @@ int run_norm(LaunchCtx &ctx, const LnShape &s, const void *x, int64_t ldx, const
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
 
-template <typename T, int NV, int R>
+// Sets of rows a stage of the gradient's ring holds: short rows come several at a time, so that one wait serves them.
+int ln_sets(size_t es, const LnShape &s, int width)
+{
+    const size_t one = 2 * (size_t)s.rpb * s.gpb * width * es;
+    return (int)std::max<size_t>(1, std::min<size_t>(4, 24 * 1024 / one));
+}
+
+template <typename T, int NV>
 int run_backward(LaunchCtx &ctx, const LnShape &s, const void *dy, const void *x, int64_t ldx, const float *w,
                  const float *mean, const float *rstd, int64_t rows, int groups, int width, int sm_count, void *dx,
                  float *partial)
 {
+    auto kern = layer_norm_backward_kernel<T, NV>;
+    const size_t weights = (size_t)s.gpb * width * sizeof(float);
+    const int sets = ln_sets(sizeof(T), s, width);
+    const size_t stage = (size_t)2 * sets * s.rpb * s.gpb * width * sizeof(T);
+    const int stages = LN_GRAD_ROOM > weights ? (int)std::min<size_t>(LN_STAGES, (LN_GRAD_ROOM - weights) / stage) : 0;
+    const LnRows a{rows, ldx, (int64_t)groups * width, groups, width, s.team, s.gpb, s.rpb, sets, std::max(1, stages)};
+    const size_t smem = std::max<size_t>(weights + a.stages * stage, LN_THREADS * 8 * sizeof(float));
+    if (!ensure_dynamic_smem((const void *)kern, smem)) return SWIMBA_ERR_CUDA;
     ctx.begin(STAGE_LAYER_NORM_BACKWARD);
-    launch_kernel(layer_norm_backward_kernel<T, NV, R>, dim3(ln_blocks(s, rows, sm_count, LN_GRAD_BLOCKS), s.ychunks),
-                  dim3(LN_THREADS), 0, ctx.stream, true, (const T *)dy, (const T *)x, ldx, w, mean, rstd, rows, groups,
-                  width, s.team, s.gpb, s.rpb, (T *)dx, partial);
+    launch_kernel(kern, dim3(ln_blocks(s, rows, sm_count, LN_GRAD_BLOCKS), s.ychunks), dim3(LN_THREADS), smem, ctx.stream,
+                  true, (const T *)dy, (const T *)x, w, mean, rstd, a, (T *)dx, partial, ctx.d_status);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
@@ -393,7 +454,6 @@ int run_backward(LaunchCtx &ctx, const LnShape &s, const void *dy, const void *x
 
 // Rows (or sets of rpb rows) a thread takes at a time: enough bytes in flight without spilling.
 constexpr int ln_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
-constexpr int ln_rows_backward(int nv) { return nv == 1 ? 2 : 1; }
 
 int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
                       int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd)
@@ -418,7 +478,7 @@ int launch_layer_norm_backward(LaunchCtx &ctx, int dtype, const void *dy, const 
                                void *dx, float *dw, float *db, float *partial)
 {
     const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES);
-#define LN_RUN(T, NV) run_backward<T, NV, ln_rows_backward(NV)>(ctx, s, dy, x, ldx, w, mean, rstd, rows, groups, width, sm_count, dx, partial)
+#define LN_RUN(T, NV) run_backward<T, NV>(ctx, s, dy, x, ldx, w, mean, rstd, rows, groups, width, sm_count, dx, partial)
     int rc;
     if (dtype == SWIMBA_DTYPE_FP32)
         rc = s.nv == 1 ? LN_RUN(float, 1) : s.nv == 2 ? LN_RUN(float, 2) : s.nv == 4 ? LN_RUN(float, 4) : LN_RUN(float, 8);
