@@ -7,6 +7,7 @@
 // they differ from it, so that difference is taken from the whole numbers before anything is rounded.
 // The counts come first (from the active sets alone), so that one pass over u gives the loss and the gradients.
 #include <algorithm>
+#include <cstddef>
 
 #include "la.h"
 #include "tc05.cuh"
@@ -61,15 +62,17 @@ __device__ __forceinline__ float share_difference(int count, int valid, int k, i
 
 // ------------------------------------------------------------------------------------------
 // Up to 16 experts, bf16, F a multiple of 16 up to 2048: one pass over u for everything.  A block keeps 16 tokens of u in
-// shared memory and its eight warps a share of the features each; all products are m16n8k16:
+// shared memory and its sixteen warps a share of the features each; all products are m16n8k16:
 //   logits  u [16 tokens, features] x W^T, the warps' parts added in order; softmax and dg with an expert a lane
 //   dW      dg^T [experts, 16 tokens] x u, in registers over all the block's tokens (one partial sum a block)
 //   du      dg [16 tokens, experts] x W, staged where u stood and copied out from there
 // dg enters the products as bf16 parts: three for dW, an fp32 result (2^-24 of it), two for du, which is bf16 itself.  With
 // up to eight experts the first two parts lie side by side, as the rows (dW) or the depth (du) of one product.
-// Bound by the bytes of u and du (32768 tokens, F = 2048, E = 8: FMA kernels with u read twice 284 us).
+// The work between two barriers is short and its latency counts: eight warps that also made the copies took 88 us for 32768
+// tokens, F = 2048, E = 8 (FMA kernels with u read twice: 284 us for the call).
 // ------------------------------------------------------------------------------------------
-constexpr int BF_TOK = 16, BF_WARPS = 8, BF_NT = 32;       // tokens of a tile, warps, most n-tiles of 8 features a warp has
+constexpr int BF_TOK = 16, BF_WARPS = 16, BF_NT = 16;      // tokens of a tile, warps, most n-tiles of 8 features a warp has
+constexpr int BF_MATH = BF_WARPS * 32, BF_THREADS = BF_MATH + 32;        // and one warp for the copies
 constexpr int BF_COUNT_HERE = 8192;                         // entries that every block counts by itself
 
 __device__ __forceinline__ void bf_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -93,17 +96,18 @@ __device__ __forceinline__ void bf_ldmatrix_trans(uint32_t addr, uint32_t (&r)[4
 }
 
 template <int EP> struct BfSmall {
-    uint64_t full[2];
+    uint64_t full[2], done[2];
     int abort_flag;
+    uint32_t ok;                                            // tokens of the tile that count
     int total[SWIMBA_MAX_EXPERTS + 1];
-    uint8_t ok[BF_TOK];
-    float part[BF_WARPS][BF_TOK][EP];
+    alignas(16) float part[BF_WARPS][BF_TOK][EP];
     alignas(16) __nv_bfloat16 dg[3][BF_TOK][24];           // parts of dg (rows of 48 bytes); EP = 8: [0] the first two side by side
     float psum[BF_TOK][EP];
 };
+static_assert(offsetof(BfSmall<8>, part) % 16 == 0 && offsetof(BfSmall<8>, dg) % 16 == 0 && offsetof(BfSmall<16>, dg) % 16 == 0, "read in pairs and rows of 16 bytes");
 
 template <int EP>
-__global__ void __launch_bounds__(256, 1)
+__global__ void __launch_bounds__(BF_THREADS, 1)
 balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *__restrict__ W,
                      const int32_t *__restrict__ idx, const uint8_t *__restrict__ valid, int64_t Tn, int F, int E, int k,
                      float coef, int *__restrict__ cnt, int ncnt, bool count_here, bool check, __nv_bfloat16 *__restrict__ du,
@@ -118,34 +122,51 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
     if (tid == 0) {
         tc::mbar_init(&sm.full[0], 1);
         tc::mbar_init(&sm.full[1], 1);
+        tc::mbar_init(&sm.done[0], BF_WARPS);
+        tc::mbar_init(&sm.done[1], BF_WARPS);
         sm.abort_flag = 0;
         tc::fence_mbar_init();
     }
-    for (int i = tid; i < 3 * BF_TOK * 24; i += 256) (&sm.dg[0][0][0])[i] = __float2bfloat16_rn(0.f);
+    for (int i = tid; i < 3 * BF_TOK * 24; i += BF_THREADS) (&sm.dg[0][0][0])[i] = __float2bfloat16_rn(0.f);
     __syncthreads();
     grid_dep_launch();
     grid_dep_wait();
-    // (warp 0) tile t into stage s: a row a lane
-    auto load = [&](int64_t t, int s) {
-        if (t >= ntiles) return;
-        const int n = (int)min((int64_t)BF_TOK, Tn - t * BF_TOK);
-        if (lane == 0) tc::mbar_arrive_expect_tx(&sm.full[s], (uint32_t)(n * F * 2));
-        __syncwarp();
-        if (lane < n) tc::bulk_load(sU + (s * BF_TOK + lane) * pitch, u + (t * BF_TOK + lane) * F, (uint32_t)(F * 2), &sm.full[s]);
-    };
-    if (warp == 0) {
+    if (warp == BF_WARPS) {
+        // ---- copies: a row a lane; a tile's du goes out before the tile after next comes in
+        auto load = [&](int64_t t, int s) {
+            if (t >= ntiles) return;
+            const int n = (int)min((int64_t)BF_TOK, Tn - t * BF_TOK);
+            if (lane == 0) tc::mbar_arrive_expect_tx(&sm.full[s], (uint32_t)(n * F * 2));
+            __syncwarp();
+            if (lane < n) tc::bulk_load(sU + (s * BF_TOK + lane) * pitch, u + (t * BF_TOK + lane) * F, (uint32_t)(F * 2), &sm.full[s]);
+        };
         load(blockIdx.x, 0);
         load((int64_t)blockIdx.x + gridDim.x, 1);
+        int64_t it = 0;
+        for (int64_t t = blockIdx.x; t < ntiles; t += gridDim.x, ++it) {
+            const int s = (int)(it & 1);
+            tc::mbar_wait(&sm.done[s], (uint32_t)((it >> 1) & 1), &sm.abort_flag, d_status);
+            if (du && lane < BF_TOK && t * BF_TOK + lane < Tn) {
+                tc::bulk_store(du + (t * BF_TOK + lane) * F, sU + (s * BF_TOK + lane) * pitch, (uint32_t)(F * 2));
+                tc::bulk_commit_group();
+                tc::bulk_wait_read_all();
+            }
+            __syncwarp();
+            load(t + 2 * (int64_t)gridDim.x, s);
+        }
+        return;
     }
-    for (int i = tid; i < EP * (F / 8); i += 256) {
+    // (from here on the warps that calculate)
+    auto meet = [] { tc::named_bar_sync(1, BF_MATH); };
+    for (int i = tid; i < EP * (F / 8); i += BF_MATH) {
         const int e = i / (F / 8), c = i % (F / 8);
         *reinterpret_cast<uint4 *>(sW + e * pitch + c * 16) =
             e < E ? *reinterpret_cast<const uint4 *>(W + (int64_t)e * F + c * 8) : make_uint4(0, 0, 0, 0);
     }
     if (count_here) {
-        for (int i = tid; i <= E; i += 256) sm.total[i] = 0;
-        __syncthreads();
-        for (int64_t i = tid; i < Tn * k; i += 256) {
+        for (int i = tid; i <= E; i += BF_MATH) sm.total[i] = 0;
+        meet();
+        for (int64_t i = tid; i < Tn * k; i += BF_MATH) {
             const int64_t t = i / k;
             if (valid && !valid[t]) continue;
             if (i % k == 0) atomicAdd(&sm.total[E], 1);
@@ -153,11 +174,17 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
             if ((unsigned)e < (unsigned)E) atomicAdd(&sm.total[e], 1);
             else if (check) atomicCAS(d_status, 0, SWIMBA_ERR_DEVICE_BOUNDS);
         }
-        __syncthreads();
+        meet();
         if (blockIdx.x == 0)
-            for (int i = tid; i <= E; i += 256) cnt[i] = sm.total[i];
+            for (int i = tid; i <= E; i += BF_MATH) cnt[i] = sm.total[i];
     } else {
-        total_counts(cnt, ncnt, E, sm.total);
+        for (int i = tid; i <= E; i += BF_MATH) {
+            int v = 0;
+#pragma unroll 8
+            for (int b = 0; b < ncnt; ++b) v += cnt[b * (E + 1) + i];
+            sm.total[i] = v;
+        }
+        meet();
     }
     const int nv = sm.total[E];
     const int te = tid % EP, tt = tid / EP;                 // softmax: expert and token of this thread (tt < 16)
@@ -182,18 +209,19 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
         const int s = (int)(it & 1);
         uint8_t *tile = sU + s * BF_TOK * pitch;
         const uint32_t bT = bU + s * BF_TOK * pitch;
-        bool bad = false;
-        if (tid < BF_TOK) {
-            sm.ok[tid] = ok_next;
-            bad = !ok_next;
+        if (warp == 0) {
+            const uint32_t m = __ballot_sync(0xffffffffu, ok_next) & 0xffffu;
+            if (lane == 0) sm.ok = m;
             const int64_t nt = (t + gridDim.x) * BF_TOK + tid;
-            ok_next = nt < Tn && (!valid || valid[nt]);
+            ok_next = tid < BF_TOK && nt < Tn && (!valid || valid[nt]);
         }
         tc::mbar_wait(&sm.full[s], (uint32_t)((it >> 1) & 1), &sm.abort_flag, d_status);
-        if (__syncthreads_or(bad)) {                        // padding may hold anything, and rows behind the last token do
-            for (int i = tid; i < BF_TOK * (F / 8); i += 256)
-                if (!sm.ok[i / (F / 8)]) *reinterpret_cast<uint4 *>(tile + i / (F / 8) * pitch + i % (F / 8) * 16) = make_uint4(0, 0, 0, 0);
-            __syncthreads();
+        meet();
+        const uint32_t ok = sm.ok;
+        if (ok != 0xffffu) {                                // padding may hold anything, and rows behind the last token do
+            for (int i = tid; i < BF_TOK * (F / 8); i += BF_MATH)
+                if (!(ok >> (i / (F / 8)) & 1u)) *reinterpret_cast<uint4 *>(tile + i / (F / 8) * pitch + i % (F / 8) * 16) = make_uint4(0, 0, 0, 0);
+            meet();
         }
         // ---- logits
         float lg[EP / 8][4];
@@ -216,7 +244,7 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
                 *reinterpret_cast<float2 *>(&sm.part[warp][g + 8][n * 8 + q]) = make_float2(lg[n][2], lg[n][3]);
             }
         }
-        __syncthreads();
+        meet();
         // ---- softmax over the experts, dg
         if (tt < BF_TOK) {
             float g = 0.f;
@@ -230,7 +258,7 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
             float sum = x;
 #pragma unroll
             for (int o = EP / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float p = sm.ok[tt] ? x / sum : 0.f;
+            const float p = (ok >> tt & 1u) ? x / sum : 0.f;
             psum += p;
             float fb = p * dev;
 #pragma unroll
@@ -248,7 +276,7 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
                 sm.dg[2][tt][te] = p2;
             }
         }
-        __syncthreads();
+        meet();
         // ---- dW and du, 16 features at a time
         uint32_t at[3][4], ad[2][4];                        // dg^T (rows: experts), dg (rows: tokens)
 #pragma unroll
@@ -295,21 +323,11 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
             }
         }
         if (du) tc::fence_proxy_async_smem();
-        __syncthreads();
-        if (warp == 0) {
-            if (du) {
-                if (lane < BF_TOK && t * BF_TOK + lane < Tn) {
-                    tc::bulk_store(du + (t * BF_TOK + lane) * F, tile + lane * pitch, (uint32_t)(F * 2));
-                    tc::bulk_commit_group();
-                    tc::bulk_wait_read_all();
-                }
-                __syncwarp();
-            }
-            load(t + 2 * (int64_t)gridDim.x, s);
-        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sm.done[s]);
     }
     if (tt < BF_TOK) sm.psum[tt][te] = psum;
-    __syncthreads();
+    meet();
     if (tid < E) {
         float v = 0.f;
         for (int i = 0; i < BF_TOK; ++i) v += sm.psum[i][tid];
@@ -622,7 +640,7 @@ int run_fused(LaunchCtx &ctx, const void *u, const void *W, const int32_t *idx, 
     const size_t smem = bl_fused_smem(F, E);
     if (!ensure_dynamic_smem((const void *)kern, smem)) return SWIMBA_ERR_CUDA;
     ctx.begin(STAGE_BALANCE_TOKENS);
-    launch_kernel(kern, dim3(nblk), dim3(256), smem, ctx.stream, true, (const __nv_bfloat16 *)u, (const __nv_bfloat16 *)W,
+    launch_kernel(kern, dim3(nblk), dim3(BF_THREADS), smem, ctx.stream, true, (const __nv_bfloat16 *)u, (const __nv_bfloat16 *)W,
                   idx, valid, Tn, F, E, k, coef, cnt, ncnt, here, ctx.check_indices, (__nv_bfloat16 *)du,
                   dW ? part : (float *)nullptr, mean, ctx.d_status);
     ctx.end();
