@@ -59,6 +59,36 @@ __device__ __forceinline__ LaDecay la_decay(float g)
     return LaDecay{(float)l, (float)(l - (double)(float)l)};
 }
 
+// w v in bf16 parts, for two values and their weights at a time.  A weight goes in as three bf16 parts of its own; the
+// remainder of a bf16 product is itself a bf16 number, so a fused multiply-add gives it exactly:
+//   four parts  wh v and its remainder, wm v, its remainder and wl v in one (together 2^-24 of w v)
+//   two parts   wh v, its remainder and wm v in one (2^-17)
+__device__ __forceinline__ void la_split(float w0, float w1, uint32_t (&p)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        p[i] = tc::pack_bf16x2(w0, w1);
+        w0 -= __uint_as_float(p[i] << 16);
+        w1 -= __uint_as_float(p[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ __nv_bfloat162 la_pair(uint32_t v) { return *reinterpret_cast<const __nv_bfloat162 *>(&v); }
+__device__ __forceinline__ uint32_t la_bits(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+__device__ __forceinline__ void la_parts4(uint32_t v, const uint32_t (&w)[3], uint32_t (&p)[4])
+{
+    const __nv_bfloat162 x = la_pair(v), h = __hmul2(la_pair(w[0]), x), m = __hmul2(la_pair(w[1]), x);
+    p[0] = la_bits(h);
+    p[1] = la_bits(__hfma2(la_pair(w[0]), x, __hneg2(h)));
+    p[2] = la_bits(m);
+    p[3] = la_bits(__hfma2(la_pair(w[2]), x, __hfma2(la_pair(w[1]), x, __hneg2(m))));
+}
+__device__ __forceinline__ void la_parts2(uint32_t v, const uint32_t (&w)[3], uint32_t (&p)[4])
+{
+    const __nv_bfloat162 x = la_pair(v), h = __hmul2(la_pair(w[0]), x);
+    p[0] = la_bits(h);
+    p[1] = la_bits(__hfma2(la_pair(w[1]), x, __hfma2(la_pair(w[0]), x, __hneg2(h))));
+}
+
 // Segments the kernels cut every sequence of a call into, and the bytes they keep for that.
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg);
 // (bytes of one job's segment states; grows with B and with L)

@@ -43,8 +43,9 @@ struct Small {
     float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
     float pow[LT + 1];                       // lambda^m
     float weight[LT];                        // of a whole tile's tokens in w V
+    alignas(16) uint32_t wsplit[LT / 2][4];  // their parts, two tokens at a time
 };
-static_assert(offsetof(Small, pow_col) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
+static_assert(offsetof(Small, pow_col) % 16 == 0 && offsetof(Small, wsplit) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
 
 struct Maps {
     CUtensorMap q[LA_MAX_JOBS], k[LA_MAX_JOBS], v[LA_MAX_JOBS], o[LA_MAX_JOBS];
@@ -78,8 +79,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     const int h = (int)(id % a.H), b = (int)(id / a.H);
     const LaJob &j = a.job[ji];
     const bool rev = j.reverse != 0;
-    // three parts where the state is a result; two (2^-16) where only the read of it is, whose copy is rounded to bf16
-    const int parts = j.s_out ? 3 : 2;
+    // four parts where the state is a result; two where only the read of it is, whose copy is rounded to bf16
+    const int parts = j.s_out ? 4 : 2;
     const int place = rev ? a.nseg - 1 - seg : seg;
     const int t_begin = place * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     const int ntiles = (t_end - t_begin + LT - 1) / LT;
@@ -130,6 +131,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     else if (tid >= 256 && tid < 288) sm->pow_col[tid - 256] = exp2f((rev ? tid - 256 : 287 - tid) * g2);
     else if (tid >= 320 && tid < 383) sm->pow_diag[tid - 320] = j.scale_p * exp2f(abs(tid - 351) * g2);
     else if (tid >= 512 && tid < 640) sm->weight[tid - 512] = j.scale_a * exp2f((rev ? tid - 511 : 639 - tid) * g2);
+    else if (tid >= 640 && tid < 704) {
+        const int q = 2 * (tid - 640);
+        uint32_t p[3];
+        la_split(j.scale_a * exp2f((rev ? q + 1 : 127 - q) * g2), j.scale_a * exp2f((rev ? q + 2 : 126 - q) * g2), p);
+        *reinterpret_cast<uint4 *>(sm->wsplit[tid - 640]) = make_uint4(p[0], p[1], p[2], 0u);
+    }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -311,7 +318,6 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         // ------------------------------------------------------------------ (w V)^T: 32 values and 32 tokens of half a tile,
         // 16 values at a time, transposed on the way from shared memory
         const int q4 = warp & 3, tk = (warp - WARP_W) >> 2;
-        const uint64_t neg = tc::f32x2(-1.f, -1.f);
         // this lane's row of the 8 x 8 blocks: (token octet, value octet) = (lane / 16, lane / 8 % 2), token lane % 8
         const int tok = tk * 32 + (lane >> 4) * 8 + (lane & 7);
         const uint32_t slab = L::V + (q4 >> 1) * SLAB, ch0 = (q4 & 1) * 4 + ((lane >> 3) & 1);
@@ -324,58 +330,67 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             const float tail = STATE_ONLY ? exp2f((rev ? tile_at(t) - t_begin : t_end - tile_at(t) - n) * g2) : 1.f;
             tc::mbar_wait(&sm->full_v[s], (t / NV) & 1, abort_flag, d_status);
             const uint32_t src = base + slab + s * VB;
-            uint32_t odd = 0;
+            __nv_bfloat162 odd = la_pair(0u);         // becomes NaN with the first entry that is not finite
 #pragma unroll 1
             for (int hf = 0; hf < 2; ++hf) {
-                uint64_t w[4];
+                uint32_t w[4][3];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int jj = hf * 64 + tk * 32 + c * 8 + (lane & 3) * 2;
-                    w[c] = tc::f32x2(jj < n ? tail * sm->weight[jj + shift] : 0.f, jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f);
+                    if (!STATE_ONLY && n == LT) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(sm->wsplit[jj >> 1]);
+                        w[c][0] = x.x; w[c][1] = x.y; w[c][2] = x.z;
+                    } else {
+                        la_split(jj < n ? tail * sm->weight[jj + shift] : 0.f, jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f, w[c]);
+                    }
                 }
 #pragma unroll 1
                 for (int lg = 0; lg < 2; ++lg) {
-                    uint32_t r[8], p[3][8];
+                    uint32_t r[8], p[4][8];
                     const uint32_t at = src + tc::sw128_offset(hf * 64 + tok, ch0 + lg * 2);
                     tc::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]);
                     tc::ldmatrix_x4_trans(at + 16 * 128, r[4], r[5], r[6], r[7]);      // (16 tokens on: same swizzle)
-                    if (!STATE_ONLY && hf == 0) {      // the other half too: PV must find no infinity and no NaN in V
-                        uint32_t u[8];
-                        tc::ldmatrix_x4_trans(at + 64 * 128, u[0], u[1], u[2], u[3]);
-                        tc::ldmatrix_x4_trans(at + 80 * 128, u[4], u[5], u[6], u[7]);
+                    if (!STATE_ONLY)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)    // (an exponent of all ones carries into the sign's place)
-                            odd |= ((r[e] & 0x7f807f80u) + 0x00800080u) | ((u[e] & 0x7f807f80u) + 0x00800080u);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        uint64_t x = tc::f32x2_mul(w[e >> 1], pair_of(r[e] << 16, r[e] & 0xffff0000u));
-                        p[0][e] = tc::f32x2_bf16(x);
-                        x = tc::f32x2_fma(neg, pair_of(p[0][e] << 16, p[0][e] & 0xffff0000u), x);
-                        p[1][e] = tc::f32x2_bf16(x);
-                        x = tc::f32x2_fma(neg, pair_of(p[1][e] << 16, p[1][e] & 0xffff0000u), x);
-                        p[2][e] = tc::f32x2_bf16(x);
-                    }
+                        for (int e = 0; e < 8; ++e) odd = __hfma2(la_pair(r[e]), la_pair(0u), odd);
                     const uint32_t dst = to + ((uint32_t)(q4 * 32 + lg * 16) << 16);
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) {
-                        if (q == 2 && parts == 2) break;
+                    auto put = [&](int q) {
                         const int u = unit + q;
                         if (lg == 0 && u >= 4) {           // (the part that stood there has been multiplied)
                             tc::mbar_wait(&sm->vw_done[u & 3], ((u >> 2) & 1) ^ 1, abort_flag, d_status);
                             tc::tc_fence_after();
                         }
                         tc::tmem_st_16x128b_x4(dst + (u & 3) * 32, p[q]);
+                    };
+                    if (parts == 4) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            uint32_t x[4];
+                            la_parts4(r[e], w[e >> 1], x);
+                            p[0][e] = x[0]; p[1][e] = x[1]; p[2][e] = x[2]; p[3][e] = x[3];
+                        }
+                        put(0);
+                        put(1);
+                        put(2);
+                        put(3);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            uint32_t x[4];
+                            la_parts2(r[e], w[e >> 1], x);
+                            p[0][e] = x[0]; p[1][e] = x[1];
+                        }
+                        put(0);
+                        put(1);
                     }
                 }
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (!STATE_ONLY && __any_sync(0xffffffffu, (odd & 0x80008000u) != 0)) {
-                    // seen with the first half; what is not finite gives way to zeros once both halves have been read, and
-                    // PV waits for that
-                    if (hf == 0) ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
-                    else {
+                if (!STATE_ONLY && hf == 1 && __any_sync(0xffffffffu, __hisnan(odd.x) || __hisnan(odd.y))) {
+                    // what is not finite gives way to zeros, now that both halves have been read; PV comes behind KV
+                    ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
+                    {
 #pragma unroll 1
                         for (int i = 0; i < 64; ++i) {
                             unsigned short *e = reinterpret_cast<unsigned short *>(

@@ -154,7 +154,7 @@ def run(n, ns, state_only, rng):
 
 def run_wide(n, nq, state_only, rng):
     ns = {"q": nq, "k": nq + 1, "v": 3}
-    parts = rng.choice([2, 3])
+    parts = rng.choice([2, 4])
     need = {f"{k}_{x}{s}": 1 for x in "qkv" for s in range(ns[x]) for k in ("full", "free")}
     need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "kv_done", "vw_full0",
                                 "vw_full1", "vw_done0", "vw_done1", "vw_done2", "vw_done3")})
