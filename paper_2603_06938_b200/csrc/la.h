@@ -74,21 +74,6 @@ __device__ __forceinline__ void la_split(float w0, float w1, uint32_t (&p)[3])
 }
 __device__ __forceinline__ __nv_bfloat162 la_pair(uint32_t v) { return *reinterpret_cast<const __nv_bfloat162 *>(&v); }
 __device__ __forceinline__ uint32_t la_bits(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
-__device__ __forceinline__ void la_parts4(uint32_t v, const uint32_t (&w)[3], uint32_t (&p)[4])
-{
-    const __nv_bfloat162 x = la_pair(v), h = __hmul2(la_pair(w[0]), x), m = __hmul2(la_pair(w[1]), x);
-    p[0] = la_bits(h);
-    p[1] = la_bits(__hfma2(la_pair(w[0]), x, __hneg2(h)));
-    p[2] = la_bits(m);
-    p[3] = la_bits(__hfma2(la_pair(w[2]), x, __hfma2(la_pair(w[1]), x, __hneg2(m))));
-}
-__device__ __forceinline__ void la_parts2(uint32_t v, const uint32_t (&w)[3], uint32_t (&p)[4])
-{
-    const __nv_bfloat162 x = la_pair(v), h = __hmul2(la_pair(w[0]), x);
-    p[0] = la_bits(h);
-    p[1] = la_bits(__hfma2(la_pair(w[1]), x, __hfma2(la_pair(w[0]), x, __hneg2(h))));
-}
-
 // Segments the kernels cut every sequence of a call into, and the bytes they keep for that.
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg);
 // (bytes of one job's segment states; grows with B and with L)

@@ -1,8 +1,8 @@
 // Linear attention with a decay for each head on the tensor cores, heads of 128 values (bf16; 64 or 128 keys): the
 // same five steps per tile of 128 tokens as in la_tiles.cu, with all values of a head in one CTA, so that scores and masks
 // are made once.  What makes room for that in shared memory (two or three stages of Q, K and V, the bf16 state):
-//   w V   is made transposed, [DV, tokens], straight into tensor memory, half a tile's three parts at a time, and is the A
-//         operand of KV:  D = (w V)^T K
+//   w V   is made transposed, [DV, tokens], straight into tensor memory, a quarter of a tile at a time and two of them in
+//         turn, and is the A operand of KV:  D = (w V)^T K
 //   S     lies in tensor memory in fp32, [DV, DK]; between two tiles it is read, rounded for QS and scaled by lambda^n,
 //         and KV adds to it
 //   O     one region: Q S^T, scaled row by row in place, then P V on top
@@ -24,7 +24,7 @@ constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
 // warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 4 for the state, 8 for o
 constexpr int THREADS = 1024;
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 24;
-// tensor memory columns: scores and over them P (bf16), O, S, a ring of four parts of half a tile's w V
+// tensor memory columns: scores and over them P (bf16), O, S, w V of two quarters of a tile, up to four parts of each
 constexpr uint32_t TM_QK = 0, TM_O = 128, TM_S = 256, TM_VW = 384, TM_COLS = 512;
 
 template <int DK> struct Sm {
@@ -35,7 +35,7 @@ template <int DK> struct Sm {
 };
 struct Small {
     uint64_t full_q[2], full_k[3], full_v[3], free_q[2], free_k[3], free_v[3];
-    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, kv_done, vw_full[2], vw_done[4];
+    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, kv_done, vw_full[2], vw_done[2];
     uint32_t tmem;
     int abort_flag;
     int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
@@ -51,7 +51,7 @@ struct Maps {
     CUtensorMap q[LA_MAX_JOBS], k[LA_MAX_JOBS], v[LA_MAX_JOBS], o[LA_MAX_JOBS];
 };
 
-__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b) { return tc::f32x2(__uint_as_float(a), __uint_as_float(b)); }
+__device__ __forceinline__ uint32_t bits2(uint32_t a, uint32_t b) { return tc::pack_bf16x2(__uint_as_float(a), __uint_as_float(b)); }
 
 // STATE_ONLY: from a zero state, and only the end state is kept (in seg).
 template <int DK, bool STATE_ONLY>
@@ -100,7 +100,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             tc::mbar_init(&sm->full_v[s], 1);
             tc::mbar_init(&sm->free_v[s], STATE_ONLY || j.o_f32 ? 8 : 2);
         }
-        for (int s = 0; s < 4; ++s) tc::mbar_init(&sm->vw_done[s], 1);
+        for (int s = 0; s < 2; ++s) tc::mbar_init(&sm->vw_done[s], 1);
         sm->odd_tile[0] = sm->odd_tile[1] = 0;
         tc::mbar_init(&sm->qk_full, 1);
         tc::mbar_init(&sm->p_full, 8);
@@ -203,7 +203,6 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             __syncwarp();
         };
         if (!STATE_ONLY && ntiles > 0) scores(0);
-        int unit = 0;                            // parts of half tiles multiplied so far
         for (int t = 0; t < ntiles; ++t) {
             if (STATE_ONLY) {
                 tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
@@ -224,25 +223,24 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 }
                 __syncwarp();
             }
-            // KV, by halves of the tile and their parts
+            // KV, by quarters of the tile
 #pragma unroll 1
-            for (int hf = 0; hf < 2; ++hf) {
-                tc::mbar_wait(&sm->vw_full[hf], t & 1, abort_flag, d_status);
+            for (int qd = 0; qd < 4; ++qd) {
+                const int buf = qd & 1;
+                tc::mbar_wait(&sm->vw_full[buf], qd >> 1, abort_flag, d_status);
                 tc::tc_fence_after();
-                const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + hf * 8192));
+                if (leader) {
+                    uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + qd * 4096));
 #pragma unroll 1
-                for (int p = 0; p < parts; ++p, ++unit) {
-                    if (leader) {
-#pragma unroll
-                        for (int kk = 0; kk < LT / 32; ++kk)
-                            tc::mma_ts(tm + TM_S, tm + TM_VW + (unit & 3) * 32 + kk * 8, tc::smem_desc_advance(k, kk * 2048), id_kv,
-                                       !STATE_ONLY || t + hf + p + kk > 0);
-                        tc::mma_commit(&sm->vw_done[unit & 3]);
+                    for (int p = 0; p < parts; ++p) {
+                        tc::mma_ts(tm + TM_S, tm + TM_VW + buf * 64 + p * 16, k, id_kv, !STATE_ONLY || t + qd + p > 0);
+                        tc::mma_ts(tm + TM_S, tm + TM_VW + buf * 64 + p * 16 + 8, tc::smem_desc_advance(k, 2048), id_kv, 1);
                     }
-                }
-                if (leader && hf == 1) {
-                    if (!STATE_ONLY || t == ntiles - 1) tc::mma_commit(&sm->kv_done);
-                    tc::mma_commit(&sm->free_k[t % NK]);
+                    tc::mma_commit(&sm->vw_done[buf]);
+                    if (qd == 3) {
+                        if (!STATE_ONLY || t == ntiles - 1) tc::mma_commit(&sm->kv_done);
+                        tc::mma_commit(&sm->free_k[t % NK]);
+                    }
                 }
                 __syncwarp();
             }
@@ -298,12 +296,11 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                         for (int e = 0; e < 16; ++e) o[e] = tc::pack_bf16x2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
                     } else {                     // a factor for the row's place before the block, one for each column's in it
                         const float rho = scale_p * sm->pow[rev ? 32 * bl - i : i - 32 * bl - 31];
-                        const uint64_t r2 = tc::f32x2(rho, rho);
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const float4 c = *reinterpret_cast<const float4 *>(&sm->pow_col[2 * e]);
-                            o[e] = tc::f32x2_bf16(tc::f32x2_mul(pair_of(x[2 * e], x[2 * e + 1]), tc::f32x2_mul(r2, tc::f32x2(c.x, c.y))));
-                            o[e + 1] = tc::f32x2_bf16(tc::f32x2_mul(pair_of(x[2 * e + 2], x[2 * e + 3]), tc::f32x2_mul(r2, tc::f32x2(c.z, c.w))));
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 c = *reinterpret_cast<const float4 *>(&sm->pow_col[e]);
+                            o[e / 2] = tc::pack_bf16x2(__uint_as_float(x[e]) * (rho * c.x), __uint_as_float(x[e + 1]) * (rho * c.y));
+                            o[e / 2 + 1] = tc::pack_bf16x2(__uint_as_float(x[e + 2]) * (rho * c.z), __uint_as_float(x[e + 3]) * (rho * c.w));
                         }
                     }
                 }
@@ -315,94 +312,86 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             if (lane == 0) tc::mbar_arrive(&sm->p_full);
         }
     } else if (warp >= WARP_W && warp < WARP_STATE) {
-        // ------------------------------------------------------------------ (w V)^T: 32 values and 32 tokens of half a tile,
-        // 16 values at a time, transposed on the way from shared memory
-        const int q4 = warp & 3, tk = (warp - WARP_W) >> 2;
+        // ------------------------------------------------------------------ (w V)^T: 16 values of a quarter of a tile, 32
+        // tokens, transposed on the way from shared memory
+        const int q4 = warp & 3, lg = (warp - WARP_W) >> 2;
         // this lane's row of the 8 x 8 blocks: (token octet, value octet) = (lane / 16, lane / 8 % 2), token lane % 8
-        const int tok = tk * 32 + (lane >> 4) * 8 + (lane & 7);
-        const uint32_t slab = L::V + (q4 >> 1) * SLAB, ch0 = (q4 & 1) * 4 + ((lane >> 3) & 1);
-        const uint32_t to = tmem + TM_VW + tk * 16;
-        const uint32_t base = tc::smem_u32(smem);
-        int unit = 0;                            // parts of half tiles made so far
+        const uint32_t row0 = tc::sw128_offset((lane >> 4) * 8 + (lane & 7), (q4 & 1) * 4 + lg * 2 + ((lane >> 3) & 1));
+        const uint32_t slab = L::V + (q4 >> 1) * SLAB, src0 = tc::smem_u32(smem) + slab + row0;
+        const uint32_t to = tmem + TM_VW + ((uint32_t)(q4 * 32 + lg * 16) << 16);
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NV, n = tile_n(t), shift = rev ? 0 : LT - n;
             // (states alone: every tile's additions as they are at the end of the walk)
             const float tail = STATE_ONLY ? exp2f((rev ? tile_at(t) - t_begin : t_end - tile_at(t) - n) * g2) : 1.f;
             tc::mbar_wait(&sm->full_v[s], (t / NV) & 1, abort_flag, d_status);
-            const uint32_t src = base + slab + s * VB;
             __nv_bfloat162 odd = la_pair(0u);         // becomes NaN with the first entry that is not finite
 #pragma unroll 1
-            for (int hf = 0; hf < 2; ++hf) {
-                uint32_t w[4][3];
+            for (int qd = 0; qd < 4; ++qd) {
+                uint32_t r[8], w[4][3];
+                const uint32_t at = src0 + s * VB + qd * 4096;
+                tc::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]);
+                tc::ldmatrix_x4_trans(at + 2048, r[4], r[5], r[6], r[7]);      // (16 tokens on: same swizzle)
+                const int j0 = qd * 32 + (lane & 3) * 2;
+                if (!STATE_ONLY && n == LT) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int jj = hf * 64 + tk * 32 + c * 8 + (lane & 3) * 2;
-                    if (!STATE_ONLY && n == LT) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(sm->wsplit[jj >> 1]);
+                    for (int c = 0; c < 4; ++c) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(sm->wsplit[(j0 >> 1) + c * 4]);
                         w[c][0] = x.x; w[c][1] = x.y; w[c][2] = x.z;
-                    } else {
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int jj = j0 + c * 8;
                         la_split(jj < n ? tail * sm->weight[jj + shift] : 0.f, jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f, w[c]);
                     }
                 }
-#pragma unroll 1
-                for (int lg = 0; lg < 2; ++lg) {
-                    uint32_t r[8], p[4][8];
-                    const uint32_t at = src + tc::sw128_offset(hf * 64 + tok, ch0 + lg * 2);
-                    tc::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]);
-                    tc::ldmatrix_x4_trans(at + 16 * 128, r[4], r[5], r[6], r[7]);      // (16 tokens on: same swizzle)
-                    if (!STATE_ONLY)
+                if (2 * t + (qd >> 1) > 0) {          // (what stood in this half of the ring has been multiplied)
+                    tc::mbar_wait(&sm->vw_done[qd & 1], (qd >> 1) ^ 1, abort_flag, d_status);
+                    tc::tc_fence_after();
+                }
+                if (!STATE_ONLY)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) odd = __hfma2(la_pair(r[e]), la_pair(0u), odd);
-                    const uint32_t dst = to + ((uint32_t)(q4 * 32 + lg * 16) << 16);
-                    auto put = [&](int q) {
-                        const int u = unit + q;
-                        if (lg == 0 && u >= 4) {           // (the part that stood there has been multiplied)
-                            tc::mbar_wait(&sm->vw_done[u & 3], ((u >> 2) & 1) ^ 1, abort_flag, d_status);
-                            tc::tc_fence_after();
-                        }
-                        tc::tmem_st_16x128b_x4(dst + (u & 3) * 32, p[q]);
-                    };
-                    if (parts == 4) {
+                    for (int e = 0; e < 8; ++e) odd = __hfma2(la_pair(r[e]), la_pair(0u), odd);
+                const uint32_t dst = to + (qd & 1) * 64;
+                uint32_t p[8];
+                // (the remainder of a bf16 product is a bf16 number: la.h)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            uint32_t x[4];
-                            la_parts4(r[e], w[e >> 1], x);
-                            p[0][e] = x[0]; p[1][e] = x[1]; p[2][e] = x[2]; p[3][e] = x[3];
-                        }
-                        put(0);
-                        put(1);
-                        put(2);
-                        put(3);
-                    } else {
+                for (int e = 0; e < 8; ++e) p[e] = la_bits(__hmul2(la_pair(w[e >> 1][0]), la_pair(r[e])));
+                tc::tmem_st_16x128b_x4(dst, p);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            uint32_t x[4];
-                            la_parts2(r[e], w[e >> 1], x);
-                            p[0][e] = x[0]; p[1][e] = x[1];
-                        }
-                        put(0);
-                        put(1);
-                    }
+                for (int e = 0; e < 8; ++e) p[e] = la_bits(__hfma2(la_pair(w[e >> 1][0]), la_pair(r[e]), __hneg2(la_pair(p[e]))));
+                if (parts == 2) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = la_bits(__hfma2(la_pair(w[e >> 1][1]), la_pair(r[e]), la_pair(p[e])));
+                    tc::tmem_st_16x128b_x4(dst + 16, p);
+                } else {
+                    tc::tmem_st_16x128b_x4(dst + 16, p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = la_bits(__hmul2(la_pair(w[e >> 1][1]), la_pair(r[e])));
+                    tc::tmem_st_16x128b_x4(dst + 32, p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        p[e] = la_bits(__hfma2(la_pair(w[e >> 1][2]), la_pair(r[e]),
+                                               __hfma2(la_pair(w[e >> 1][1]), la_pair(r[e]), __hneg2(la_pair(p[e])))));
+                    tc::tmem_st_16x128b_x4(dst + 48, p);
                 }
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (!STATE_ONLY && hf == 1 && __any_sync(0xffffffffu, __hisnan(odd.x) || __hisnan(odd.y))) {
-                    // what is not finite gives way to zeros, now that both halves have been read; PV comes behind KV
+                if (!STATE_ONLY && qd == 3 && __any_sync(0xffffffffu, __hisnan(odd.x) || __hisnan(odd.y))) {
+                    // what is not finite gives way to zeros, now that all of it has been read; PV comes behind KV
                     ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
-                    {
+                    const int col = lg * 16 + (lane & 15);
 #pragma unroll 1
-                        for (int i = 0; i < 64; ++i) {
-                            unsigned short *e = reinterpret_cast<unsigned short *>(
-                                smem + slab + s * VB + tc::sw128_offset((i >> 5) * 64 + tk * 32 + (i & 31), (q4 & 1) * 4 + (lane >> 3))) + (lane & 7);
-                            if ((*e & 0x7f80) == 0x7f80) *e = 0;
-                        }
-                        tc::fence_proxy_async_smem();
-                        __syncwarp();
+                    for (int i = lane >> 4; i < LT; i += 2) {
+                        unsigned short *e = reinterpret_cast<unsigned short *>(
+                            smem + slab + s * VB + tc::sw128_offset(i, (q4 & 1) * 4 + (col >> 3))) + (col & 7);
+                        if ((*e & 0x7f80) == 0x7f80) *e = 0;
                     }
+                    tc::fence_proxy_async_smem();
+                    __syncwarp();
                 }
-                if (lane == 0) tc::mbar_arrive(&sm->vw_full[hf]);
-                unit += parts;
+                if (lane == 0) tc::mbar_arrive(&sm->vw_full[qd & 1]);
             }
             if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
         }
@@ -417,22 +406,27 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                             : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
                             : j.s_in   ? j.s_in + bh * ssize
                                        : nullptr;
+        if (!STATE_ONLY) {                       // the state that enters
+#pragma unroll 1
+            for (int c = 0; c < DK; c += 16) {
+                uint32_t x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
+                __syncwarp();
+                tc::tmem_st16(row + c, x);
+            }
+            tc::tmem_st_wait();
+        }
+        uint8_t *copy = smem + L::S + d * 128;   // (its chunks of 16 bytes are swizzled by the row)
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             const float dec = sm->pow[tile_n(t)];
-            const uint64_t dec2 = tc::f32x2(dec, dec);
-            uint32_t x[2][16];
-            auto fetch = [&](int c, uint32_t (&r)[16]) {
-                if (t > 0) tc::tmem_ld16(row + c, r);
-                else
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) r[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
-            };
             if (t > 0) {
                 tc::mbar_wait(&sm->kv_done, (t - 1) & 1, abort_flag, d_status);
                 tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
             }
-            fetch(0, x[0]);
+            uint32_t x[2][16];
+            tc::tmem_ld16(row, x[0]);
 #pragma unroll 1
             for (int c = 0; c < DK; c += 32) {
 #pragma unroll
@@ -440,22 +434,20 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     const int cz = c + z * 16;
                     uint32_t (&r)[16] = x[z];
                     tc::tmem_ld_wait();
-                    if (cz + 16 < DK) fetch(cz + 16, x[z ^ 1]);
-                    uint8_t *dst = smem + L::S + (cz >> 6) * SLAB;
+                    tc::tmem_ld16(row + (cz + 16) % DK, x[z ^ 1]);         // (behind the last: the first once more, unused)
+                    uint8_t *dst = copy + (cz >> 6) * SLAB;
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8)
-                        *reinterpret_cast<uint4 *>(dst + tc::sw128_offset(d, ((cz & 63) + e) >> 3)) =
-                            make_uint4(tc::f32x2_bf16(pair_of(r[e], r[e + 1])), tc::f32x2_bf16(pair_of(r[e + 2], r[e + 3])),
-                                       tc::f32x2_bf16(pair_of(r[e + 4], r[e + 5])), tc::f32x2_bf16(pair_of(r[e + 6], r[e + 7])));
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        const float2 v = tc::f32x2_get(tc::f32x2_mul(dec2, pair_of(r[e], r[e + 1])));
-                        r[e] = __float_as_uint(v.x);
-                        r[e + 1] = __float_as_uint(v.y);
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t *v = r + 8 * e;
+                        *reinterpret_cast<uint4 *>(dst + ((((cz & 63) >> 3) + e) ^ (d & 7)) * 16) = make_uint4(
+                            bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
                     }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
                     tc::tmem_st16(row + cz, r);
                 }
             }
+            tc::tmem_ld_wait();
             tc::tmem_st_wait();
             tc::fence_proxy_async_smem();
             tc::tc_fence_before();
@@ -484,7 +476,6 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             const int s = t % NV, n = tile_n(t), at = tile_at(t);
             const float w = r < n ? j.scale_c * sm->pow[rev ? n - 1 - r : r + 1] : 0.f;
-            const uint64_t w2 = tc::f32x2(w, w);
             tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll 1
@@ -493,11 +484,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::tmem_ld32(mine + c, x);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float2 v = tc::f32x2_get(tc::f32x2_mul(w2, pair_of(x[e], x[e + 1])));
-                    x[e] = __float_as_uint(v.x);
-                    x[e + 1] = __float_as_uint(v.y);
-                }
+                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(w * __uint_as_float(x[e]));
                 tc::tmem_st32(mine + c, x);
             }
             tc::tmem_st_wait();
@@ -550,8 +537,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
                         *reinterpret_cast<uint4 *>(stage + tc::sw128_offset(r, (c + e) >> 3)) =
-                            make_uint4(tc::f32x2_bf16(pair_of(y[e], y[e + 1])), tc::f32x2_bf16(pair_of(y[e + 2], y[e + 3])),
-                                       tc::f32x2_bf16(pair_of(y[e + 4], y[e + 5])), tc::f32x2_bf16(pair_of(y[e + 6], y[e + 7])));
+                            make_uint4(bits2(y[e], y[e + 1]), bits2(y[e + 2], y[e + 3]), bits2(y[e + 4], y[e + 5]), bits2(y[e + 6], y[e + 7]));
                 }
             }
             if (j.o_f32) {

@@ -154,10 +154,9 @@ def run(n, ns, state_only, rng):
 
 def run_wide(n, nq, state_only, rng):
     ns = {"q": nq, "k": nq + 1, "v": 3}
-    parts = rng.choice([2, 4])
     need = {f"{k}_{x}{s}": 1 for x in "qkv" for s in range(ns[x]) for k in ("full", "free")}
     need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "kv_done", "vw_full0",
-                                "vw_full1", "vw_done0", "vw_done1", "vw_done2", "vw_done3")})
+                                "vw_full1", "vw_done0", "vw_done1")})
     bars, buf = Bars(need), Buffers()
     odd = lambda t: not state_only and t % 3 == 1
     async_ops = []
@@ -185,11 +184,11 @@ def run_wide(n, nq, state_only, rng):
             queue.append(lambda: (buf.read(slot("k", t), t), buf.read(slot("q", t), t), buf.write("qk", ("a", t), 1),
                                   bars.arrive("qk_full")))
 
-        def half(t, hf, p, u):
+        def quarter(t, qd):
             def done():
-                buf.read(f"vw{u & 3}", u)
-                bars.arrive(f"vw_done{u & 3}")
-                if hf == 1 and p == parts - 1:
+                buf.read(f"vw{qd & 1}", 4 * t + qd)
+                bars.arrive(f"vw_done{qd & 1}")
+                if qd == 3:
                     buf.read(slot("k", t), t)
                     if not state_only:
                         buf.read("s_scaled", t)
@@ -200,7 +199,6 @@ def run_wide(n, nq, state_only, rng):
             queue.append(done)
         if not state_only and n:
             yield from scores(0)
-        u = 0
         for t in range(n):
             if state_only:
                 yield f"full_{slot('k', t)}", t // ns["k"]
@@ -210,11 +208,9 @@ def run_wide(n, nq, state_only, rng):
                     yield "o_free", t - 1
                 queue.append(lambda t=t: (buf.read(slot("q", t), t), buf.read("s16", t), buf.write("o", ("s", t), 1),
                                           bars.arrive("qs_done"), bars.arrive(f"free_{slot('q', t)}")))
-            for hf in (0, 1):
-                yield f"vw_full{hf}", t
-                for p in range(parts):
-                    half(t, hf, p, u)
-                    u += 1
+            for qd in range(4):
+                yield f"vw_full{qd & 1}", 2 * t + (qd >> 1)
+                quarter(t, qd)
             if state_only:
                 continue
             yield f"full_{slot('v', t)}", t // ns["v"]
@@ -237,24 +233,21 @@ def run_wide(n, nq, state_only, rng):
             bars.arrive("p_full")
 
     def values():
-        u = 0
         for t in range(n):
             v = slot("v", t)
             yield f"full_{v}", t // ns["v"]
-            for hf in (0, 1):
-                for p in range(parts):
-                    if u >= 4:
-                        yield f"vw_done{u & 3}", (u >> 2) - 1
-                    assert buf.v[v][0] == t, "w V from what replaced V"
-                    buf.write(f"vw{u & 3}", u, 1)
-                    u += 1
+            for qd in range(4):
+                if 2 * t + (qd >> 1):
+                    yield f"vw_done{qd & 1}", 2 * t + (qd >> 1) - 1
+                assert buf.v[v][0] == t, "w V from what replaced V"
+                buf.write(f"vw{qd & 1}", 4 * t + qd, 1)
                 yield None
-                if hf:
+                if qd == 3:
                     buf.read(v, t)
                     if odd(t):                            # what is not finite gives way to zeros
                         assert buf.v[v][1] == 1
                         buf.v[v] = [("z", t), 1]
-                bars.arrive(f"vw_full{hf}")
+                bars.arrive(f"vw_full{qd & 1}")
             if state_only:
                 bars.arrive(f"free_{v}")
 
