@@ -43,14 +43,14 @@ int check_sizes(swimba_handle *h, int32_t B, int32_t L)
 // Workspace of a call of njobs jobs: the segment states of each, then (gradients with shared heads) the per-head
 // gradients of queries and keys in fp32.
 struct LaLayout {
-    int seg_len, nseg;
+    int seg_len, nseg, per;
     size_t seg[LA_MAX_JOBS], dq, dk, total;
 };
 LaLayout la_layout(const swimba_handle *h, int B, int L, int njobs)
 {
     const swimba_config &c = h->cfg;
     LaLayout l;
-    la_plan(c.dtype, B, L, c.n_heads, c.d_state, c.head_dim, njobs, h->sm_count, &l.seg_len, &l.nseg);
+    la_plan(c.dtype, B, L, c.n_heads, c.d_state, c.head_dim, njobs, h->sm_count, &l.seg_len, &l.nseg, &l.per);
     size_t off = 0;
     for (int i = 0; i < njobs; ++i) {
         l.seg[i] = off;
@@ -103,7 +103,7 @@ int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void
     a.njobs = 1;
     a.log_decay = log_decay;
     a.B = B; a.L = L; a.H = c.n_heads;
-    a.seg_len = l.seg_len; a.nseg = l.nseg;
+    a.seg_len = l.seg_len; a.nseg = l.nseg; a.per = l.per;
     const int r = c.n_heads / c.n_groups;
     a.job[0] = LaJob{q, k, v, ldq, ldk, ldv, r, r, 1, c.d_state, c.head_dim, 0, 0, state_in, state_out, o, HP, 0,
                      scale, scale, 1.f, (float *)((char *)workspace + l.seg[0])};
@@ -147,7 +147,7 @@ int swimba_linear_attention_backward(swimba_handle *h, const float *log_decay, c
     a.njobs = 3;
     a.log_decay = log_decay;
     a.B = B; a.L = L; a.H = c.n_heads;
-    a.seg_len = l.seg_len; a.nseg = l.nseg;
+    a.seg_len = l.seg_len; a.nseg = l.nseg; a.per = l.per;
     const int r = c.n_heads / c.n_groups, N = c.d_state, P = c.head_dim;
     const bool shared = r > 1;
     void *gq = shared ? (void *)(ws + l.dq) : dq, *gk = shared ? (void *)(ws + l.dk) : dk;

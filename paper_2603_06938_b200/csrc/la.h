@@ -28,7 +28,7 @@ struct LaJob {
     int64_t ldo;
     int o_f32;                   // o is float whatever the dtype
     float scale_p, scale_c, scale_a;   // of the scores inside a tile, of the carried state's part, of what the state adds
-    float *seg;                  // [B, H, nseg] states in the layout of s_in, when sequences are cut
+    float *seg;                  // [B, H, nseg per] states in the layout of s_in, when sequences are cut
 };
 
 constexpr int LA_MAX_JOBS = 3;
@@ -38,6 +38,7 @@ struct LaArgs {
     const float *log_decay;      // [H]
     int B, L, H;
     int seg_len, nseg;           // tokens per segment (the last in the sequence may be shorter), segments per sequence
+    int per;                     // pieces per segment, of seg_len / per tokens, that the pass for the states works
 };
 
 // log2 of the decay.  Held above -1e4, where one step underflows to nothing already, so that the zeroth
@@ -75,7 +76,7 @@ __device__ __forceinline__ void la_split(float w0, float w1, uint32_t (&p)[3])
 __device__ __forceinline__ __nv_bfloat162 la_pair(uint32_t v) { return *reinterpret_cast<const __nv_bfloat162 *>(&v); }
 __device__ __forceinline__ uint32_t la_bits(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
 // Segments the kernels cut every sequence of a call into, and the bytes they keep for that.
-void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg);
+void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg, int *per);
 // (bytes of one job's segment states; grows with B and with L)
 size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count);
 // Tensor map of [B, L, streams, D], rows ld apart, for boxes of 128 tokens of 64 entries of one stream.  Rows behind

@@ -83,16 +83,17 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     id /= slices;
     const int ji = (int)(id % a.njobs);
     id /= a.njobs;
-    const int nrun = STATE_ONLY ? a.nseg - 1 : a.nseg;     // (the last segment's end state enters nothing)
-    const int seg = (int)(id % nrun);                      // in the order of the walk
+    // segments, or pieces of them for the states alone, in the order of the walk (the last segment's end state enters nothing)
+    const int nall = STATE_ONLY ? a.nseg * a.per : a.nseg, nrun = STATE_ONLY ? nall - a.per : nall;
+    const int seg = (int)(id % nrun), len = STATE_ONLY ? a.seg_len / a.per : a.seg_len;
     id /= nrun;
     const int h = (int)(id % a.H), b = (int)(id / a.H);
     const LaJob &j = a.job[ji];
     const bool rev = j.reverse != 0;
     // three parts where the state is a result; two (2^-16) where only the read of it is, whose copy is rounded to bf16
     const int parts = j.s_out ? 3 : 2;
-    const int place = rev ? a.nseg - 1 - seg : seg;
-    const int t_begin = place * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    const int place = rev ? nall - 1 - seg : seg;
+    const int t_begin = min(a.L, place * len), t_end = min(a.L, t_begin + len);
     const int ntiles = (t_end - t_begin + LT - 1) / LT;
     auto tile_at = [&](int t) { return t_begin + (rev ? ntiles - 1 - t : t) * LT; };       // first token of tile t
     auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
@@ -388,7 +389,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         const int64_t at0 = j.transposed ? (int64_t)d * j.dv + c0 + cc : (int64_t)(c0 + cc) * DK + d;
         const int64_t step = j.transposed ? 1 : DK;
         const float *from = STATE_ONLY ? nullptr
-                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
+                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
                             : j.s_in   ? j.s_in + bh * ssize
                                        : nullptr;
         uint64_t st[NC / 2];
@@ -433,7 +434,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->kv_read);
         }
-        float *to = STATE_ONLY ? j.seg + (bh * a.nseg + seg + 1) * ssize
+        float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
                     : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
         if (to) {
 #pragma unroll
@@ -542,7 +543,7 @@ bool run_tiles(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 {
     const size_t smem = Sm<DK>::SMALL + sizeof(Small);
     if (!ensure_dynamic_smem((const void *)la_tiles_kernel<DK, STATE_ONLY>, smem)) return false;
-    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? a.nseg - 1 : a.nseg) * (a.job[0].dv / LDV);
+    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.per : a.nseg) * (a.job[0].dv / LDV);
     ctx.begin(STATE_ONLY ? STAGE_LA_STATES : STAGE_LA_TILES);
     launch_kernel(la_tiles_kernel<DK, STATE_ONLY>, dim3((unsigned)n), dim3(THREADS), smem, ctx.stream, true, maps, a,
                   ctx.d_status);

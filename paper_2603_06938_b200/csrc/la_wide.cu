@@ -24,7 +24,7 @@ constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
 // warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 4 for the state, 8 for o
 constexpr int THREADS = 1024;
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 24;
-// tensor memory columns: scores and over them P (bf16), O, S, w V of two quarters of a tile, up to four parts of each
+// tensor memory columns: scores and over them P (bf16), O, S, w V of quarters of a tile: four of them in two parts, or two in four
 constexpr uint32_t TM_QK = 0, TM_O = 128, TM_S = 256, TM_VW = 384, TM_COLS = 512;
 
 template <int DK> struct Sm {
@@ -35,7 +35,7 @@ template <int DK> struct Sm {
 };
 struct Small {
     uint64_t full_q[2], full_k[3], full_v[3], free_q[2], free_k[3], free_v[3];
-    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, kv_done, vw_full[2], vw_done[2];
+    uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, s_scaled, kv_done, vw_full[4], vw_done[4];
     uint32_t tmem;
     int abort_flag;
     int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
@@ -73,16 +73,17 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     int64_t id = blockIdx.x;
     const int ji = (int)(id % a.njobs);
     id /= a.njobs;
-    const int nrun = STATE_ONLY ? a.nseg - 1 : a.nseg;     // (the last segment's end state enters nothing)
-    const int seg = (int)(id % nrun);                      // in the order of the walk
+    // segments, or pieces of them for the states alone, in the order of the walk (the last segment's end state enters nothing)
+    const int nall = STATE_ONLY ? a.nseg * a.per : a.nseg, nrun = STATE_ONLY ? nall - a.per : nall;
+    const int seg = (int)(id % nrun), len = STATE_ONLY ? a.seg_len / a.per : a.seg_len;
     id /= nrun;
     const int h = (int)(id % a.H), b = (int)(id / a.H);
     const LaJob &j = a.job[ji];
     const bool rev = j.reverse != 0;
     // four parts where the state is a result; two where only the read of it is, whose copy is rounded to bf16
-    const int parts = j.s_out ? 4 : 2;
-    const int place = rev ? a.nseg - 1 - seg : seg;
-    const int t_begin = place * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    const int parts = j.s_out ? 4 : 2, ring = 8 / parts;       // quarters of w V there is room for
+    const int place = rev ? nall - 1 - seg : seg;
+    const int t_begin = min(a.L, place * len), t_end = min(a.L, t_begin + len);
     const int ntiles = (t_end - t_begin + LT - 1) / LT;
     auto tile_at = [&](int t) { return t_begin + (rev ? ntiles - 1 - t : t) * LT; };       // first token of tile t
     auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
@@ -100,7 +101,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             tc::mbar_init(&sm->full_v[s], 1);
             tc::mbar_init(&sm->free_v[s], STATE_ONLY || j.o_f32 ? 8 : 2);
         }
-        for (int s = 0; s < 2; ++s) tc::mbar_init(&sm->vw_done[s], 1);
+        for (int s = 0; s < 4; ++s) {
+            tc::mbar_init(&sm->vw_full[s], 8);
+            tc::mbar_init(&sm->vw_done[s], 1);
+        }
         sm->odd_tile[0] = sm->odd_tile[1] = 0;
         tc::mbar_init(&sm->qk_full, 1);
         tc::mbar_init(&sm->p_full, 8);
@@ -109,9 +113,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         tc::mbar_init(&sm->pv_done, 1);
         tc::mbar_init(&sm->o_free, 8);
         tc::mbar_init(&sm->s_full, 4);
+        tc::mbar_init(&sm->s_scaled, 4);
         tc::mbar_init(&sm->kv_done, 1);
-        tc::mbar_init(&sm->vw_full[0], 8);
-        tc::mbar_init(&sm->vw_full[1], 8);
         *abort_flag = 0;
         tc::fence_mbar_init();
     }
@@ -226,15 +229,16 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             // KV, by quarters of the tile
 #pragma unroll 1
             for (int qd = 0; qd < 4; ++qd) {
-                const int buf = qd & 1;
-                tc::mbar_wait(&sm->vw_full[buf], qd >> 1, abort_flag, d_status);
+                const int buf = qd & (ring - 1);
+                tc::mbar_wait(&sm->vw_full[buf], parts == 4 ? qd >> 1 : t & 1, abort_flag, d_status);
+                if (!STATE_ONLY && qd == 0) tc::mbar_wait(&sm->s_scaled, t & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 if (leader) {
                     uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + qd * 4096));
 #pragma unroll 1
                     for (int p = 0; p < parts; ++p) {
-                        tc::mma_ts(tm + TM_S, tm + TM_VW + buf * 64 + p * 16, k, id_kv, !STATE_ONLY || t + qd + p > 0);
-                        tc::mma_ts(tm + TM_S, tm + TM_VW + buf * 64 + p * 16 + 8, tc::smem_desc_advance(k, 2048), id_kv, 1);
+                        tc::mma_ts(tm + TM_S, tm + TM_VW + (buf * parts + p) * 16, k, id_kv, !STATE_ONLY || t + qd + p > 0);
+                        tc::mma_ts(tm + TM_S, tm + TM_VW + (buf * parts + p) * 16 + 8, tc::smem_desc_advance(k, 2048), id_kv, 1);
                     }
                     tc::mma_commit(&sm->vw_done[buf]);
                     if (qd == 3) {
@@ -345,14 +349,15 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                         la_split(jj < n ? tail * sm->weight[jj + shift] : 0.f, jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f, w[c]);
                     }
                 }
-                if (2 * t + (qd >> 1) > 0) {          // (what stood in this half of the ring has been multiplied)
-                    tc::mbar_wait(&sm->vw_done[qd & 1], (qd >> 1) ^ 1, abort_flag, d_status);
+                const int buf = qd & (ring - 1);
+                if (4 * t + qd >= ring) {             // (what stood in this place of the ring has been multiplied)
+                    tc::mbar_wait(&sm->vw_done[buf], (parts == 4 ? qd >> 1 : t & 1) ^ 1, abort_flag, d_status);
                     tc::tc_fence_after();
                 }
                 if (!STATE_ONLY)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) odd = __hfma2(la_pair(r[e]), la_pair(0u), odd);
-                const uint32_t dst = to + (qd & 1) * 64;
+                const uint32_t dst = to + buf * parts * 16;
                 uint32_t p[8];
                 // (the remainder of a bf16 product is a bf16 number: la.h)
 #pragma unroll
@@ -391,7 +396,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     tc::fence_proxy_async_smem();
                     __syncwarp();
                 }
-                if (lane == 0) tc::mbar_arrive(&sm->vw_full[qd & 1]);
+                if (lane == 0) tc::mbar_arrive(&sm->vw_full[buf]);
             }
             if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
         }
@@ -403,7 +408,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * DV;
         const int64_t at0 = j.transposed ? d : (int64_t)d * DK, step = j.transposed ? DV : 1;
         const float *from = STATE_ONLY ? nullptr
-                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
+                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
                             : j.s_in   ? j.s_in + bh * ssize
                                        : nullptr;
         if (!STATE_ONLY) {                       // the state that enters
@@ -425,40 +430,49 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
             }
+            // the copy first: QS runs while the state is scaled for KV to add to
             uint32_t x[2][16];
-            tc::tmem_ld16(row, x[0]);
 #pragma unroll 1
-            for (int c = 0; c < DK; c += 32) {
+            for (int pass = 0; pass < 2; ++pass) {
+                tc::tmem_ld16(row, x[0]);
+#pragma unroll 1
+                for (int c = 0; c < DK; c += 32) {
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const int cz = c + z * 16;
-                    uint32_t (&r)[16] = x[z];
-                    tc::tmem_ld_wait();
-                    tc::tmem_ld16(row + (cz + 16) % DK, x[z ^ 1]);         // (behind the last: the first once more, unused)
-                    uint8_t *dst = copy + (cz >> 6) * SLAB;
+                    for (int z = 0; z < 2; ++z) {
+                        const int cz = c + z * 16;
+                        uint32_t (&r)[16] = x[z];
+                        tc::tmem_ld_wait();
+                        tc::tmem_ld16(row + (cz + 16) % DK, x[z ^ 1]);     // (behind the last: the first once more, unused)
+                        if (pass == 0) {
+                            uint8_t *dst = copy + (cz >> 6) * SLAB;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t *v = r + 8 * e;
-                        *reinterpret_cast<uint4 *>(dst + ((((cz & 63) >> 3) + e) ^ (d & 7)) * 16) = make_uint4(
-                            bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t *v = r + 8 * e;
+                                *reinterpret_cast<uint4 *>(dst + ((((cz & 63) >> 3) + e) ^ (d & 7)) * 16) = make_uint4(
+                                    bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
+                            tc::tmem_st16(row + cz, r);
+                        }
                     }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
-                    tc::tmem_st16(row + cz, r);
                 }
+                tc::tmem_ld_wait();
+                if (pass == 0) tc::fence_proxy_async_smem();
+                else tc::tmem_st_wait();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(pass == 0 ? &sm->s_full : &sm->s_scaled);
             }
-            tc::tmem_ld_wait();
-            tc::tmem_st_wait();
-            tc::fence_proxy_async_smem();
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sm->s_full);
         }
-        float *to = STATE_ONLY ? j.seg + (bh * a.nseg + seg + 1) * ssize
+        float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
                     : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
-        if (to && ntiles > 0) {
-            tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - 1) & 1, abort_flag, d_status);
-            tc::tc_fence_after();
+        if (to) {
+            if (ntiles > 0) {
+                tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - 1) & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+            }
 #pragma unroll 1
             for (int c = 0; c < DK; c += 32) {
                 uint32_t x[32];
@@ -466,7 +480,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::tmem_ld32(row + c, x);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) to[at0 + (c + e) * step] = __uint_as_float(x[e]);
+                for (int e = 0; e < 32; ++e) to[at0 + (c + e) * step] = ntiles > 0 ? __uint_as_float(x[e]) : 0.f;
             }
         }
     } else if (warp >= WARP_O) {
@@ -568,7 +582,7 @@ bool run_wide(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 {
     const size_t smem = Sm<DK>::SMALL + sizeof(Small);
     if (!ensure_dynamic_smem((const void *)la_wide_kernel<DK, STATE_ONLY>, smem)) return false;
-    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? a.nseg - 1 : a.nseg);
+    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.per : a.nseg);
     ctx.begin(STATE_ONLY ? STAGE_LA_STATES : STAGE_LA_TILES);
     launch_kernel(la_wide_kernel<DK, STATE_ONLY>, dim3((unsigned)n), dim3(THREADS), smem, ctx.stream, true, maps, a,
                   ctx.d_status);

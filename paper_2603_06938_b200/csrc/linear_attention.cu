@@ -127,8 +127,8 @@ la_steps_kernel(const __grid_constant__ LaArgs a)
 
 }  // namespace
 
-// seg[.., i] holds the end state of segment i - 1 from a zero entry (i >= 1); on exit the state that enters
-// segment i.  One thread per four entries walks a sequence's segments.
+// seg[.., i] holds the end state of piece i - 1 from a zero entry (i >= 1); on exit the state that enters piece i.  One
+// thread per four entries walks a sequence's pieces.
 __global__ void __launch_bounds__(256)
 la_chain_kernel(const __grid_constant__ LaArgs a)
 {
@@ -140,15 +140,17 @@ la_chain_kernel(const __grid_constant__ LaArgs a)
     if (i >= ssize) return;
     const int h = (int)(blockIdx.y % a.H);
     const double l2 = la_log2_decay(a.log_decay[h]);
-    // every segment but the sequence's last, the first of a walk backward, is whole
-    const float whole = (float)exp2(l2 * a.seg_len), first = j.reverse ? (float)exp2(l2 * (a.L - (a.nseg - 1) * a.seg_len)) : whole;
+    // every piece but the sequence's last, the first of a walk backward, is whole (and behind the last there may be empty ones)
+    const int len = a.seg_len / a.per, all = a.nseg * a.per, last = (a.nseg - 1) * a.per;
+    const float whole = (float)exp2(l2 * len);
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.s_in) s = *reinterpret_cast<const float4 *>(j.s_in + blockIdx.y * ssize + i);
-    float *p = j.seg + (int64_t)blockIdx.y * a.nseg * ssize + i;
+    float *p = j.seg + (int64_t)blockIdx.y * all * ssize + i;
 #pragma unroll 4
-    for (int g = 1; g < a.nseg; ++g) {
+    for (int g = 1; g <= last; ++g) {
         const float4 l = *reinterpret_cast<const float4 *>(p + g * ssize);
-        const float lam = g == 1 ? first : whole;
+        const int tokens = j.reverse ? a.L - (all - g) * len : len;        // of the piece in front
+        const float lam = tokens >= len ? whole : (float)exp2(l2 * max(0, tokens));
         s.x = fmaf(lam, s.x, l.x);
         s.y = fmaf(lam, s.y, l.y);
         s.z = fmaf(lam, s.z, l.z);
@@ -318,16 +320,17 @@ namespace {
 // What a segment's length is a multiple of: token-by-token segments have 64 tokens at least, tiles 128.
 constexpr int LA_STEP_SEG = 64, LA_TILE_SEG = 128;
 // The most segments a sequence is cut into: token by token, as many as give every SM two blocks; by tiles, as many
-// as fill two waves.
+// as fill four waves (pieces included).
 int la_most(bool tiles, int B, int H, int N, int P, int njobs, int sm_count)
 {
     const int64_t blocks = (int64_t)njobs * B * H * (tiles ? 1 : ceil_div(std::max(N, P), LA_COLS));
-    return (int)std::max<int64_t>(1, 2 * sm_count / blocks);
+    return (int)std::max<int64_t>(1, (tiles ? 4 : 2) * sm_count / blocks);
 }
 }  // namespace
 
-void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg)
+void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg, int *per)
 {
+    *per = 1;
     const bool tiles = la_tiles_shape(dtype, N, P);
     const int most = la_most(tiles, B, H, N, P, njobs, sm_count);
     if (!tiles) {
@@ -336,26 +339,36 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
         *nseg = ceil_div(L, *seg_len);
         return;
     }
-    // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states
-    // (about 0.6 of a tile each) with what two more launches take (about 6 tiles).
+    // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states (about
+    // 0.7 of a tile each, in pieces that fill the SMs), their chain (0.15 a piece) and two more launches (about 4).
     const int nt = ceil_div(L, LA_TILE_SEG);
     const int64_t items = (int64_t)njobs * B * H;
     double best = 1e30;
     for (int n = 1; n <= std::min(most, nt); ++n) {
         const int len = ceil_div(nt, n), ns = ceil_div(nt, len);
-        const double cost = (double)ceil_div64(items * ns, sm_count) * len +
-                            (ns > 1 ? 0.6 * ceil_div64(items * (ns - 1), sm_count) * len + 6 : 0);
+        double states = 0;
+        int pieces = 1;
+        if (ns > 1) {
+            states = 1e30;
+            for (int p = 1; p <= 4 && p * ns <= most; ++p) {
+                if (len % p != 0) continue;
+                const double c = 0.7 * ceil_div64(items * (ns - 1) * p, sm_count) * (len / p) + 4 + 0.15 * ns * p;
+                if (c < states) { states = c; pieces = p; }
+            }
+        }
+        const double cost = (double)ceil_div64(items * ns, sm_count) * len + states;
         if (cost < best) {
             best = cost;
             *seg_len = len * LA_TILE_SEG;
             *nseg = ns;
+            *per = pieces;
         }
     }
 }
 
 size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count)
 {
-    // the most that a call of up to B sequences and L tokens is cut into; none where sequences stay whole
+    // the most pieces that a call of up to B sequences and L tokens is cut into; none where sequences stay whole
     const bool tiles = la_tiles_shape(dtype, N, P);
     int64_t most = 0;
     for (int b = 1; b <= B; ++b) {

@@ -155,8 +155,9 @@ def run(n, ns, state_only, rng):
 def run_wide(n, nq, state_only, rng):
     ns = {"q": nq, "k": nq + 1, "v": 3}
     need = {f"{k}_{x}{s}": 1 for x in "qkv" for s in range(ns[x]) for k in ("full", "free")}
-    need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "kv_done", "vw_full0",
-                                "vw_full1", "vw_done0", "vw_done1")})
+    need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "s_scaled", "kv_done")})
+    ring = rng.choice([2, 4])                             # quarters of w V there is room for
+    need.update({f"vw_{k}{i}": 1 for i in range(ring) for k in ("full", "done")})
     bars, buf = Bars(need), Buffers()
     odd = lambda t: not state_only and t % 3 == 1
     async_ops = []
@@ -186,8 +187,8 @@ def run_wide(n, nq, state_only, rng):
 
         def quarter(t, qd):
             def done():
-                buf.read(f"vw{qd & 1}", 4 * t + qd)
-                bars.arrive(f"vw_done{qd & 1}")
+                buf.read(f"vw{qd % ring}", 4 * t + qd)
+                bars.arrive(f"vw_done{qd % ring}")
                 if qd == 3:
                     buf.read(slot("k", t), t)
                     if not state_only:
@@ -209,7 +210,9 @@ def run_wide(n, nq, state_only, rng):
                 queue.append(lambda t=t: (buf.read(slot("q", t), t), buf.read("s16", t), buf.write("o", ("s", t), 1),
                                           bars.arrive("qs_done"), bars.arrive(f"free_{slot('q', t)}")))
             for qd in range(4):
-                yield f"vw_full{qd & 1}", 2 * t + (qd >> 1)
+                yield f"vw_full{qd % ring}", (4 * t + qd) // ring
+                if not state_only and qd == 0:
+                    yield "s_scaled", t
                 quarter(t, qd)
             if state_only:
                 continue
@@ -237,17 +240,17 @@ def run_wide(n, nq, state_only, rng):
             v = slot("v", t)
             yield f"full_{v}", t // ns["v"]
             for qd in range(4):
-                if 2 * t + (qd >> 1):
-                    yield f"vw_done{qd & 1}", 2 * t + (qd >> 1) - 1
+                if 4 * t + qd >= ring:
+                    yield f"vw_done{qd % ring}", (4 * t + qd) // ring - 1
                 assert buf.v[v][0] == t, "w V from what replaced V"
-                buf.write(f"vw{qd & 1}", 4 * t + qd, 1)
+                buf.write(f"vw{qd % ring}", 4 * t + qd, 1)
                 yield None
                 if qd == 3:
                     buf.read(v, t)
                     if odd(t):                            # what is not finite gives way to zeros
                         assert buf.v[v][1] == 1
                         buf.v[v] = [("z", t), 1]
-                bars.arrive(f"vw_full{qd & 1}")
+                bars.arrive(f"vw_full{qd % ring}")
             if state_only:
                 bars.arrive(f"free_{v}")
 
@@ -276,10 +279,12 @@ def run_wide(n, nq, state_only, rng):
                 yield "kv_done", t - 1
                 buf.read("s", t)
                 yield "qs_done", t - 1
-            buf.write("s_scaled", t, 1)
             buf.write("s16", t, 1)
             yield None
             bars.arrive("s_full")
+            buf.write("s_scaled", t, 1)
+            yield None
+            bars.arrive("s_scaled")
         if state_only and n:
             yield "kv_done", 0
 
