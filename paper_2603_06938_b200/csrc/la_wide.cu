@@ -21,9 +21,9 @@ constexpr int LT = 128;                      // tokens per tile
 constexpr int DV = 128;
 constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
 constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
-// warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 4 for the state, 8 for o
-constexpr int THREADS = 1024;
-constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_STATE = 20, WARP_O = 24;
+// warps: copies, products, tensor memory, spare; 8 for the masks and, while scores are made, the state, 8 for w V, 8 for o
+constexpr int THREADS = 896;
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_O = 20;
 // tensor memory columns: scores and over them P (bf16), O, S, w V of quarters of a tile: four of them in two parts, or two in four
 constexpr uint32_t TM_QK = 0, TM_O = 128, TM_S = 256, TM_VW = 384, TM_COLS = 512;
 
@@ -112,8 +112,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         tc::mbar_init(&sm->o_scaled, 8);
         tc::mbar_init(&sm->pv_done, 1);
         tc::mbar_init(&sm->o_free, 8);
-        tc::mbar_init(&sm->s_full, 4);
-        tc::mbar_init(&sm->s_scaled, 4);
+        tc::mbar_init(&sm->s_full, 8);
+        tc::mbar_init(&sm->s_scaled, 8);
         tc::mbar_init(&sm->kv_done, 1);
         *abort_flag = 0;
         tc::fence_mbar_init();
@@ -162,8 +162,22 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         auto load_q = [&](int t) { if (!STATE_ONLY) load(t, NQ, sm->full_q, sm->free_q, L::Q, L::QB, &maps.q[ji], h / j.rq); };
         auto load_k = [&](int t) { load(t, NK, sm->full_k, sm->free_k, L::K, L::QB, &maps.k[ji], h / j.rk); };
         auto load_v = [&](int t) { load(t, NV, sm->full_v, sm->free_v, L::V, VB, &maps.v[ji], h / j.rv); };
+        // with one Q tile at a time the next one's load is waited for: its rows are brought to L2 a step before
+        auto ahead_q = [&](int t) {
+            if (STATE_ONLY || NQ > 1 || t >= ntiles) return;
+#pragma unroll 1
+            for (int r = tile_at(t) + lane; r < tile_at(t) + tile_n(t); r += 32) {
+                const char *p = (const char *)((const __nv_bfloat16 *)j.q + ((int64_t)b * a.L + r) * j.ldq + (int64_t)(h / j.rq) * DK);
+#pragma unroll
+                for (int o = 0; o < DK * 2; o += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + o));
+            }
+            __syncwarp();
+        };
         for (int t = -NV; t < ntiles; ++t) {
-            if (t + NQ >= 0) load_q(t + NQ);
+            if (t + NQ >= 0) {
+                load_q(t + NQ);
+                ahead_q(t + NQ + 1);
+            }
             if (t + NK >= 0) load_k(t + NK);
             load_v(t + NV);
         }
@@ -271,11 +285,70 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         }
     } else if (warp >= WARP_MASK && warp < WARP_W) {
         // ------------------------------------------------------------------ masks: half a row of the scores per thread, its
-        // result over the first half of what it was made from
+        // result over the first half of what it was made from; and the state, half a value's row per thread: between two
+        // tiles its bf16 copy for QS goes to shared memory and it is scaled where it stands
         const int q4 = warp & 3, half = (warp - WARP_MASK) >> 2, i = q4 * 32 + lane;
-        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_QK + half * 64;
+        const uint32_t quarter = tmem + ((uint32_t)(q4 * 32) << 16), row = quarter + TM_QK + half * 64;
         const float scale_p = j.scale_p;
         const uint32_t keep = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+        constexpr int NC = DK / 2;
+        const uint32_t srow = quarter + TM_S + half * NC;
+        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * DV;
+        const int64_t at0 = j.transposed ? (int64_t)half * NC * DV + i : (int64_t)i * DK + half * NC, step = j.transposed ? DV : 1;
+        if (!STATE_ONLY) {                       // the state that enters
+            const float *from = seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
+                                : j.s_in ? j.s_in + bh * ssize
+                                         : nullptr;
+#pragma unroll 1
+            for (int c = 0; c < NC; c += 16) {
+                uint32_t x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
+                __syncwarp();
+                tc::tmem_st16(srow + c, x);
+            }
+            tc::tmem_st_wait();
+        }
+        uint8_t *copy = smem + L::S + i * 128 + (DK == 128 ? half * SLAB : 0);       // (its chunks of 16 bytes are swizzled by the row)
+        const int chunk0 = DK == 128 ? 0 : half * 4;
+        // the state that enters tile t; the copy first: QS runs while the state is scaled for KV to add to
+        auto hand_over = [&](int t) {
+            const float dec = sm->pow[tile_n(t)];
+            uint32_t x[2][16];
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {
+                tc::tmem_ld16(srow, x[0]);
+#pragma unroll 1
+                for (int c = 0; c < NC; c += 32) {
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const int cz = c + z * 16;
+                        uint32_t (&r)[16] = x[z];
+                        tc::tmem_ld_wait();
+                        tc::tmem_ld16(srow + (cz + 16) % NC, x[z ^ 1]);    // (behind the last: the first once more, unused)
+                        if (pass == 0) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t *v = r + 8 * e;
+                                *reinterpret_cast<uint4 *>(copy + (((chunk0 + (cz >> 3) + e) ^ (i & 7)) * 16)) = make_uint4(
+                                    bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
+                            tc::tmem_st16(srow + cz, r);
+                        }
+                    }
+                }
+                tc::tmem_ld_wait();
+                if (pass == 0) tc::fence_proxy_async_smem();
+                else tc::tmem_st_wait();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(pass == 0 ? &sm->s_full : &sm->s_scaled);
+            }
+        };
+        if (!STATE_ONLY && ntiles > 0) hand_over(0);
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             tc::mbar_wait(&sm->qk_full, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
@@ -314,8 +387,31 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->p_full);
+            if (t + 1 < ntiles) {
+                tc::mbar_wait(&sm->kv_done, t & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+                hand_over(t + 1);
+            }
         }
-    } else if (warp >= WARP_W && warp < WARP_STATE) {
+        float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
+                    : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
+        if (to) {
+            if (ntiles > 0) {
+                tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - 1) & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+            }
+#pragma unroll 1
+            for (int c = 0; c < NC; c += 16) {
+                uint32_t x[16];
+                __syncwarp();
+                tc::tmem_ld16(srow + c, x);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) to[at0 + (c + e) * step] = ntiles > 0 ? __uint_as_float(x[e]) : 0.f;
+            }
+        }
+    } else if (warp >= WARP_W && warp < WARP_O) {
         // ------------------------------------------------------------------ (w V)^T: 16 values of a quarter of a tile, 32
         // tokens, transposed on the way from shared memory
         const int q4 = warp & 3, lg = (warp - WARP_W) >> 2;
@@ -399,89 +495,6 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 if (lane == 0) tc::mbar_arrive(&sm->vw_full[buf]);
             }
             if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
-        }
-    } else if (warp >= WARP_STATE && warp < WARP_O) {
-        // ------------------------------------------------------------------ the state, a value's row per thread: between two
-        // tiles its bf16 copy for QS goes to shared memory and it is scaled where it stands
-        const int q4 = warp & 3, d = q4 * 32 + lane;
-        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_S;
-        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * DV;
-        const int64_t at0 = j.transposed ? d : (int64_t)d * DK, step = j.transposed ? DV : 1;
-        const float *from = STATE_ONLY ? nullptr
-                            : seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
-                            : j.s_in   ? j.s_in + bh * ssize
-                                       : nullptr;
-        if (!STATE_ONLY) {                       // the state that enters
-#pragma unroll 1
-            for (int c = 0; c < DK; c += 16) {
-                uint32_t x[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
-                __syncwarp();
-                tc::tmem_st16(row + c, x);
-            }
-            tc::tmem_st_wait();
-        }
-        uint8_t *copy = smem + L::S + d * 128;   // (its chunks of 16 bytes are swizzled by the row)
-        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
-            const float dec = sm->pow[tile_n(t)];
-            if (t > 0) {
-                tc::mbar_wait(&sm->kv_done, (t - 1) & 1, abort_flag, d_status);
-                tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
-                tc::tc_fence_after();
-            }
-            // the copy first: QS runs while the state is scaled for KV to add to
-            uint32_t x[2][16];
-#pragma unroll 1
-            for (int pass = 0; pass < 2; ++pass) {
-                tc::tmem_ld16(row, x[0]);
-#pragma unroll 1
-                for (int c = 0; c < DK; c += 32) {
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const int cz = c + z * 16;
-                        uint32_t (&r)[16] = x[z];
-                        tc::tmem_ld_wait();
-                        tc::tmem_ld16(row + (cz + 16) % DK, x[z ^ 1]);     // (behind the last: the first once more, unused)
-                        if (pass == 0) {
-                            uint8_t *dst = copy + (cz >> 6) * SLAB;
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint32_t *v = r + 8 * e;
-                                *reinterpret_cast<uint4 *>(dst + ((((cz & 63) >> 3) + e) ^ (d & 7)) * 16) = make_uint4(
-                                    bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
-                            }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
-                            tc::tmem_st16(row + cz, r);
-                        }
-                    }
-                }
-                tc::tmem_ld_wait();
-                if (pass == 0) tc::fence_proxy_async_smem();
-                else tc::tmem_st_wait();
-                tc::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(pass == 0 ? &sm->s_full : &sm->s_scaled);
-            }
-        }
-        float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
-                    : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
-        if (to) {
-            if (ntiles > 0) {
-                tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - 1) & 1, abort_flag, d_status);
-                tc::tc_fence_after();
-            }
-#pragma unroll 1
-            for (int c = 0; c < DK; c += 32) {
-                uint32_t x[32];
-                __syncwarp();
-                tc::tmem_ld32(row + c, x);
-                tc::tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 32; ++e) to[at0 + (c + e) * step] = ntiles > 0 ? __uint_as_float(x[e]) : 0.f;
-            }
         }
     } else if (warp >= WARP_O) {
         // ------------------------------------------------------------------ o: half a row per thread, staged where V stood

@@ -227,13 +227,31 @@ def run_wide(n, nq, state_only, rng):
                     yield "o_free", t
                 yield from scores(t + 1)
 
-    def masks():
+    def masks():                                          # and the state
+        def hand_over(t):
+            if t:
+                buf.read("s", t)
+            buf.write("s16", t, 1)
+            yield None
+            bars.arrive("s_full")
+            buf.write("s_scaled", t, 1)
+            yield None
+            bars.arrive("s_scaled")
+        if state_only:
+            if n:
+                yield "kv_done", 0
+            return
+        yield from hand_over(0)
         for t in range(n):
             yield "qk_full", t
             buf.read("qk", ("a", t))
             buf.write("qk", ("p", t), 1 + odd(t))
             yield None
             bars.arrive("p_full")
+            if t + 1 < n:
+                yield "kv_done", t
+                yield "qs_done", t
+                yield from hand_over(t + 1)
 
     def values():
         for t in range(n):
@@ -273,22 +291,7 @@ def run_wide(n, nq, state_only, rng):
             buf.read(v, f"o{t}")
             bars.arrive(f"free_{v}")
 
-    def state():
-        for t in range(0 if state_only else n):
-            if t:
-                yield "kv_done", t - 1
-                buf.read("s", t)
-                yield "qs_done", t - 1
-            buf.write("s16", t, 1)
-            yield None
-            bars.arrive("s_full")
-            buf.write("s_scaled", t, 1)
-            yield None
-            bars.arrive("s_scaled")
-        if state_only and n:
-            yield "kv_done", 0
-
-    drive([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]), bars, async_ops, rng)
+    drive([tma(), mma(), values(), masks()] + ([] if state_only else [outputs()]), bars, async_ops, rng)
 
 
 def drive(roles, bars, async_ops, rng):
