@@ -107,7 +107,7 @@ int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void
     const int r = c.n_heads / c.n_groups;
     a.job[0] = LaJob{q, k, v, ldq, ldk, ldv, r, r, 1, c.d_state, c.head_dim, 0, 0, state_in, state_out, o, HP, 0,
                      scale, scale, 1.f, (float *)((char *)workspace + l.seg[0])};
-    return close_ctx(h, ctx, launch_la(ctx, c.dtype, a), "linear attention launch failed");
+    return close_ctx(h, ctx, launch_la(ctx, c.dtype, a, h->sm_count), "linear attention launch failed");
 }
 
 size_t swimba_linear_attention_backward_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L)
@@ -156,7 +156,7 @@ int swimba_linear_attention_backward(swimba_handle *h, const float *log_decay, c
     a.job[0] = LaJob{d_o, v, k, HP, ldv, ldk, 1, 1, r, P, N, 0, 1, state_in, nullptr, gq, HN, shared, scale, scale, 1.f, seg[0]};
     a.job[1] = LaJob{v, d_o, q, ldv, HP, ldq, 1, 1, r, P, N, 1, 1, d_state_out, nullptr, gk, HN, shared, scale, 1.f, scale, seg[1]};
     a.job[2] = LaJob{k, q, d_o, ldk, ldq, HP, r, r, 1, N, P, 1, 0, d_state_out, d_state_in, dv, HP, 0, scale, 1.f, scale, seg[2]};
-    rc = launch_la(ctx, c.dtype, a);
+    rc = launch_la(ctx, c.dtype, a, h->sm_count);
     if (rc == SWIMBA_OK && shared) {
         rc = launch_la_head_sum(ctx, c.dtype, (const float *)gq, (int64_t)B * L, c.n_groups, r, N, dq);
         if (rc == SWIMBA_OK)

@@ -39,6 +39,10 @@ struct LaArgs {
     int B, L, H;
     int seg_len, nseg;           // tokens per segment (the last in the sequence may be shorter), segments per sequence
     int per;                     // pieces per segment, of seg_len / per tokens, that the pass for the states works
+    // CTAs of the kernel for 128 values: the first `whole` (job, segment, head, sequence)s have one each; the tiles of the others
+    // are shared by ncut, of which number c gives the outputs of tiles cut[c] .. cut[c + 1] - 1 of the walk and carries only
+    // the state through those in front
+    int whole, ncut, cut[5];
 };
 
 // log2 of the decay.  Held above -1e4, where one step underflows to nothing already, so that the zeroth
@@ -75,6 +79,8 @@ __device__ __forceinline__ void la_split(float w0, float w1, uint32_t (&p)[3])
 }
 __device__ __forceinline__ __nv_bfloat162 la_pair(uint32_t v) { return *reinterpret_cast<const __nv_bfloat162 *>(&v); }
 __device__ __forceinline__ uint32_t la_bits(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+// How the CTAs of the kernel for 128 values share `items` walks of nt tiles; returns the time, in tiles.
+double la_cuts(int64_t items, int nt, int sm_count, LaArgs *a);
 // Segments the kernels cut every sequence of a call into, and the bytes they keep for that.
 void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_count, int *seg_len, int *nseg, int *per);
 // (bytes of one job's segment states; grows with B and with L)
@@ -86,10 +92,10 @@ bool la_stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int s
 // (states: the pass that leaves every segment's end state).
 bool la_tiles_shape(int dtype, int N, int P);
 bool la_tiles_reach(const LaArgs &a);
-int launch_la_tiles(LaunchCtx &ctx, const LaArgs &a, bool states);
-int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states);      // its jobs of 128 values (la_wide.cu)
+int launch_la_tiles(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);
+int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);      // its jobs of 128 values (la_wide.cu)
 // Runs the jobs: per-segment states, their chain, outputs; or outputs alone when nseg == 1.
-int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a);
+int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a, int sm_count);
 // out[t, g, :] = sum over the r heads of group g of part[t, g r + i, :], in that order.
 int launch_la_head_sum(LaunchCtx &ctx, int dtype, const float *part, int64_t T, int G, int r, int N, void *out);
 int launch_la_step(LaunchCtx &ctx, int dtype, const float *log_decay, const void *q, int64_t ldq, const void *k,

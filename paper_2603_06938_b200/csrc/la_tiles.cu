@@ -575,7 +575,7 @@ bool la_tiles_reach(const LaArgs &a)
     return true;
 }
 
-int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states)
+int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states, int sm_count)
 {
     // jobs of one pair of head sizes go in one launch
     for (int dk : {64, 128})
@@ -586,7 +586,7 @@ int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states)
                 if (all.job[i].dk == dk && all.job[i].dv == dv) a.job[a.njobs++] = all.job[i];
             if (a.njobs == 0) continue;
             if (dv == 128) {
-                const int rc = launch_la_wide(ctx, a, states);
+                const int rc = launch_la_wide(ctx, a, states, sm_count);
                 if (rc != SWIMBA_OK) return rc;
                 continue;
             }

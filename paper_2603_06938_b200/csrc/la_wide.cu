@@ -8,6 +8,7 @@
 //   O     one region: Q S^T, scaled row by row in place, then P V on top
 // Shared memory is what bounds such a tile: 7860 cycles of reads and writes for two CTAs of 64 values each against 3900 here.
 #include <algorithm>
+#include <cmath>
 #include <cstddef>
 
 #include "la.h"
@@ -71,6 +72,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
 
     // the jobs on one head side by side: they read the same rows at about the same time
     int64_t id = blockIdx.x;
+    int part = 0, nparts = 1;
+    if (!STATE_ONLY && id >= a.whole) {
+        nparts = a.ncut;
+        part = (int)((id - a.whole) % nparts);
+        id = a.whole + (id - a.whole) / nparts;
+    }
     const int ji = (int)(id % a.njobs);
     id /= a.njobs;
     // segments, or pieces of them for the states alone, in the order of the walk (the last segment's end state enters nothing)
@@ -84,9 +91,18 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     const int parts = j.s_out ? 4 : 2, ring = 8 / parts;       // quarters of w V there is room for
     const int place = rev ? nall - 1 - seg : seg;
     const int t_begin = min(a.L, place * len), t_end = min(a.L, t_begin + len);
-    const int ntiles = (t_end - t_begin + LT - 1) / LT;
-    auto tile_at = [&](int t) { return t_begin + (rev ? ntiles - 1 - t : t) * LT; };       // first token of tile t
+    const int nwalk = (t_end - t_begin + LT - 1) / LT;
+    auto tile_at = [&](int t) { return t_begin + (rev ? nwalk - 1 - t : t) * LT; };        // first token of tile t
     auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
+    // this CTA's tiles: those in front of n_pre only carry the state; barriers that the others alone use count from there
+    const int n_pre = STATE_ONLY ? nwalk : nparts > 1 ? a.cut[part] : 0;
+    const int ntiles = STATE_ONLY || nparts == 1 ? nwalk : a.cut[part + 1];
+    const int pre = n_pre > 0 ? 1 : 0;
+    // tokens walked behind tile t in front of tile n_pre; tile -1: all of them
+    auto tokens_left = [&](int t) {
+        return rev ? (t < 0 ? t_end : tile_at(t)) - (n_pre > 0 ? tile_at(n_pre - 1) : t_end)
+                   : min(t_end, t_begin + n_pre * LT) - (t < 0 ? t_begin : min(t_end, tile_at(t) + LT));
+    };
 
     if (tid == 0) {
         for (int s = 0; s < NQ; ++s) {
@@ -99,7 +115,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         }
         for (int s = 0; s < NV; ++s) {
             tc::mbar_init(&sm->full_v[s], 1);
-            tc::mbar_init(&sm->free_v[s], STATE_ONLY || j.o_f32 ? 8 : 2);
+            tc::mbar_init(&sm->free_v[s], 8);
         }
         for (int s = 0; s < 4; ++s) {
             tc::mbar_init(&sm->vw_full[s], 8);
@@ -148,10 +164,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     if (warp == WARP_TMA) {
         // ------------------------------------------------------------------ loads, in the order in which room comes free
         const bool leader = tc::elect_one();
-        auto load = [&](int t, int ns, uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int stream) {
-            if (t >= ntiles) return;
-            const int st = t % ns;
-            tc::mbar_wait(&room[st], ((t / ns) & 1) ^ 1, abort_flag, d_status);
+        auto load = [&](int t, int i, int ns, uint64_t *full, uint64_t *room, uint32_t dst, uint32_t bytes, const CUtensorMap *m, int stream) {
+            if (i < 0 || t >= ntiles) return;
+            const int st = i % ns;
+            tc::mbar_wait(&room[st], ((i / ns) & 1) ^ 1, abort_flag, d_status);
             if (leader && !*(volatile int *)abort_flag) {
                 tc::mbar_arrive_expect_tx(&full[st], bytes);
                 for (uint32_t o = 0; o < bytes; o += SLAB)
@@ -159,12 +175,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             __syncwarp();
         };
-        auto load_q = [&](int t) { if (!STATE_ONLY) load(t, NQ, sm->full_q, sm->free_q, L::Q, L::QB, &maps.q[ji], h / j.rq); };
-        auto load_k = [&](int t) { load(t, NK, sm->full_k, sm->free_k, L::K, L::QB, &maps.k[ji], h / j.rk); };
-        auto load_v = [&](int t) { load(t, NV, sm->full_v, sm->free_v, L::V, VB, &maps.v[ji], h / j.rv); };
+        auto load_q = [&](int t) { if (!STATE_ONLY) load(t, t - n_pre, NQ, sm->full_q, sm->free_q, L::Q, L::QB, &maps.q[ji], h / j.rq); };
+        auto load_k = [&](int t) { load(t, t, NK, sm->full_k, sm->free_k, L::K, L::QB, &maps.k[ji], h / j.rk); };
+        auto load_v = [&](int t) { load(t, t, NV, sm->full_v, sm->free_v, L::V, VB, &maps.v[ji], h / j.rv); };
         // with one Q tile at a time the next one's load is waited for: its rows are brought to L2 a step before
         auto ahead_q = [&](int t) {
-            if (STATE_ONLY || NQ > 1 || t >= ntiles) return;
+            if (STATE_ONLY || NQ > 1 || t < n_pre || t >= ntiles) return;
 #pragma unroll 1
             for (int r = tile_at(t) + lane; r < tile_at(t) + tile_n(t); r += 32) {
                 const char *p = (const char *)((const __nv_bfloat16 *)j.q + ((int64_t)b * a.L + r) * j.ldq + (int64_t)(h / j.rq) * DK);
@@ -174,11 +190,9 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             __syncwarp();
         };
         for (int t = -NV; t < ntiles; ++t) {
-            if (t + NQ >= 0) {
-                load_q(t + NQ);
-                ahead_q(t + NQ + 1);
-            }
-            if (t + NK >= 0) load_k(t + NK);
+            load_q(t + NQ);
+            ahead_q(t + NQ + 1);
+            load_k(t + NK);
             load_v(t + NV);
         }
         // No copy may be in flight when the CTA leaves: after an abort nobody else has waited for the last ones (those
@@ -189,7 +203,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             else tc::mbar_wait(full, ph, abort_flag, d_status);
         };
         if (!STATE_ONLY)
-            for (int t = max(0, ntiles - NQ); t < ntiles; ++t) settle(&sm->full_q[t % NQ], (t / NQ) & 1);
+            for (int t = max(0, ntiles - n_pre - NQ); t < ntiles - n_pre; ++t) settle(&sm->full_q[t % NQ], (t / NQ) & 1);
         for (int t = max(0, ntiles - NK); t < ntiles; ++t) settle(&sm->full_k[t % NK], (t / NK) & 1);
         for (int t = max(0, ntiles - NV); t < ntiles; ++t) settle(&sm->full_v[t % NV], (t / NV) & 1);
     } else if (warp == WARP_MMA) {
@@ -204,11 +218,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const uint64_t dKt = tc::smem_desc_sw128(base + L::K, SLAB, 1024), dV = tc::smem_desc_sw128(base + L::V, SLAB, 1024);
         const uint64_t dS = tc::smem_desc_sw128(base + L::S, 16, 1024);
         auto scores = [&](int t) {
+            const int f = t - n_pre;
             tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
-            tc::mbar_wait(&sm->full_q[t % NQ], (t / NQ) & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->full_q[f % NQ], (f / NQ) & 1, abort_flag, d_status);
             tc::tc_fence_after();
             if (leader) {
-                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, t % NQ * L::QB));
+                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, f % NQ * L::QB));
                 const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dK, t % NK * L::QB));
 #pragma unroll
                 for (int kk = 0; kk < DK / 16; ++kk) {
@@ -219,33 +234,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             __syncwarp();
         };
-        if (!STATE_ONLY && ntiles > 0) scores(0);
-        for (int t = 0; t < ntiles; ++t) {
-            if (STATE_ONLY) {
-                tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
-            } else {
-                // QS: the carried part, once the state is there and the epilogue has read the tile in front
-                tc::mbar_wait(&sm->s_full, t & 1, abort_flag, d_status);
-                if (t > 0) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
-                tc::tc_fence_after();
-                if (leader) {
-                    const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, t % NQ * L::QB)), st = tc::smem_desc_fresh(dS);
-#pragma unroll
-                    for (int kk = 0; kk < DK / 16; ++kk) {
-                        const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
-                        tc::mma_ss(tm + TM_O, tc::smem_desc_advance(q, o), tc::smem_desc_advance(st, o), id_qk, kk > 0);
-                    }
-                    tc::mma_commit(&sm->qs_done);
-                    tc::mma_commit(&sm->free_q[t % NQ]);
-                }
-                __syncwarp();
-            }
-            // KV, by quarters of the tile
+        // KV, by quarters of the tile
+        auto add = [&](int t, bool done) {
 #pragma unroll 1
             for (int qd = 0; qd < 4; ++qd) {
                 const int buf = qd & (ring - 1);
                 tc::mbar_wait(&sm->vw_full[buf], parts == 4 ? qd >> 1 : t & 1, abort_flag, d_status);
-                if (!STATE_ONLY && qd == 0) tc::mbar_wait(&sm->s_scaled, t & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 if (leader) {
                     uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + qd * 4096));
@@ -256,17 +250,44 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     }
                     tc::mma_commit(&sm->vw_done[buf]);
                     if (qd == 3) {
-                        if (!STATE_ONLY || t == ntiles - 1) tc::mma_commit(&sm->kv_done);
+                        if (done) tc::mma_commit(&sm->kv_done);
                         tc::mma_commit(&sm->free_k[t % NK]);
                     }
                 }
                 __syncwarp();
             }
-            if (STATE_ONLY) continue;
+        };
+        if (!STATE_ONLY && pre) tc::mbar_wait(&sm->s_scaled, 0, abort_flag, d_status);         // (the state that enters is there)
+#pragma unroll 1
+        for (int t = 0; t < n_pre; ++t) {
+            tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
+            add(t, t == n_pre - 1);
+        }
+        if (ntiles > n_pre) scores(n_pre);
+#pragma unroll 1
+        for (int t = n_pre; t < ntiles; ++t) {
+            const int f = t - n_pre;
+            // QS: the carried part, once the state is there and the epilogue has read the tile in front
+            tc::mbar_wait(&sm->s_full, f & 1, abort_flag, d_status);
+            if (f > 0) tc::mbar_wait(&sm->o_free, (f - 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            if (leader) {
+                const uint64_t q = tc::smem_desc_fresh(tc::smem_desc_advance(dQ, f % NQ * L::QB)), st = tc::smem_desc_fresh(dS);
+#pragma unroll
+                for (int kk = 0; kk < DK / 16; ++kk) {
+                    const uint32_t o = (kk >> 2) * SLAB + (kk & 3) * 32;
+                    tc::mma_ss(tm + TM_O, tc::smem_desc_advance(q, o), tc::smem_desc_advance(st, o), id_qk, kk > 0);
+                }
+                tc::mma_commit(&sm->qs_done);
+                tc::mma_commit(&sm->free_q[f % NQ]);
+            }
+            __syncwarp();
+            tc::mbar_wait(&sm->s_scaled, (f + pre) & 1, abort_flag, d_status);
+            add(t, true);
             // PV, on top of the scaled carried part (and behind KV: by then w V has been made of all of V, where o is staged)
             tc::mbar_wait(&sm->full_v[t % NV], (t / NV) & 1, abort_flag, d_status);
-            tc::mbar_wait(&sm->p_full, t & 1, abort_flag, d_status);
-            tc::mbar_wait(&sm->o_scaled, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->p_full, f & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->o_scaled, f & 1, abort_flag, d_status);
             tc::tc_fence_after();
             if (leader) {
                 const uint64_t v = tc::smem_desc_fresh(tc::smem_desc_advance(dV, t % NV * VB));
@@ -278,8 +299,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             __syncwarp();
             if (t + 1 < ntiles) {
                 // the next scores go where P stands, which the epilogue reads too if V was not all finite
-                tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
-                if (((volatile int *)sm->odd_tile)[t & 1] == t + 1) tc::mbar_wait(&sm->o_free, t & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->pv_done, f & 1, abort_flag, d_status);
+                if (((volatile int *)sm->odd_tile)[t & 1] == t + 1) tc::mbar_wait(&sm->o_free, f & 1, abort_flag, d_status);
                 scores(t + 1);
             }
         }
@@ -299,15 +320,23 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             const float *from = seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
                                 : j.s_in ? j.s_in + bh * ssize
                                          : nullptr;
+            const float dec = pre ? exp2f(tokens_left(-1) * g2) : 1.f;
 #pragma unroll 1
             for (int c = 0; c < NC; c += 16) {
                 uint32_t x[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = from ? __float_as_uint(from[at0 + (c + e) * step]) : 0u;
+                for (int e = 0; e < 16; ++e) x[e] = from ? __float_as_uint(dec * from[at0 + (c + e) * step]) : 0u;
                 __syncwarp();
                 tc::tmem_st16(srow + c, x);
             }
             tc::tmem_st_wait();
+            if (pre) {
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm->s_scaled);
+                tc::mbar_wait(&sm->kv_done, 0, abort_flag, d_status);
+                tc::tc_fence_after();
+            }
         }
         uint8_t *copy = smem + L::S + i * 128 + (DK == 128 ? half * SLAB : 0);       // (its chunks of 16 bytes are swizzled by the row)
         const int chunk0 = DK == 128 ? 0 : half * 4;
@@ -348,9 +377,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 if (lane == 0) tc::mbar_arrive(pass == 0 ? &sm->s_full : &sm->s_scaled);
             }
         };
-        if (!STATE_ONLY && ntiles > 0) hand_over(0);
-        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
-            tc::mbar_wait(&sm->qk_full, t & 1, abort_flag, d_status);
+        if (ntiles > n_pre) hand_over(n_pre);
+        for (int t = n_pre; t < ntiles; ++t) {
+            const int f = t - n_pre;
+            tc::mbar_wait(&sm->qk_full, f & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll 1
             for (int k = 0; k < 2; ++k) {
@@ -388,17 +418,17 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->p_full);
             if (t + 1 < ntiles) {
-                tc::mbar_wait(&sm->kv_done, t & 1, abort_flag, d_status);
-                tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->kv_done, (f + pre) & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->qs_done, f & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 hand_over(t + 1);
             }
         }
         float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
-                    : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
+                    : seg == a.nseg - 1 && part == nparts - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
         if (to) {
             if (ntiles > 0) {
-                tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - 1) & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - n_pre - 1 + pre) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
             }
 #pragma unroll 1
@@ -421,8 +451,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const uint32_t to = tmem + TM_VW + ((uint32_t)(q4 * 32 + lg * 16) << 16);
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NV, n = tile_n(t), shift = rev ? 0 : LT - n;
-            // (states alone: every tile's additions as they are at the end of the walk)
-            const float tail = STATE_ONLY ? exp2f((rev ? tile_at(t) - t_begin : t_end - tile_at(t) - n) * g2) : 1.f;
+            // (tiles that only carry the state: their additions as they are in front of the first that does not)
+            const float tail = t < n_pre ? exp2f(tokens_left(t) * g2) : 1.f;
             tc::mbar_wait(&sm->full_v[s], (t / NV) & 1, abort_flag, d_status);
             __nv_bfloat162 odd = la_pair(0u);         // becomes NaN with the first entry that is not finite
 #pragma unroll 1
@@ -432,7 +462,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]);
                 tc::ldmatrix_x4_trans(at + 2048, r[4], r[5], r[6], r[7]);      // (16 tokens on: same swizzle)
                 const int j0 = qd * 32 + (lane & 3) * 2;
-                if (!STATE_ONLY && n == LT) {
+                if (t >= n_pre && n == LT) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const uint4 x = *reinterpret_cast<const uint4 *>(sm->wsplit[(j0 >> 1) + c * 4]);
@@ -479,7 +509,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (!STATE_ONLY && qd == 3 && __any_sync(0xffffffffu, __hisnan(odd.x) || __hisnan(odd.y))) {
+                if (t >= n_pre && qd == 3 && __any_sync(0xffffffffu, __hisnan(odd.x) || __hisnan(odd.y))) {
                     // what is not finite gives way to zeros, now that all of it has been read; PV comes behind KV
                     ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
                     const int col = lg * 16 + (lane & 15);
@@ -494,16 +524,16 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 }
                 if (lane == 0) tc::mbar_arrive(&sm->vw_full[buf]);
             }
-            if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
+            if (t < n_pre && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
         }
     } else if (warp >= WARP_O) {
         // ------------------------------------------------------------------ o: half a row per thread, staged where V stood
         const int q4 = warp & 3, half = (warp - WARP_O) >> 2, r = q4 * 32 + lane;
         const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16), mine = row + TM_O + half * 64;
-        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
-            const int s = t % NV, n = tile_n(t), at = tile_at(t);
+        for (int t = n_pre; t < ntiles; ++t) {
+            const int f = t - n_pre, s = t % NV, n = tile_n(t), at = tile_at(t);
             const float w = r < n ? j.scale_c * sm->pow[rev ? n - 1 - r : r + 1] : 0.f;
-            tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->qs_done, f & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < 64; c += 32) {   // the carried part, for PV to add to
@@ -518,7 +548,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->o_scaled);
-            tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
+            tc::mbar_wait(&sm->pv_done, f & 1, abort_flag, d_status);
             tc::tc_fence_after();
             const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
             uint8_t *stage = smem + L::V + s * VB + half * SLAB;
@@ -579,7 +609,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     tc::tma_store_4d(&maps.o[ji], stage, half * 64, h, at, b);
                     tc::bulk_commit_group();
                     tc::bulk_wait_read_all();
-                    tc::mbar_arrive(&sm->free_v[s]);
+                    tc::mbar_arrive_n(&sm->free_v[s], 4);
                 }
                 __syncwarp();
             }
@@ -595,7 +625,8 @@ bool run_wide(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 {
     const size_t smem = Sm<DK>::SMALL + sizeof(Small);
     if (!ensure_dynamic_smem((const void *)la_wide_kernel<DK, STATE_ONLY>, smem)) return false;
-    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.per : a.nseg);
+    const int64_t items = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.per : a.nseg);
+    const int64_t n = STATE_ONLY ? items : a.whole + (items - a.whole) * a.ncut;
     ctx.begin(STATE_ONLY ? STAGE_LA_STATES : STAGE_LA_TILES);
     launch_kernel(la_wide_kernel<DK, STATE_ONLY>, dim3((unsigned)n), dim3(THREADS), smem, ctx.stream, true, maps, a,
                   ctx.d_status);
@@ -605,8 +636,40 @@ bool run_wide(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 
 }  // namespace
 
-int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states)
+double la_cuts(int64_t items, int nt, int sm_count, LaArgs *a)
 {
+    // Whole waves of walks first, what is left shared so that its CTAs end together: a tile that only carries the state takes
+    // about half the time of the others, so each part is half as long as the one in front.
+    const int64_t whole = items / sm_count * sm_count, rest = items - whole;
+    double best = (double)ceil_div64(items, sm_count) * nt;
+    a->whole = (int)items;
+    a->ncut = 1;
+    if (rest == 0) return best;
+    for (int m = 2; m <= 4 && m <= nt; ++m) {
+        const double first = nt / (2.0 - pow(0.5, m - 1));
+        const double cost = (double)(whole / sm_count) * nt + (double)ceil_div64(rest * m, sm_count) * (first + 1.0);
+        if (cost >= best) continue;
+        best = cost;
+        a->whole = (int)whole;
+        a->ncut = m;
+        double at = 0;
+        for (int c = 0; c < m; ++c) {
+            a->cut[c] = std::max(c, (int)(at + 0.5));
+            at += first * pow(0.5, c);
+        }
+        a->cut[m] = nt;
+        for (int c = m - 1; c > 0; --c) a->cut[c] = std::min(a->cut[c], a->cut[c + 1] - 1);
+    }
+    return best;
+}
+
+int launch_la_wide(LaunchCtx &ctx, const LaArgs &all, bool states, int sm_count)
+{
+    LaArgs a = all;
+    const int64_t items = (int64_t)a.njobs * a.B * a.H * a.nseg;
+    a.whole = (int)items;
+    a.ncut = 1;
+    if (a.nseg == 1) la_cuts(items, ceil_div(a.L, LT), sm_count, &a);
     Maps maps;
     for (int i = 0; i < a.njobs; ++i) {
         const LaJob &j = a.job[i];

@@ -343,6 +343,7 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
     // 0.7 of a tile each, in pieces that fill the SMs), their chain (0.15 a piece) and two more launches (about 4).
     const int nt = ceil_div(L, LA_TILE_SEG);
     const int64_t items = (int64_t)njobs * B * H;
+    const bool wide = P == 128 && (njobs == 1 || N == 128);
     double best = 1e30;
     for (int n = 1; n <= std::min(most, nt); ++n) {
         const int len = ceil_div(nt, n), ns = ceil_div(nt, len);
@@ -356,7 +357,8 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
                 if (c < states) { states = c; pieces = p; }
             }
         }
-        const double cost = (double)ceil_div64(items * ns, sm_count) * len + states;
+        LaArgs cuts;
+        const double cost = n == 1 && wide ? la_cuts(items, nt, sm_count, &cuts) : (double)ceil_div64(items * ns, sm_count) * len + states;
         if (cost < best) {
             best = cost;
             *seg_len = len * LA_TILE_SEG;
@@ -379,16 +381,16 @@ size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs,
     return (size_t)most * H * N * P * sizeof(float);
 }
 
-int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a)
+int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a, int sm_count)
 {
     if (!la_tiles_shape(dtype, a.job[0].dk, a.job[0].dv) || !la_tiles_reach(a))
         return dtype == SWIMBA_DTYPE_FP32 ? launch_steps<float>(ctx, a) : launch_steps<__nv_bfloat16>(ctx, a);
     if (a.nseg > 1) {
-        int rc = launch_la_tiles(ctx, a, true);
+        int rc = launch_la_tiles(ctx, a, true, sm_count);
         if (rc == SWIMBA_OK) rc = launch_chain(ctx, a);
         if (rc != SWIMBA_OK) return rc;
     }
-    return launch_la_tiles(ctx, a, false);
+    return launch_la_tiles(ctx, a, false, sm_count);
 }
 
 int launch_la_head_sum(LaunchCtx &ctx, int dtype, const float *part, int64_t T, int G, int r, int N, void *out)

@@ -32,7 +32,7 @@ def forward(i, absolute=False):
     """(o, S) of the inputs i, or the same sums over magnitudes."""
     f = torch.abs if absolute else (lambda x: x)
     q, k, v = (f(per_head(i[n], i["H"])) for n in ("q", "k", "v"))
-    s0 = f(i["s0"].double()) if i["s0"] is not None else torch.zeros(i["B"], i["H"], i["P"], i["N"], dtype=torch.float64)
+    s0 = f(i["s0"].double()) if i["s0"] is not None else torch.zeros(i["B"], i["H"], i["P"], i["N"], dtype=torch.float64, device=q.device)
     o, S = scan(i["g"], v, k, q, s0)
     return i["scale"] * o, S
 
@@ -41,7 +41,7 @@ def backward(i, absolute=False):
     f = torch.abs if absolute else (lambda x: x)
     H, G, sc, g = i["H"], i["G"], i["scale"], i["g"]
     q, k, v, do = (f(per_head(i[n], H)) for n in ("q", "k", "v", "do"))
-    zero = torch.zeros(i["B"], H, i["P"], i["N"], dtype=torch.float64)
+    zero = torch.zeros(i["B"], H, i["P"], i["N"], dtype=torch.float64, device=q.device)
     s0 = f(i["s0"].double()) if i["s0"] is not None else zero
     ds = f(i["ds"].double()) if i["ds"] is not None else zero
     dq, _ = scan(g, k, v, do, s0.transpose(2, 3))

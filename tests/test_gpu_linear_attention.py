@@ -102,6 +102,36 @@ def test_sequences_cut_into_segments(dtype, B, L, H, G, N, P):
     check_backward(i, run_backward(i))
 
 
+@pytest.mark.parametrize("B,H,G,N,L", [(5, 14, 14, 128, 1100), (10, 8, 4, 64, 700), (2, 37, 37, 128, 1536), (13, 12, 12, 128, 650)])
+def test_walks_shared_between_blocks(B, H, G, N, L):
+    """Heads of 128 values, as many as occupy a part of the SMs only: a walk's tiles are shared by several blocks, each of
+    which carries the state through the tiles in front of its own.  (References on the GPU, in 64 bits.)"""
+    i = ref.inputs("bf16", B, L, H, G, N, 128, seed=31)
+    dev = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in i.items()}
+    o, s = run_forward(i)
+    zero = dev["s0"].double()
+    q, k, v = (ref.per_head(dev[n], H) for n in ("q", "k", "v"))
+    for f, bound in ((lambda x: x, False), (torch.abs, True)):
+        w, ws = ref.scan(dev["g"], f(v), f(k), f(q), f(zero))
+        if bound:
+            mag, ms = i["scale"] * w.cpu(), ws.cpu()
+        else:
+            want, wants = i["scale"] * w.cpu(), ws.cpu()
+    ref.close(o, want, ref.slack("bf16", L) * mag, "bf16", "o")
+    ref.close(s, wants, ref.state_slack("bf16", L) * ms, "fp32", "state")
+
+
+@pytest.mark.parametrize("B,H,G,N,L", [(1, 23, 23, 128, 1100), (4, 14, 7, 128, 640)])
+def test_gradients_of_shared_walks(B, H, G, N, L):
+    i = ref.inputs("bf16", B, L, H, G, N, 128, seed=33, grad=True)
+    dev = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in i.items()}
+    got = run_backward(i)
+    want, mag = ref.backward(dev), ref.backward(dev, absolute=True)
+    for n, g, w, m in zip(("dq", "dk", "dv"), got, want, mag):
+        ref.close(g, w.cpu(), ref.slack("bf16", L) * m.cpu(), "bf16", n)
+    ref.close(got[3], want[3].cpu(), ref.state_slack("bf16", L) * mag[3].cpu(), "fp32", "d state")
+
+
 def test_gradients_agree_with_differences():
     """Central differences of sum(do * o) + sum(ds * S) in the fp32 path: outputs carry 2^-24 (L + ...) of their
     magnitudes, so a difference over a step of 1/8 (the map is linear in q, and bilinear in k, v: exact) is good to a

@@ -153,23 +153,26 @@ def run(n, ns, state_only, rng):
 
 
 def run_wide(n, nq, state_only, rng):
+    n_pre = n if state_only else rng.choice([0, 0, rng.randrange(n)])      # tiles that only carry the state
+    pre = 1 if n_pre else 0
     ns = {"q": nq, "k": nq + 1, "v": 3}
     need = {f"{k}_{x}{s}": 1 for x in "qkv" for s in range(ns[x]) for k in ("full", "free")}
     need.update({n: 1 for n in ("qk_full", "p_full", "qs_done", "o_scaled", "pv_done", "o_free", "s_full", "s_scaled", "kv_done")})
     ring = rng.choice([2, 4])                             # quarters of w V there is room for
     need.update({f"vw_{k}{i}": 1 for i in range(ring) for k in ("full", "done")})
     bars, buf = Bars(need), Buffers()
-    odd = lambda t: not state_only and t % 3 == 1
+    odd = lambda t: t >= n_pre and t % 3 == 1
     async_ops = []
-    slot = lambda x, t: f"{x}{t % ns[x]}"
+    slot = lambda x, t: f"{x}{(t - n_pre if x == 'q' else t) % ns[x]}"
 
     def tma():
         def load(x, t):
-            if t < 0 or t >= n or (state_only and x == "q"):
+            i = t - n_pre if x == "q" else t
+            if i < 0 or t >= n or (state_only and x == "q"):
                 return
-            if t >= ns[x]:
-                yield f"free_{slot(x, t)}", t // ns[x] - 1
-            readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 2}[x]
+            if i >= ns[x]:
+                yield f"free_{slot(x, t)}", i // ns[x] - 1
+            readers = {"q": 2, "k": 1 if t < n_pre else 2, "v": 1 if t < n_pre else 2}[x]
             async_ops.append([lambda: (buf.write(slot(x, t), t, readers), bars.arrive(f"full_{slot(x, t)}"))])
         for t in range(-3, n):
             for x in "qkv":
@@ -181,50 +184,51 @@ def run_wide(n, nq, state_only, rng):
 
         def scores(t):
             yield f"full_{slot('k', t)}", t // ns["k"]
-            yield f"full_{slot('q', t)}", t // ns["q"]
+            yield f"full_{slot('q', t)}", (t - n_pre) // ns["q"]
             queue.append(lambda: (buf.read(slot("k", t), t), buf.read(slot("q", t), t), buf.write("qk", ("a", t), 1),
                                   bars.arrive("qk_full")))
 
-        def quarter(t, qd):
-            def done():
-                buf.read(f"vw{qd % ring}", 4 * t + qd)
-                bars.arrive(f"vw_done{qd % ring}")
-                if qd == 3:
-                    buf.read(slot("k", t), t)
-                    if not state_only:
-                        buf.read("s_scaled", t)
-                        buf.write("s", t + 1, 1)
-                    if not state_only or t == n - 1:
-                        bars.arrive("kv_done")
-                    bars.arrive(f"free_{slot('k', t)}")
-            queue.append(done)
-        if not state_only and n:
-            yield from scores(0)
-        for t in range(n):
-            if state_only:
-                yield f"full_{slot('k', t)}", t // ns["k"]
-            else:
-                yield "s_full", t
-                if t:
-                    yield "o_free", t - 1
-                queue.append(lambda t=t: (buf.read(slot("q", t), t), buf.read("s16", t), buf.write("o", ("s", t), 1),
-                                          bars.arrive("qs_done"), bars.arrive(f"free_{slot('q', t)}")))
+        def add(t, done):
             for qd in range(4):
                 yield f"vw_full{qd % ring}", (4 * t + qd) // ring
-                if not state_only and qd == 0:
-                    yield "s_scaled", t
-                quarter(t, qd)
-            if state_only:
-                continue
+
+                def ready(t=t, qd=qd):
+                    buf.read(f"vw{qd % ring}", 4 * t + qd)
+                    bars.arrive(f"vw_done{qd % ring}")
+                    if qd == 3:
+                        buf.read(slot("k", t), t)
+                        if t >= n_pre or (t == 0 and not state_only):
+                            buf.read("s_scaled", t)
+                        if done and not (state_only and t < n - 1):
+                            buf.write("s", t + 1, 1)
+                            bars.arrive("kv_done")
+                        bars.arrive(f"free_{slot('k', t)}")
+                queue.append(ready)
+        if pre and not state_only:
+            yield "s_scaled", 0
+        for t in range(n_pre):
+            yield f"full_{slot('k', t)}", t // ns["k"]
+            yield from add(t, t == n_pre - 1)
+        if n > n_pre:
+            yield from scores(n_pre)
+        for t in range(n_pre, n):
+            f = t - n_pre
+            yield "s_full", f
+            if f:
+                yield "o_free", f - 1
+            queue.append(lambda t=t: (buf.read(slot("q", t), t), buf.read("s16", t), buf.write("o", ("s", t), 1),
+                                      bars.arrive("qs_done"), bars.arrive(f"free_{slot('q', t)}")))
+            yield "s_scaled", f + pre
+            yield from add(t, True)
             yield f"full_{slot('v', t)}", t // ns["v"]
-            yield "p_full", t
-            yield "o_scaled", t
+            yield "p_full", f
+            yield "o_scaled", f
             queue.append(lambda t=t: (buf.read(slot("v", t), ("z", t) if odd(t) else t), buf.read("qk", ("p", t)),
                                       buf.read("o", ("w", t)), buf.write("o", ("o", t), 1), bars.arrive("pv_done")))
             if t + 1 < n:
-                yield "pv_done", t
+                yield "pv_done", f
                 if odd(t):
-                    yield "o_free", t
+                    yield "o_free", f
                 yield from scores(t + 1)
 
     def masks():                                          # and the state
@@ -241,16 +245,22 @@ def run_wide(n, nq, state_only, rng):
             if n:
                 yield "kv_done", 0
             return
-        yield from hand_over(0)
-        for t in range(n):
-            yield "qk_full", t
+        if pre:
+            buf.write("s_scaled", 0, 1)
+            yield None
+            bars.arrive("s_scaled")
+            yield "kv_done", 0
+        yield from hand_over(n_pre)
+        for t in range(n_pre, n):
+            f = t - n_pre
+            yield "qk_full", f
             buf.read("qk", ("a", t))
             buf.write("qk", ("p", t), 1 + odd(t))
             yield None
             bars.arrive("p_full")
             if t + 1 < n:
-                yield "kv_done", t
-                yield "qs_done", t
+                yield "kv_done", f + pre
+                yield "qs_done", f
                 yield from hand_over(t + 1)
 
     def values():
@@ -269,18 +279,19 @@ def run_wide(n, nq, state_only, rng):
                         assert buf.v[v][1] == 1
                         buf.v[v] = [("z", t), 1]
                 bars.arrive(f"vw_full{qd % ring}")
-            if state_only:
+            if t < n_pre:
                 bars.arrive(f"free_{v}")
 
     def outputs():
-        for t in range(n):
+        for t in range(n_pre, n):
+            f = t - n_pre
             v = slot("v", t)
-            yield "qs_done", t
+            yield "qs_done", f
             buf.read("o", ("s", t))
             buf.write("o", ("w", t), 1)
             yield None
             bars.arrive("o_scaled")
-            yield "pv_done", t
+            yield "pv_done", f
             buf.read("o", ("o", t))
             yield None
             if odd(t):
