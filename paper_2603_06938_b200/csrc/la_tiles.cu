@@ -43,7 +43,7 @@ template <int DK> struct Sm {
 };
 struct Small {
     uint64_t full_q[3], full_k[3], full_v[3], free_q[3], free_k[3], free_v[3];
-    uint64_t qk_full, qk_read, p_full, qs_done, pv_done, vw_full[2], kv_done[2], kv_read, s_full, o_free;
+    uint64_t qk_full, qk_read, p_full, qs_done, pv_done, vw_full[4], kv_done[4], kv_read, s_full, o_free;
     uint32_t tmem;
     int abort_flag;
     int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
@@ -90,13 +90,18 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     const int h = (int)(id % a.H), b = (int)(id / a.H);
     const LaJob &j = a.job[ji];
     const bool rev = j.reverse != 0;
-    // three parts where the state is a result; two (2^-16) where only the read of it is, whose copy is rounded to bf16
-    const int parts = j.s_out ? 3 : 2;
+    // three parts where the state is a result; two (2^-17) where only the read of it is, whose copy is rounded to bf16
+    const int parts = j.s_out && (STATE_ONLY || seg == nall - 1) ? 3 : 2;
     const int place = rev ? nall - 1 - seg : seg;
     const int t_begin = min(a.L, place * len), t_end = min(a.L, t_begin + len);
     const int ntiles = (t_end - t_begin + LT - 1) / LT;
     auto tile_at = [&](int t) { return t_begin + (rev ? ntiles - 1 - t : t) * LT; };       // first token of tile t
     auto tile_n = [&](int t) { return min(LT, t_end - tile_at(t)); };
+
+    // w V of the halves of a tile; for the states alone two tiles, the second where Q would be
+    static_assert(NS * L::QB >= PARTS * SLAB, "w V over Q");
+    auto vw_slot = [](int t, int hf) { return STATE_ONLY ? (t & 1) * 2 + hf : hf; };
+    auto vw_phase = [](int t) { return STATE_ONLY ? t >> 1 : t; };
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) {
@@ -105,13 +110,13 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             tc::mbar_init(&sm->full_v[s], 1);
             tc::mbar_init(&sm->free_q[s], 1);
             tc::mbar_init(&sm->free_k[s], 1);
-            tc::mbar_init(&sm->free_v[s], STATE_ONLY ? 8 : j.o_f32 ? 4 : 1);
+            tc::mbar_init(&sm->free_v[s], STATE_ONLY ? 16 : j.o_f32 ? 4 : 1);
         }
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < 4; ++s) {
             tc::mbar_init(&sm->vw_full[s], 8);
             tc::mbar_init(&sm->kv_done[s], 1);
-            sm->odd_tile[s] = 0;
         }
+        sm->odd_tile[0] = sm->odd_tile[1] = 0;
         tc::mbar_init(&sm->qk_full, 1);
         tc::mbar_init(&sm->qk_read, 8);
         tc::mbar_init(&sm->p_full, 8);
@@ -186,7 +191,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         const uint64_t dQ = tc::smem_desc_sw128(base + L::Q, 16, 1024), dK = tc::smem_desc_sw128(base + L::K, 16, 1024);
         // (64 keys: both halves of the 128 rows of D are the same 64 keys)
         const uint64_t dKt = tc::smem_desc_sw128(base + L::K, DK == 128 ? SLAB : 0, 1024);
-        const uint64_t dV = tc::smem_desc_sw128(base + L::V, SLAB, 1024), dW = tc::smem_desc_sw128(base + L::VW, SLAB, 1024);
+        const uint64_t dV = tc::smem_desc_sw128(base + L::V, SLAB, 1024), dW = tc::smem_desc_sw128(base + L::VW, SLAB, 1024),
+                       dW2 = tc::smem_desc_sw128(base + L::Q, SLAB, 1024);
         const uint64_t dS = tc::smem_desc_sw128(base + L::S, SLAB, 1024);
         auto scores = [&](int t) {
             const int s = t % NS;
@@ -213,20 +219,22 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             const uint32_t ph = (t / NS) & 1;
             // KV, by halves of the tile: w V of one is made while the other is multiplied.  It does not wait for the state.
             if (STATE_ONLY) tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
-            if (t > 0) tc::mbar_wait(&sm->kv_read, (t - 1) & 1, abort_flag, d_status);
+            else if (t > 0) tc::mbar_wait(&sm->kv_read, (t - 1) & 1, abort_flag, d_status);
 #pragma unroll 1
             for (int hf = 0; hf < 2; ++hf) {
-                tc::mbar_wait(&sm->vw_full[hf], t & 1, abort_flag, d_status);
+                const int u = vw_slot(t, hf);
+                tc::mbar_wait(&sm->vw_full[u], vw_phase(t) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 if (leader) {
                     const uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, s * L::QB + hf * 8192));
-                    const uint64_t w = tc::smem_desc_fresh(tc::smem_desc_advance(dW, hf * 8192));
+                    const uint64_t w = tc::smem_desc_fresh(tc::smem_desc_advance(u < 2 ? dW : dW2, hf * 8192));
 #pragma unroll
                     for (int kk = 0; kk < LT / 32; ++kk)
                         tc::mma_ss(tm + TM_KV, tc::smem_desc_advance(k, kk * 2048), tc::smem_desc_advance(w, kk * 2048), id_kv,
-                                   hf + kk > 0);
-                    tc::mma_commit(&sm->kv_done[hf]);
+                                   hf + kk + (STATE_ONLY ? t : 0) > 0);
+                    tc::mma_commit(&sm->kv_done[u]);
                     if (hf == 1) tc::mma_commit(&sm->free_k[s]);
+                    if (STATE_ONLY && hf == 1 && t == ntiles - 1) tc::mma_commit(&sm->qs_done);
                 }
                 __syncwarp();
             }
@@ -260,17 +268,13 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             }
             __syncwarp();
         }
-    } else if (warp >= WARP_MASK && warp < WARP_W) {
+    } else if (!STATE_ONLY && warp >= WARP_MASK && warp < WARP_W) {
         // ------------------------------------------------------------------ masks: half a row of the scores per thread
         const int q4 = warp & 3, half = (warp - WARP_MASK) >> 2, i = q4 * 32 + lane;
         const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16), from = row + TM_QK + half * 64, to = row + TM_P + half * 32;
         const float scale_p = j.scale_p;
         const uint32_t keep = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
-            if (t > 0) {                         // (P has been read, by the epilogue too where V was not all finite)
-                tc::mbar_wait(&sm->pv_done, (t - 1) & 1, abort_flag, d_status);
-                if (((volatile int *)sm->odd_tile)[(t - 1) & 1] == t) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
-            }
             tc::mbar_wait(&sm->qk_full, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll 1
@@ -311,6 +315,11 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                         }
                     }
                 }
+                if (k == 0 && t > 0) {           // (P has been read, by the epilogue too where V was not all finite)
+                    tc::mbar_wait(&sm->pv_done, (t - 1) & 1, abort_flag, d_status);
+                    if (((volatile int *)sm->odd_tile)[(t - 1) & 1] == t) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
+                    tc::tc_fence_after();
+                }
                 tc::tmem_st16(to + k * 16, o);
             }
             tc::tmem_st_wait();
@@ -318,48 +327,65 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->p_full);
         }
-    } else if (warp >= WARP_W && warp < WARP_STATE) {
-        // ------------------------------------------------------------------ w V: eight entries of two rows at a time
-        const int ltid = tid - WARP_W * 32, r0 = ltid >> 3;
+    } else if (warp >= WARP_MASK && warp < WARP_STATE) {
+        // ------------------------------------------------------------------ w V: eight entries of two rows at a time (for the
+        // states alone the warps of the masks make the first half of a tile)
+        const int ltid = (tid - WARP_MASK * 32) & 255, r0 = ltid >> 3;
+        const int hf_begin = STATE_ONLY && warp >= WARP_W ? 1 : 0, hf_end = STATE_ONLY ? hf_begin + 1 : 2;
         const uint64_t neg = tc::f32x2(-1.f, -1.f);
         const float scale_a = j.scale_a;
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NS, n = tile_n(t);
             tc::mbar_wait(&sm->full_v[s], (t / NS) & 1, abort_flag, d_status);
+            // (states alone: every tile's additions as they are at the end of the walk, so that all tiles add up in D)
+            const float tail = STATE_ONLY ? scale_a * exp2f((rev ? tile_at(t) - t_begin : t_end - tile_at(t) - n) * g2) : scale_a;
             const uint32_t off = tc::sw128_offset(r0, ltid & 7);           // (32 rows on: 4096 bytes, same swizzle)
             uint32_t odd = 0;
 #pragma unroll 1
-            for (int hf = 0; hf < 2; ++hf) {
+            for (int hf = hf_begin; hf < hf_end; ++hf) {
                 const int i = hf * 2;
                 uint4 v[2];
-                uint64_t w2[2];
-                if (t > 0) tc::mbar_wait(&sm->kv_done[hf], (t - 1) & 1, abort_flag, d_status);
+                float w[2];
+                const int u = vw_slot(t, hf);
+                if (vw_phase(t) > 0) tc::mbar_wait(&sm->kv_done[u], (vw_phase(t) - 1) & 1, abort_flag, d_status);
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const int rr = r0 + 32 * (i + z), e = rev ? rr + 1 : n - 1 - rr;      // n - r - first steps of decay
                     v[z] = *reinterpret_cast<const uint4 *>(smem + L::V + s * SLAB + off + (i + z) * 4096);
-                    const float w = rr < n ? scale_a * sm->pow[e] : 0.f;
-                    w2[z] = tc::f32x2(w, w);
+                    w[z] = rr < n ? tail * sm->pow[e] : 0.f;
                 }
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const uint32_t in[4] = {v[z].x, v[z].y, v[z].z, v[z].w};
+                    uint8_t *dst = smem + (u < 2 ? L::VW : L::Q) + off + (i + z) * 4096;
                     uint32_t p[PARTS][4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        // (an exponent of all ones, infinity or NaN, carries into the sign's place)
+                    for (int k = 0; k < 4; ++k)      // (an exponent of all ones, infinity or NaN, carries into the sign's place)
                         odd |= (in[k] & 0x7f807f80u) + 0x00800080u;
-                        uint64_t x = tc::f32x2_mul(w2[z], pair_of(in[k] << 16, in[k] & 0xffff0000u));
-                        p[0][k] = tc::f32x2_bf16(x);
-                        x = tc::f32x2_fma(neg, pair_of(p[0][k] << 16, p[0][k] & 0xffff0000u), x);
-                        p[1][k] = tc::f32x2_bf16(x);
-                        x = tc::f32x2_fma(neg, pair_of(p[1][k] << 16, p[1][k] & 0xffff0000u), x);
-                        p[2][k] = tc::f32x2_bf16(x);
+                    if (parts == 2) {
+                        uint32_t wp[3];
+                        la_split(w[z], w[z], wp);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const __nv_bfloat162 x = la_pair(in[k]), wh = la_pair(wp[0]), p0 = __hmul2(wh, x);
+                            p[0][k] = la_bits(p0);
+                            p[1][k] = la_bits(__hfma2(la_pair(wp[1]), x, __hfma2(wh, x, __hneg2(p0))));
+                        }
+                    } else {
+                        const uint64_t w2 = tc::f32x2(w[z], w[z]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint64_t x = tc::f32x2_mul(w2, pair_of(in[k] << 16, in[k] & 0xffff0000u));
+                            p[0][k] = tc::f32x2_bf16(x);
+                            x = tc::f32x2_fma(neg, pair_of(p[0][k] << 16, p[0][k] & 0xffff0000u), x);
+                            p[1][k] = tc::f32x2_bf16(x);
+                            x = tc::f32x2_fma(neg, pair_of(p[1][k] << 16, p[1][k] & 0xffff0000u), x);
+                            p[2][k] = tc::f32x2_bf16(x);
+                        }
+                        *reinterpret_cast<uint4 *>(dst + 2 * SLAB) = make_uint4(p[2][0], p[2][1], p[2][2], p[2][3]);
                     }
-                    uint8_t *dst = smem + L::VW + off + (i + z) * 4096;
                     *reinterpret_cast<uint4 *>(dst) = make_uint4(p[0][0], p[0][1], p[0][2], p[0][3]);
                     *reinterpret_cast<uint4 *>(dst + SLAB) = make_uint4(p[1][0], p[1][1], p[1][2], p[1][3]);
-                    if (parts == 3) *reinterpret_cast<uint4 *>(dst + 2 * SLAB) = make_uint4(p[2][0], p[2][1], p[2][2], p[2][3]);
                 }
                 if (!STATE_ONLY && (odd & 0x80008000u)) {
 #pragma unroll 1
@@ -374,7 +400,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                 }
                 tc::fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&sm->vw_full[hf]);
+                if (lane == 0) tc::mbar_arrive(&sm->vw_full[u]);
             }
             if (STATE_ONLY && lane == 0) tc::mbar_arrive(&sm->free_v[s]);
         }
@@ -405,15 +431,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             if (lane == 0) tc::mbar_arrive(&sm->s_full);
         };
         const uint64_t one = tc::f32x2(1.f, 1.f);
-        for (int t = 0; t < ntiles; ++t) {
-            if (!STATE_ONLY) {
-                if (t > 0) tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
-                publish();
-            }
-            const float dec = sm->pow[tile_n(t)];
+        auto collect = [&](float dec) {          // S <- dec S + D
             const uint64_t dec2 = tc::f32x2(dec, dec);
-            tc::mbar_wait(&sm->kv_done[1], t & 1, abort_flag, d_status);
-            tc::tc_fence_after();
 #pragma unroll
             for (int k = 0; k < NC; k += 16) {
                 uint32_t x[16], y[16];
@@ -430,9 +449,22 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                     for (int e = 0; e < 8; ++e) st[k / 2 + e] = tc::f32x2_fma(one, pair_of(x[2 * e], x[2 * e + 1]), st[k / 2 + e]);
                 }
             }
+        };
+        for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
+            if (t > 0) tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
+            publish();
+            const float dec = sm->pow[tile_n(t)];
+            tc::mbar_wait(&sm->kv_done[1], t & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+            collect(dec);
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->kv_read);
+        }
+        if (STATE_ONLY && ntiles > 0) {
+            tc::mbar_wait(&sm->qs_done, 0, abort_flag, d_status);      // (every product)
+            tc::tc_fence_after();
+            collect(1.f);
         }
         float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
                     : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
@@ -568,7 +600,7 @@ bool la_tiles_shape(int dtype, int N, int P)
 
 bool la_tiles_reach(const LaArgs &a)
 {
-    // (a tensor map's strides stay below 2^40 bytes)
+    // (a tensor map's strides stay below 2^40 bytes, which in this memory only a sequence of one token exceeds: never one that is cut)
     for (int i = 0; i < a.njobs; ++i)
         for (int64_t ld : {a.job[i].ldq, a.job[i].ldk, a.job[i].ldv})
             if (ld * 2 * a.L >= (int64_t)1 << 40) return false;

@@ -578,6 +578,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                             }
                         }
                     }
+                    __syncwarp();
                 }
                 if (c == 32) {                   // everything in tensor memory has been read
                     tc::tc_fence_before();

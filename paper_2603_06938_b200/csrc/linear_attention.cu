@@ -351,7 +351,7 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
         int pieces = 1;
         if (ns > 1) {
             states = 1e30;
-            for (int p = 1; p <= 4 && p * ns <= most; ++p) {
+            for (int p = 1; p <= 4 && p * ns <= std::min(most, nt); ++p) {
                 if (len % p != 0) continue;
                 const double c = 0.7 * ceil_div64(items * (ns - 1) * p, sm_count) * (len / p) + 4 + 0.15 * ns * p;
                 if (c < states) { states = c; pieces = p; }

@@ -39,9 +39,11 @@ class Buffers:
 def run(n, ns, state_only, rng):
     need = {f"{k}_{x}{s}": 1 for s in range(ns) for k in ("full", "free") for x in "qkv"}
     for s in range(ns):
-        need[f"free_v{s}"] = 1
-    need.update({n: 1 for n in ("qk_full", "qk_read", "p_full", "qs_done", "pv_done", "vw_full0", "vw_full1", "kv_done0",
-                                "kv_done1", "kv_read", "s_full", "o_free")})
+        need[f"free_v{s}"] = 2 if state_only else 1
+    need.update({n: 1 for n in ("qk_full", "qk_read", "p_full", "qs_done", "pv_done", "kv_read", "s_full", "o_free")})
+    need.update({f"{x}{u}": 1 for x in ("vw_full", "kv_done") for u in range(4)})
+    slot = lambda t, half: (t & 1) * 2 + half if state_only else half
+    phase = lambda t: t >> 1 if state_only else t
     bars, buf = Bars(need), Buffers()
     odd = lambda t: t % 3 == 1
     async_ops = []                       # products and copies, each queue in order: callables
@@ -52,7 +54,7 @@ def run(n, ns, state_only, rng):
             for x in "kv" if state_only else "kqv":
                 if t >= ns:
                     yield f"free_{x}{s}", t // ns - 1
-                readers = {"q": 2, "k": 1 if state_only else 2, "v": 1 if state_only else 2}[x]
+                readers = {"q": 2, "k": 1 if state_only else 2, "v": 2}[x]
                 async_ops.append([lambda x=x, s=s, t=t, r=readers: (buf.write(f"{x}{s}", t, r), bars.arrive(f"full_{x}{s}"))])
 
     def mma():
@@ -72,13 +74,15 @@ def run(n, ns, state_only, rng):
             s = t % ns
             if state_only:
                 yield f"full_k{s}", t // ns
-            if t:
+            elif t:
                 yield "kv_read", t - 1
-            yield "vw_full0", t
-            queue.append(lambda t=t: (buf.read("vw0", t), buf.write("d", t, 1), bars.arrive("kv_done0")))
-            yield "vw_full1", t
-            queue.append(lambda t=t, s=s: (buf.read(f"k{s}", t), buf.read("vw1", t), bars.arrive("kv_done1"),
-                                           bars.arrive(f"free_k{s}")))
+            a, b = slot(t, 0), slot(t, 1)
+            yield f"vw_full{a}", phase(t)
+            queue.append(lambda t=t, a=a: (buf.read(f"vw{a}", t), state_only or buf.write("d", t, 1), bars.arrive(f"kv_done{a}")))
+            yield f"vw_full{b}", phase(t)
+            queue.append(lambda t=t, s=s, b=b: (buf.read(f"k{s}", t), buf.read(f"vw{b}", t), bars.arrive(f"kv_done{b}"),
+                                           bars.arrive(f"free_k{s}"),
+                                           bars.arrive("qs_done") if state_only and t == n - 1 else None))
             if state_only:
                 continue
             yield "s_full", t
@@ -95,11 +99,11 @@ def run(n, ns, state_only, rng):
 
     def masks():
         for t in range(n):
+            yield "qk_full", t
             if t:
                 yield "pv_done", t - 1
                 if odd(t - 1):
                     yield "o_free", t - 1
-            yield "qk_full", t
             buf.read("a", t)
             yield None
             bars.arrive("qk_read")
@@ -107,16 +111,17 @@ def run(n, ns, state_only, rng):
             yield None
             bars.arrive("p_full")
 
-    def values():
+    def values(halves):
         for t in range(n):
             yield f"full_v{t % ns}", t // ns
             buf.read(f"v{t % ns}", t)
-            for half in (0, 1):
-                if t:
-                    yield f"kv_done{half}", t - 1
-                buf.write(f"vw{half}", t, 1)
+            for half in halves:
+                u = slot(t, half)
+                if phase(t):
+                    yield f"kv_done{u}", phase(t) - 1
+                buf.write(f"vw{u}", t, 1)
                 yield None
-                bars.arrive(f"vw_full{half}")
+                bars.arrive(f"vw_full{u}")
             if state_only:
                 bars.arrive(f"free_v{t % ns}")
 
@@ -137,19 +142,23 @@ def run(n, ns, state_only, rng):
             bars.arrive(f"free_v{t % ns}")
 
     def state():
+        if state_only:
+            if n:
+                yield "qs_done", 0
+            return
         for t in range(n):
-            if not state_only:
-                if t:
-                    yield "qs_done", t - 1
-                buf.write("s", t, 1)
-                yield None
-                bars.arrive("s_full")
+            if t:
+                yield "qs_done", t - 1
+            buf.write("s", t, 1)
+            yield None
+            bars.arrive("s_full")
             yield "kv_done1", t
             buf.read("d", t)
             yield None
             bars.arrive("kv_read")
 
-    drive([tma(), mma(), values(), state()] + ([] if state_only else [masks(), outputs()]), bars, async_ops, rng)
+    drive([tma(), mma(), state()] + ([values((0,)), values((1,))] if state_only else [values((0, 1)), masks(), outputs()]),
+          bars, async_ops, rng)
 
 
 def run_wide(n, nq, state_only, rng):
