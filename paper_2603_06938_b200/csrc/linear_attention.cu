@@ -2,6 +2,7 @@
 // tensor-core kernel does not take), the chain of segment states, the sum over shared heads and the
 // single-token step.  What a job is: la.h.
 #include <algorithm>
+#include <type_traits>
 
 #include "la.h"
 
@@ -9,120 +10,283 @@ namespace swimba {
 
 namespace {
 
-constexpr int LA_TS = 16;        // tokens staged in shared memory at a time
+__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p)
+{
+    const uint2 r = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                       __uint_as_float(r.y & 0xffff0000u));
+}
+
+constexpr int LA_C = 32;         // tokens of a chunk
 constexpr int LA_COLS = 64;      // columns of v (and o) a block of 256 threads works
 
-// One (job, sequence, head, segment) and LA_COLS columns of its v: the recurrence token by token with the
-// state in registers.  Lane l of a half-warp holds the entries dk = l + 16 m (m < KR) of four columns;
-// per token it adds k v, multiplies by the decay and contributes to o, which the sixteen lanes sum.
-// STATE_ONLY: from a zero state, and only the end state is kept (in seg).
-template <typename T, int KR, bool STATE_ONLY>
-__global__ void __launch_bounds__(256, KR <= 8 ? 2 : 1)
-la_steps_kernel(const __grid_constant__ LaArgs a)
+// Shared memory of a block, for jobs of up to dk entries: the chunk in fp32 (rows of q and k padded by four, so that threads on
+// neighbouring rows read different banks), the scores, the state, and the next chunk as it arrives.
+struct ChunkSmem {
+    int q, k, v, wv, p, s, stage, bytes;      // (offsets in floats; bytes in all)
+};
+__host__ __device__ constexpr ChunkSmem chunk_smem(int dk, int elt, bool state_only)
 {
-    constexpr int DKP = KR * 16;
-    __shared__ float sq[STATE_ONLY ? 1 : LA_TS * DKP], sk[LA_TS * DKP], sv[LA_TS * LA_COLS],
-        so[STATE_ONLY ? 1 : LA_TS * LA_COLS];
+    ChunkSmem m{};
+    int at = 0;
+    m.q = at;     at += state_only ? 0 : LA_C * (dk + 4);
+    m.k = at;     at += LA_C * (dk + 4);
+    m.v = at;     at += state_only ? 0 : LA_C * LA_COLS;
+    m.wv = at;    at += LA_C * LA_COLS;
+    m.p = at;     at += state_only ? 0 : LA_C * (LA_C + 4);
+    m.s = at;     at += dk * LA_COLS;
+    m.stage = at;
+    m.bytes = at * 4 + LA_C * ((state_only ? 1 : 2) * dk + LA_COLS) * elt;
+    return m;
+}
+
+__device__ __forceinline__ void copy16(void *dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+
+// R rows of o by two columns a thread: o_i = sum_{j <= i} P_ij v_j + w_i sum_d q_id S_d.  The rows i0 .. i0 + R - 1 lie in one
+// group of four, whose scores behind the diagonal are never touched (what a later token holds must not matter, NaN or not).
+template <int R>
+__device__ __forceinline__ void chunk_carried(const float *sq, int ldq, const float *ss, int dk, float (&acc)[R][2])
+{
+#pragma unroll 2
+    for (int d = 0; d < dk; d += 4) {
+        float4 qq[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) qq[r] = *reinterpret_cast<const float4 *>(sq + r * ldq + d);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const float2 s = *reinterpret_cast<const float2 *>(ss + (d + z) * LA_COLS);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float x = z == 0 ? qq[r].x : z == 1 ? qq[r].y : z == 2 ? qq[r].z : qq[r].w;
+                acc[r][0] = fmaf(x, s.x, acc[r][0]);
+                acc[r][1] = fmaf(x, s.y, acc[r][1]);
+            }
+        }
+    }
+}
+template <int R>
+__device__ __forceinline__ void chunk_inside(const float *sp, const float *sv, int i0, float (&acc)[R][2])
+{
+    const int diag = i0 & ~3;
+    for (int j = 0; j <= diag; j += 4) {
+        float4 p[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) p[r] = *reinterpret_cast<const float4 *>(sp + r * (LA_C + 4) + j);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const float2 s = *reinterpret_cast<const float2 *>(sv + (j + z) * LA_COLS);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float x = z == 0 ? p[r].x : z == 1 ? p[r].y : z == 2 ? p[r].z : p[r].w;
+                if (j + z <= i0 + r) {
+                    acc[r][0] = fmaf(x, s.x, acc[r][0]);
+                    acc[r][1] = fmaf(x, s.y, acc[r][1]);
+                }
+            }
+        }
+    }
+}
+
+// One (job, sequence, head, segment) and LA_COLS columns of its v, by chunks of 32 tokens in fp32, with r the place of a token
+// in the order of the walk and the state S in shared memory:
+//   P_ij = scale_p lambda^(i - j) q_i k_j  (j <= i),   o_i = sum_j P_ij v_j + scale_c lambda^(i + first) S^T q_i
+//   S <- lambda^n S + sum_j k_j (scale_a lambda^(n - j - first) v_j)^T
+// (first = 1 walking forward, 0 backward).  A thread works a few rows by two columns of each product.
+// STATE_ONLY: from a zero state, and only the end state is kept (in seg).
+template <typename T, bool STATE_ONLY>
+__global__ void __launch_bounds__(256)
+la_chunks_kernel(const __grid_constant__ LaArgs a, int dk_most)
+{
+    extern __shared__ __align__(16) float smf[];
+    __shared__ float pow_hi[LA_C + 1], pow_lo;           // lambda^m; the rest of lambda^LA_C, which multiplies up
+    const ChunkSmem m = chunk_smem(dk_most, sizeof(T), STATE_ONLY);
+    float *sq = smf + m.q, *sk = smf + m.k, *sv = smf + m.v, *swv = smf + m.wv, *sp = smf + m.p, *ss = smf + m.s;
+    T *stage = reinterpret_cast<T *>(smf + m.stage);
     grid_dep_launch();
     grid_dep_wait();
     int64_t id = blockIdx.x;
     const int nrun = STATE_ONLY ? a.nseg - 1 : a.nseg;   // (the last segment's end state enters nothing)
-    int seg = (int)(id % nrun);
+    const int seg = (int)(id % nrun);
     id /= nrun;
     const int h = (int)(id % a.H);
     id /= a.H;
     const int b = (int)(id % a.B);
     const LaJob &j = a.job[id / a.B];
-    const int c0 = blockIdx.y * LA_COLS;
-    if (c0 >= j.dv) return;
-    const int tid = threadIdx.x, lane16 = tid & 15, col = (tid >> 4) * 4;   // four columns c0 + col ..
-    const int dk = j.dk, dv = j.dv;
-    const LaDecay lam = la_decay(a.log_decay[h]);
+    const int c0 = blockIdx.y * LA_COLS, dk = j.dk, dv = j.dv;
+    if (c0 >= dv) return;
+    const int nc = min(LA_COLS, dv - c0), ld = dk + 4, tid = threadIdx.x;
+    const bool rev = j.reverse != 0;
+    const double l2 = la_log2_decay(a.log_decay[h]);
+    if (tid <= LA_C) {
+        const double l = exp2(l2 * tid);
+        pow_hi[tid] = (float)l;
+        if (tid == LA_C) pow_lo = (float)(l - (double)(float)l);
+    }
     // segments are numbered in the order of the walk; w counts its tokens
-    const int place = j.reverse ? a.nseg - 1 - seg : seg, first = place * a.seg_len, last = min(a.L, first + a.seg_len);
-    const int w0 = j.reverse ? a.L - last : first, w1 = w0 + (last - first);
+    const int place = rev ? a.nseg - 1 - seg : seg, begin = place * a.seg_len, end = min(a.L, begin + a.seg_len);
+    const int w0 = rev ? a.L - end : begin, w1 = w0 + (end - begin);
     const T *q = (const T *)j.q + (int64_t)b * a.L * j.ldq + (int64_t)(h / j.rq) * dk;
     const T *k = (const T *)j.k + (int64_t)b * a.L * j.ldk + (int64_t)(h / j.rk) * dk;
-    const T *v = (const T *)j.v + (int64_t)b * a.L * j.ldv + (int64_t)(h / j.rv) * dv;
+    const T *v = (const T *)j.v + (int64_t)b * a.L * j.ldv + (int64_t)(h / j.rv) * dv + c0;
     const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)dk * dv;
+    constexpr int EPC = 16 / sizeof(T);                  // entries of a copy (rows and widths are multiples of it)
 
-    auto at = [&](int m, int c) {
-        const int64_t d = lane16 + 16 * m, e = c0 + col + c;
-        return j.transposed ? d * dv + e : e * dk + d;
+    // the chunk at w: rows of k, then q, then v
+    auto fetch = [&](int w) {
+        const int n = min(LA_C, w1 - w);
+        auto rows = [&](const T *src, int64_t lds, int width, T *dst) {
+            const int per = width / EPC;
+            for (int i = tid; i < n * per; i += 256) {
+                const int r = i / per, c = (i - r * per) * EPC, t = rev ? a.L - 1 - (w + r) : w + r;
+                copy16(dst + r * width + c, src + t * lds + c);
+            }
+        };
+        rows(k, j.ldk, dk, stage);
+        if (!STATE_ONLY) rows(q, j.ldq, dk, stage + LA_C * dk);
+        rows(v, j.ldv, nc, stage + LA_C * dk * (STATE_ONLY ? 1 : 2));
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto inside = [&](int m, int c) { return lane16 + 16 * m < dk && c0 + col + c < dv; };
-    float s[KR][4];
+    if (w0 < w1) fetch(w0);
+
+    // the state, zero behind the columns
     const float *from = STATE_ONLY ? nullptr
                         : seg > 0  ? j.seg + (bh * a.nseg + seg) * ssize
                         : j.s_in   ? j.s_in + bh * ssize
                                    : nullptr;
-#pragma unroll
-    for (int m = 0; m < KR; ++m)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) s[m][c] = from && inside(m, c) ? from[at(m, c)] : 0.f;
+    // (four entries side by side in memory at a time: of a row d, or of a column)
+    auto state_at = [&](int i, int &d, int &c) {
+        if (j.transposed) { d = i >> 4; c = (i & 15) * 4; }
+        else { d = ((i >> 7) * 2 + (i & 1)) * 4; c = i >> 1 & 63; }
+        return j.transposed ? (int64_t)d * dv + c0 + c : (int64_t)(c0 + c) * dk + d;
+    };
+    for (int i = tid; i < dk * (LA_COLS / 4); i += 256) {
+        int d, c;
+        const int64_t at = state_at(i, d, c);
+        const float4 x = from && c < nc ? *reinterpret_cast<const float4 *>(from + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float *to = ss + d * LA_COLS + c;
+        if (j.transposed) *reinterpret_cast<float4 *>(to) = x;
+        else { to[0] = x.x; to[LA_COLS] = x.y; to[2 * LA_COLS] = x.z; to[3 * LA_COLS] = x.w; }
+    }
+    // threads by column pairs and rows: 32, 16 or 8 pairs wide, as the columns need
+    const int pairs = nc > 32 ? 32 : nc > 16 ? 16 : 8;
+    const int cp = (tid % pairs) * 2, rg = tid / pairs;      // row group: 4, 2 or 1 rows
+    const bool column = cp < nc;
+    const int first = rev ? 0 : 1;
 
-    for (int w = w0; w < w1; w += LA_TS) {
-        const int n = min(LA_TS, w1 - w);
-        __syncthreads();
-        for (int i = tid; i < n * DKP; i += 256) {
-            const int r = i / DKP, d = i % DKP, t = j.reverse ? a.L - 1 - (w + r) : w + r;
-            sk[i] = d < dk ? to_f32<T>(k[t * j.ldk + d]) : 0.f;
-            if (!STATE_ONLY) sq[i] = d < dk ? to_f32<T>(q[t * j.ldq + d]) : 0.f;
-        }
-        for (int i = tid; i < n * LA_COLS; i += 256) {
-            const int r = i / LA_COLS, e = c0 + i % LA_COLS, t = j.reverse ? a.L - 1 - (w + r) : w + r;
-            sv[i] = e < dv ? to_f32<T>(v[t * j.ldv + e]) : 0.f;
-        }
-        __syncthreads();
-        for (int r = 0; r < n; ++r) {
-            const float4 v4 = *reinterpret_cast<const float4 *>(sv + r * LA_COLS + col);
-            const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int m = 0; m < KR; ++m) {
-                const float kk = sk[r * DKP + lane16 + 16 * m];
-                const float qq = STATE_ONLY ? 0.f : sq[r * DKP + lane16 + 16 * m];
-                const float ka = kk * j.scale_a;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    // the decay meets the state before the token (forward) or behind it (backward)
-                    const float y = s[m][c];
-                    const float x = j.reverse ? fmaf(ka, vv[c], y) : fmaf(lam.hi, y, fmaf(lam.lo, y, ka * vv[c]));
-                    if (!STATE_ONLY) acc[c] = fmaf(x, qq, acc[c]);
-                    s[m][c] = j.reverse ? fmaf(lam.hi, x, lam.lo * x) : x;
-                }
+    for (int w = w0; w < w1; w += LA_C) {
+        const int n = min(LA_C, w1 - w);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();                                     // the chunk is there, and the one in front is done with
+        auto unpack = [&](const T *src, int width, int lds, float *dst) {
+            const int per = width / 4;
+            for (int i = tid; i < LA_C * per; i += 256) {
+                const int r = i / per, c = (i - r * per) * 4;
+                *reinterpret_cast<float4 *>(dst + r * lds + c) = r < n ? load4(src + r * width + c) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            if (!STATE_ONLY) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) acc[c] += __shfl_xor_sync(0xffffffffu, acc[c], o);
-                if (lane16 < 4) {
-                    const float x = lane16 == 0 ? acc[0] : lane16 == 1 ? acc[1] : lane16 == 2 ? acc[2] : acc[3];
-                    so[r * LA_COLS + col + lane16] = x * j.scale_c;
-                }
+        };
+        unpack(stage, dk, ld, sk);
+        if (!STATE_ONLY) unpack(stage + LA_C * dk, dk, ld, sq);
+        {
+            const T *src = stage + LA_C * dk * (STATE_ONLY ? 1 : 2);
+            for (int i = tid; i < LA_C * (LA_COLS / 4); i += 256) {
+                const int r = i / (LA_COLS / 4), c = i % (LA_COLS / 4) * 4;
+                const float4 x = r < n && c < nc ? load4(src + r * nc + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!STATE_ONLY) *reinterpret_cast<float4 *>(sv + r * LA_COLS + c) = x;
+                const float e = r < n ? j.scale_a * pow_hi[n - r - first] : 0.f;
+                *reinterpret_cast<float4 *>(swv + r * LA_COLS + c) = make_float4(e * x.x, e * x.y, e * x.z, e * x.w);
             }
         }
+        __syncthreads();
+        if (w + LA_C < w1) fetch(w + LA_C);
+        auto outputs = [&](auto rows) {
+            constexpr int R = decltype(rows)::value;
+            const int i0 = rg * R;
+            float acc[R][2];
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = 0.f;
+            if (column && i0 < n) {
+                chunk_carried<R>(sq + i0 * ld, ld, ss + cp, dk, acc);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float e = i0 + r < n ? j.scale_c * pow_hi[i0 + r + first] : 0.f;
+                    acc[r][0] *= e;
+                    acc[r][1] *= e;
+                }
+            }
+            __syncthreads();                                 // scores are there, and S has been read
+            if (column && i0 < n) {
+                chunk_inside<R>(sp + i0 * (LA_C + 4), sv + cp, i0, acc);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (i0 + r >= n) continue;
+                    const int t = rev ? a.L - 1 - (w + i0 + r) : w + i0 + r;
+                    const int64_t at = ((int64_t)b * a.L + t) * j.ldo + (int64_t)h * dv + c0 + cp;
+                    if (sizeof(T) == 4 || j.o_f32) *reinterpret_cast<float2 *>((float *)j.o + at) = make_float2(acc[r][0], acc[r][1]);
+                    else *reinterpret_cast<__nv_bfloat162 *>((__nv_bfloat16 *)j.o + at) = __floats2bfloat162_rn(acc[r][0], acc[r][1]);
+                }
+            }
+        };
         if (!STATE_ONLY) {
-            __syncthreads();
-            for (int i = tid; i < n * LA_COLS; i += 256) {
-                const int r = i / LA_COLS, e = c0 + i % LA_COLS, t = j.reverse ? a.L - 1 - (w + r) : w + r;
-                if (e >= dv) continue;
-                const int64_t p = ((int64_t)b * a.L + t) * j.ldo + (int64_t)h * dv + e;
-                if (j.o_f32) ((float *)j.o)[p] = so[i];
-                else ((T *)j.o)[p] = from_f32<T>(so[i]);
+            // scores of rows i, i + 16 by columns j, j + 16
+            const int i = tid >> 4, jj = tid & 15;
+            float s00 = 0.f, s10 = 0.f, s11 = 0.f;           // (i, jj), (i + 16, jj), (i + 16, jj + 16); the fourth is behind
+#pragma unroll 2
+            for (int d = 0; d < dk; d += 4) {
+                const float4 q0 = *reinterpret_cast<const float4 *>(sq + i * ld + d), q1 = *reinterpret_cast<const float4 *>(sq + (i + 16) * ld + d);
+                const float4 k0 = *reinterpret_cast<const float4 *>(sk + jj * ld + d), k1 = *reinterpret_cast<const float4 *>(sk + (jj + 16) * ld + d);
+                s00 = fmaf(q0.w, k0.w, fmaf(q0.z, k0.z, fmaf(q0.y, k0.y, fmaf(q0.x, k0.x, s00))));
+                s10 = fmaf(q1.w, k0.w, fmaf(q1.z, k0.z, fmaf(q1.y, k0.y, fmaf(q1.x, k0.x, s10))));
+                s11 = fmaf(q1.w, k1.w, fmaf(q1.z, k1.z, fmaf(q1.y, k1.y, fmaf(q1.x, k1.x, s11))));
+            }
+            sp[i * (LA_C + 4) + jj] = jj <= i ? j.scale_p * pow_hi[i - jj] * s00 : 0.f;
+            sp[(i + 16) * (LA_C + 4) + jj] = j.scale_p * pow_hi[i + 16 - jj] * s10;
+            sp[(i + 16) * (LA_C + 4) + jj + 16] = jj <= i ? j.scale_p * pow_hi[i - jj] * s11 : 0.f;
+            if (pairs == 32) outputs(std::integral_constant<int, 4>{});
+            else if (pairs == 16) outputs(std::integral_constant<int, 2>{});
+            else outputs(std::integral_constant<int, 1>{});
+        }
+        if (column) {
+            const float hi = pow_hi[n], lo = n == LA_C ? pow_lo : 0.f;
+            for (int d = rg * 4; d < dk; d += 1024 / pairs) {
+                float u[4][2];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) u[r][0] = u[r][1] = 0.f;
+#pragma unroll 4
+                for (int t = 0; t < (n + 3 & ~3); ++t) {     // (rows behind the last token are zeros)
+                    const float4 kk = *reinterpret_cast<const float4 *>(sk + t * ld + d);
+                    const float2 x = *reinterpret_cast<const float2 *>(swv + t * LA_COLS + cp);
+                    const float kr[4] = {kk.x, kk.y, kk.z, kk.w};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        u[r][0] = fmaf(kr[r], x.x, u[r][0]);
+                        u[r][1] = fmaf(kr[r], x.y, u[r][1]);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float2 *at = reinterpret_cast<float2 *>(ss + (d + r) * LA_COLS + cp);
+                    const float2 s = *at;
+                    *at = make_float2(fmaf(hi, s.x, fmaf(lo, s.x, u[r][0])), fmaf(hi, s.y, fmaf(lo, s.y, u[r][1])));
+                }
             }
         }
     }
+    __syncthreads();
     float *to = STATE_ONLY ? j.seg + (bh * a.nseg + seg + 1) * ssize
                 : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
-    if (to) {
-#pragma unroll
-        for (int m = 0; m < KR; ++m)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (inside(m, c)) to[at(m, c)] = s[m][c];
-    }
+    if (to)
+        for (int i = tid; i < dk * (LA_COLS / 4); i += 256) {
+            int d, c;
+            const int64_t at = state_at(i, d, c);
+            if (c >= nc) continue;
+            const float *x = ss + d * LA_COLS + c;
+            *reinterpret_cast<float4 *>(to + at) = j.transposed ? *reinterpret_cast<const float4 *>(x)
+                                                                : make_float4(x[0], x[LA_COLS], x[2 * LA_COLS], x[3 * LA_COLS]);
+        }
 }
 
 }  // namespace
@@ -172,34 +336,29 @@ int launch_chain(LaunchCtx &ctx, const LaArgs &a)
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
 
-template <typename T, int KR> int launch_steps_k(LaunchCtx &ctx, const LaArgs &a)
+template <typename T> int launch_steps(LaunchCtx &ctx, const LaArgs &a)
 {
-    int dv = 0;
-    for (int i = 0; i < a.njobs; ++i) dv = std::max(dv, a.job[i].dv);
-    const unsigned slices = ceil_div(dv, LA_COLS);
-    const unsigned one = (unsigned)(a.njobs * a.B * a.H);
+    int dk = 0, dv = 0;
+    for (int i = 0; i < a.njobs; ++i) {
+        dk = std::max(dk, a.job[i].dk);
+        dv = std::max(dv, a.job[i].dv);
+    }
+    const unsigned slices = ceil_div(dv, LA_COLS), one = (unsigned)(a.njobs * a.B * a.H);
+    const size_t states = chunk_smem(dk, sizeof(T), true).bytes, outputs = chunk_smem(dk, sizeof(T), false).bytes;
+    if (!ensure_dynamic_smem((const void *)la_chunks_kernel<T, true>, states) ||
+        !ensure_dynamic_smem((const void *)la_chunks_kernel<T, false>, outputs))
+        return SWIMBA_ERR_CUDA;
     if (a.nseg > 1) {
         ctx.begin(STAGE_LA_STATES);
-        launch_kernel(la_steps_kernel<T, KR, true>, dim3(one * (a.nseg - 1), slices), dim3(256), 0, ctx.stream, true, a);
+        launch_kernel(la_chunks_kernel<T, true>, dim3(one * (a.nseg - 1), slices), dim3(256), states, ctx.stream, true, a, dk);
         ctx.end();
         const int rc = launch_chain(ctx, a);
         if (rc != SWIMBA_OK) return rc;
     }
     ctx.begin(STAGE_LA_STEPS);
-    launch_kernel(la_steps_kernel<T, KR, false>, dim3(one * a.nseg, slices), dim3(256), 0, ctx.stream, true, a);
+    launch_kernel(la_chunks_kernel<T, false>, dim3(one * a.nseg, slices), dim3(256), outputs, ctx.stream, true, a, dk);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
-}
-
-template <typename T> int launch_steps(LaunchCtx &ctx, const LaArgs &a)
-{
-    int dk = 0;
-    for (int i = 0; i < a.njobs; ++i) dk = std::max(dk, a.job[i].dk);
-    if (dk <= 16) return launch_steps_k<T, 1>(ctx, a);
-    if (dk <= 32) return launch_steps_k<T, 2>(ctx, a);
-    if (dk <= 64) return launch_steps_k<T, 4>(ctx, a);
-    if (dk <= 128) return launch_steps_k<T, 8>(ctx, a);
-    return launch_steps_k<T, 16>(ctx, a);
 }
 
 // out[t, g, n] = sum_i part[t, g r + i, n], four entries a thread, heads in order.
@@ -223,14 +382,6 @@ la_head_sum_kernel(const float *__restrict__ part, int64_t nout, int r, int N, T
         const __nv_bfloat162 a = __floats2bfloat162_rn(s.x, s.y), b = __floats2bfloat162_rn(s.z, s.w);
         *reinterpret_cast<uint2 *>(out + i) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
-}
-
-__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p)
-{
-    const uint2 r = *reinterpret_cast<const uint2 *>(p);
-    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
-                       __uint_as_float(r.y & 0xffff0000u));
 }
 
 // One token for each of B sequences: S <- lambda S + v k^T (fp32, from s_in to s_out), o = scale S q.
@@ -334,9 +485,19 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
     const bool tiles = la_tiles_shape(dtype, N, P);
     const int most = la_most(tiles, B, H, N, P, njobs, sm_count);
     if (!tiles) {
-        const int len = std::max(LA_STEP_SEG, ceil_div(ceil_div(L, most), 16) * 16);
-        *seg_len = std::min(len, L);
-        *nseg = ceil_div(L, *seg_len);
+        // Waves of blocks times chunks, in chunks: the outputs, and, where sequences are cut, the pass for the states (half of
+        // that) and two more launches (about 6).
+        const int64_t blocks = (int64_t)njobs * B * H * ceil_div(std::max(N, P), LA_COLS);
+        double best = 1e30;
+        for (int n = 1; n <= std::min(most, ceil_div(L, LA_STEP_SEG)); ++n) {
+            const int len = ceil_div(ceil_div(L, n), LA_C), ns = ceil_div(L, len * LA_C);
+            const double cost = (double)ceil_div64(blocks * ns, sm_count) * len +
+                                (ns > 1 ? 0.5 * ceil_div64(blocks * (ns - 1), sm_count) * len + 6 : 0);
+            if (cost >= best) continue;
+            best = cost;
+            *seg_len = std::min(len * LA_C, L);
+            *nseg = ns;
+        }
         return;
     }
     // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states (about
