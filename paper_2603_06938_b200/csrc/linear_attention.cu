@@ -91,6 +91,39 @@ __device__ __forceinline__ void chunk_inside(const float *sp, const float *sv, i
     }
 }
 
+// S_d <- (hi + lo) S_d + sum_t k_td (w v)_t, R rows d by two columns at a time; group rg of `groups` takes every so many-th R.
+// (Rows behind the last token are zeros.)
+template <int R>
+__device__ __forceinline__ void chunk_state(const float *sk, int ld, const float *swv, float *ss, int rg, int groups, int dk, int n,
+                                            float hi, float lo)
+{
+    for (int d = rg * R; d < dk; d += groups * R) {
+        float u[R][2];
+#pragma unroll
+        for (int r = 0; r < R; ++r) u[r][0] = u[r][1] = 0.f;
+#pragma unroll 4
+        for (int t = 0; t < (n + 3 & ~3); ++t) {
+            const float2 x = *reinterpret_cast<const float2 *>(swv + t * LA_COLS);
+#pragma unroll
+            for (int r = 0; r < R; r += 4) {
+                const float4 kk = *reinterpret_cast<const float4 *>(sk + t * ld + d + r);
+                const float kr[4] = {kk.x, kk.y, kk.z, kk.w};
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    u[r + z][0] = fmaf(kr[z], x.x, u[r + z][0]);
+                    u[r + z][1] = fmaf(kr[z], x.y, u[r + z][1]);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float2 *at = reinterpret_cast<float2 *>(ss + (d + r) * LA_COLS);
+            const float2 s = *at;
+            *at = make_float2(fmaf(hi, s.x, fmaf(lo, s.x, u[r][0])), fmaf(hi, s.y, fmaf(lo, s.y, u[r][1])));
+        }
+    }
+}
+
 // One (job, sequence, head, segment) and LA_COLS columns of its v, by chunks of 32 tokens in fp32, with r the place of a token
 // in the order of the walk and the state S in shared memory:
 //   P_ij = scale_p lambda^(i - j) q_i k_j  (j <= i),   o_i = sum_j P_ij v_j + scale_c lambda^(i + first) S^T q_i
@@ -140,8 +173,9 @@ la_chunks_kernel(const __grid_constant__ LaArgs a, int dk_most)
         const int n = min(LA_C, w1 - w);
         auto rows = [&](const T *src, int64_t lds, int width, T *dst) {
             const int per = width / EPC;
+            const uint32_t inv = (1u << 20) / per + 1;       // (i / per for i per < 2^20)
             for (int i = tid; i < n * per; i += 256) {
-                const int r = i / per, c = (i - r * per) * EPC, t = rev ? a.L - 1 - (w + r) : w + r;
+                const int r = i * inv >> 20, c = (i - r * per) * EPC, t = rev ? a.L - 1 - (w + r) : w + r;
                 copy16(dst + r * width + c, src + t * lds + c);
             }
         };
@@ -183,8 +217,10 @@ la_chunks_kernel(const __grid_constant__ LaArgs a, int dk_most)
         __syncthreads();                                     // the chunk is there, and the one in front is done with
         auto unpack = [&](const T *src, int width, int lds, float *dst) {
             const int per = width / 4;
+            const uint32_t inv = (1u << 20) / per + 1;
+#pragma unroll 2
             for (int i = tid; i < LA_C * per; i += 256) {
-                const int r = i / per, c = (i - r * per) * 4;
+                const int r = i * inv >> 20, c = (i - r * per) * 4;
                 *reinterpret_cast<float4 *>(dst + r * lds + c) = r < n ? load4(src + r * width + c) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
         };
@@ -249,30 +285,9 @@ la_chunks_kernel(const __grid_constant__ LaArgs a, int dk_most)
             else if (pairs == 16) outputs(std::integral_constant<int, 2>{});
             else outputs(std::integral_constant<int, 1>{});
         }
-        if (column) {
-            const float hi = pow_hi[n], lo = n == LA_C ? pow_lo : 0.f;
-            for (int d = rg * 4; d < dk; d += 1024 / pairs) {
-                float u[4][2];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) u[r][0] = u[r][1] = 0.f;
-#pragma unroll 4
-                for (int t = 0; t < (n + 3 & ~3); ++t) {     // (rows behind the last token are zeros)
-                    const float4 kk = *reinterpret_cast<const float4 *>(sk + t * ld + d);
-                    const float2 x = *reinterpret_cast<const float2 *>(swv + t * LA_COLS + cp);
-                    const float kr[4] = {kk.x, kk.y, kk.z, kk.w};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        u[r][0] = fmaf(kr[r], x.x, u[r][0]);
-                        u[r][1] = fmaf(kr[r], x.y, u[r][1]);
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float2 *at = reinterpret_cast<float2 *>(ss + (d + r) * LA_COLS + cp);
-                    const float2 s = *at;
-                    *at = make_float2(fmaf(hi, s.x, fmaf(lo, s.x, u[r][0])), fmaf(hi, s.y, fmaf(lo, s.y, u[r][1])));
-                }
-            }
+        if (column) {                                        // eight rows a thread where there are as many, else four
+            if (dk * pairs >= 2048) chunk_state<8>(sk, ld, swv + cp, ss + cp, rg, 256 / pairs, dk, n, pow_hi[n], n == LA_C ? pow_lo : 0.f);
+            else chunk_state<4>(sk, ld, swv + cp, ss + cp, rg, 256 / pairs, dk, n, pow_hi[n], n == LA_C ? pow_lo : 0.f);
         }
     }
     __syncthreads();
