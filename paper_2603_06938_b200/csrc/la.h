@@ -39,7 +39,7 @@ struct LaArgs {
     int B, L, H;
     int seg_len, nseg;           // tokens per segment (the last in the sequence may be shorter), segments per sequence
     int per;                     // pieces per segment, of seg_len / per tokens, that the pass for the states works
-    // CTAs of the kernel for 128 values: the first `whole` (job, segment, head, sequence)s have one each; the tiles of the others
+    // CTAs of the kernel for more than 64 values: the first `whole` (job, segment, head, sequence)s have one each; the tiles of the others
     // are shared by ncut, of which number c gives the outputs of tiles cut[c] .. cut[c + 1] - 1 of the walk and carries only
     // the state through those in front
     int whole, ncut, cut[5];
@@ -88,12 +88,12 @@ size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs,
 // Tensor map of [B, L, streams, D], rows ld apart, for boxes of 128 tokens of 64 entries of one stream.  Rows behind
 // the sequence read as zeros and are not written.
 bool la_stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int streams, int L, int B, int64_t ld);
-// The tensor-core kernel (la_tiles.cu): the head sizes it has, whether the rows are within its reach, its launches
+// The tensor-core kernels (la_tiles.cu): the head sizes they take, whether the rows are within their reach, their launches
 // (states: the pass that leaves every segment's end state).
 bool la_tiles_shape(int dtype, int N, int P);
 bool la_tiles_reach(const LaArgs &a);
 int launch_la_tiles(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);
-int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);      // its jobs of 128 values (la_wide.cu)
+int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);      // those of more than 64 values (la_wide.cu)
 // Runs the jobs: per-segment states, their chain, outputs; or outputs alone when nseg == 1.
 int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a, int sm_count);
 // out[t, g, :] = sum over the r heads of group g of part[t, g r + i, :], in that order.

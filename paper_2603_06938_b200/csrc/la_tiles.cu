@@ -1,5 +1,5 @@
-// Linear attention with a decay for each head on the tensor cores (bf16; 64 or 128 entries of keys and of values):
-// tiles of 128 tokens, the carried state on chip.  What a job is: la.h.  Per tile, with n tokens, r the place of a
+// Linear attention with a decay for each head on the tensor cores (bf16; heads of up to 128 entries of keys and 64 of values,
+// made up to 64 or 128 by the zeros that copies read behind a head): tiles of 128 tokens, the carried state on chip.  What a job is: la.h.  Per tile, with n tokens, r the place of a
 // token in the order of the walk, and the state S [DK, DV] entering it:
 //   QK   A = Q K^T                                            scores
 //        P_ij = scale_p lambda^|i-j| A_ij  for tokens j that i sees, else 0
@@ -24,7 +24,7 @@ namespace swimba {
 namespace {
 
 constexpr int LT = 128;                      // tokens per tile
-constexpr int LDV = 64;                      // columns of v a CTA works (128 of them: two CTAs)
+constexpr int LDV = 64;                      // columns of v
 constexpr int PARTS = 3;                     // bf16 parts of w V at most
 constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
 // warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 8 for the state, 4 for o.  Every role's loops
@@ -76,11 +76,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     }
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
-    // slices of one head side by side, then the jobs on it: they read the same rows at about the same time
+    // the jobs on one head side by side: they read the same rows at about the same time
     int64_t id = blockIdx.x;
-    const int slices = a.job[0].dv / LDV;
-    const int c0 = (int)(id % slices) * LDV;
-    id /= slices;
     const int ji = (int)(id % a.njobs);
     id /= a.njobs;
     // segments, or pieces of them for the states alone, in the order of the walk (the last segment's end state enters nothing)
@@ -165,7 +162,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             };
             load(&sm->full_k[s], &sm->free_k[s], L::K + s * L::QB, L::QB, &maps.k[ji], 0, h / j.rk);
             if (!STATE_ONLY) load(&sm->full_q[s], &sm->free_q[s], L::Q + s * L::QB, L::QB, &maps.q[ji], 0, h / j.rq);
-            load(&sm->full_v[s], &sm->free_v[s], L::V + s * SLAB, SLAB, &maps.v[ji], c0, h / j.rv);
+            load(&sm->full_v[s], &sm->free_v[s], L::V + s * SLAB, SLAB, &maps.v[ji], 0, h / j.rv);
         }
         // No copy may be in flight when the CTA leaves: after an abort nobody else has waited for the last ones (those
         // that were not issued any more never arrive, and these waits run out soon).
@@ -411,16 +408,16 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         const int q4 = warp & 3, d = (q4 * 32 + lane) % DK;
         const int cc = (warp - WARP_STATE) / 4 * 32 + (DK == 128 ? 0 : (q4 >> 1) * 16);
         const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_KV + cc;
-        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * j.dv;
-        const int64_t at0 = j.transposed ? (int64_t)d * j.dv + c0 + cc : (int64_t)(c0 + cc) * DK + d;
-        const int64_t step = j.transposed ? 1 : DK;
+        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)j.dk * j.dv;
+        const int64_t step = j.transposed ? 1 : j.dk, at0 = j.transposed ? (int64_t)d * j.dv + cc : cc * step + d;
+        const int nv = d < j.dk ? j.dv - cc : 0;             // columns of this thread's that the state has (in eights)
         const float *from = STATE_ONLY ? nullptr
                             : seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
                             : j.s_in   ? j.s_in + bh * ssize
                                        : nullptr;
         uint64_t st[NC / 2];
 #pragma unroll
-        for (int e = 0; e < NC / 2; ++e) st[e] = from ? tc::f32x2(from[at0 + 2 * e * step], from[at0 + (2 * e + 1) * step]) : 0ull;
+        for (int e = 0; e < NC / 2; ++e) st[e] = from && (2 * e & ~7) < nv ? tc::f32x2(from[at0 + 2 * e * step], from[at0 + (2 * e + 1) * step]) : 0ull;
         auto publish = [&]() {                   // the bf16 copy that QS reads: row d, columns side by side
 #pragma unroll
             for (int e = 0; e < NC / 2; e += 4)
@@ -471,6 +468,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         if (to) {
 #pragma unroll
             for (int e = 0; e < NC / 2; ++e) {
+                if ((2 * e & ~7) >= nv) continue;
                 const float2 v = tc::f32x2_get(st[e]);
                 to[at0 + 2 * e * step] = v.x;
                 to[at0 + (2 * e + 1) * step] = v.y;
@@ -497,7 +495,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                 tc::tmem_ld_wait();
                 if (odd) {                       // what is not finite, for the rows that see it
                     const __nv_bfloat16 *v = (const __nv_bfloat16 *)j.v + ((int64_t)b * a.L + at) * j.ldv +
-                                             (int64_t)(h / j.rv) * j.dv + c0 + c;
+                                             (int64_t)(h / j.rv) * j.dv + c;
 #pragma unroll 1
                     for (int jb = 0; jb < 8; ++jb) {
                         uint32_t p[8];
@@ -512,9 +510,15 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                             const float pf = __uint_as_float(k & 1 ? pw & 0xffff0000u : pw << 16);
                             if (jj < n && (rev ? jj >= r : jj <= r)) {
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) {
-                                    const float u = __bfloat162float(v[jj * j.ldv + e]);
-                                    if (!isfinite(u)) y[e] = __float_as_uint(fmaf(pf, u, __uint_as_float(y[e])));
+                                for (int g = 0; g < 16; g += 8) {
+                                    if (c + g >= j.dv) continue;
+                                    const uint4 u4 = *reinterpret_cast<const uint4 *>(v + jj * j.ldv + g);
+                                    const uint32_t in[4] = {u4.x, u4.y, u4.z, u4.w};
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) {
+                                        const float u = __uint_as_float(e & 1 ? in[e >> 1] & 0xffff0000u : in[e >> 1] << 16);
+                                        if (!isfinite(u)) y[g + e] = __float_as_uint(fmaf(pf, u, __uint_as_float(y[g + e])));
+                                    }
                                 }
                             }
                         }
@@ -534,9 +538,10 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                 }
                 if (j.o_f32) {
                     if (r < n) {
-                        uint4 *p = reinterpret_cast<uint4 *>((float *)j.o + ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * j.dv + c0 + c);
+                        uint4 *p = reinterpret_cast<uint4 *>((float *)j.o + ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * j.dv + c);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) p[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                        for (int e = 0; e < 4; ++e)
+                            if (c + (4 * e & ~7) < j.dv) p[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
                     }
                     __syncwarp();
                 } else {
@@ -556,7 +561,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             tc::named_bar_sync(1, 128);
             if (q4 == 0) {                       // (rows behind the sequence are clipped by the tensor map)
                 if (tc::elect_one()) {
-                    tc::tma_store_4d(&maps.o[ji], stage, c0, h, at, b);
+                    tc::tma_store_4d(&maps.o[ji], stage, 0, h, at, b);
                     tc::bulk_commit_group();
                     tc::bulk_wait_read_all();
                     tc::mbar_arrive(&sm->free_v[s]);
@@ -575,7 +580,7 @@ bool run_tiles(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 {
     const size_t smem = Sm<DK>::SMALL + sizeof(Small);
     if (!ensure_dynamic_smem((const void *)la_tiles_kernel<DK, STATE_ONLY>, smem)) return false;
-    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.per : a.nseg) * (a.job[0].dv / LDV);
+    const int64_t n = (int64_t)a.njobs * a.B * a.H * (STATE_ONLY ? (a.nseg - 1) * a.per : a.nseg);
     ctx.begin(STATE_ONLY ? STAGE_LA_STATES : STAGE_LA_TILES);
     launch_kernel(la_tiles_kernel<DK, STATE_ONLY>, dim3((unsigned)n), dim3(THREADS), smem, ctx.stream, true, maps, a,
                   ctx.d_status);
@@ -595,7 +600,7 @@ bool la_stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int s
 
 bool la_tiles_shape(int dtype, int N, int P)
 {
-    return dtype == SWIMBA_DTYPE_BF16 && (N == 64 || N == 128) && (P == 64 || P == 128);
+    return dtype == SWIMBA_DTYPE_BF16 && N <= 128 && P <= 128;
 }
 
 bool la_tiles_reach(const LaArgs &a)
@@ -609,13 +614,14 @@ bool la_tiles_reach(const LaArgs &a)
 
 int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states, int sm_count)
 {
-    // jobs of one pair of head sizes go in one launch
+    // jobs of one pair of head sizes, made up to 64 or 128 with zeros by the copies, go in one launch
+    auto full = [](int n) { return n <= 64 ? 64 : 128; };
     for (int dk : {64, 128})
         for (int dv : {64, 128}) {
             LaArgs a = all;
             a.njobs = 0;
             for (int i = 0; i < all.njobs; ++i)
-                if (all.job[i].dk == dk && all.job[i].dv == dv) a.job[a.njobs++] = all.job[i];
+                if (full(all.job[i].dk) == dk && full(all.job[i].dv) == dv) a.job[a.njobs++] = all.job[i];
             if (a.njobs == 0) continue;
             if (dv == 128) {
                 const int rc = launch_la_wide(ctx, a, states, sm_count);

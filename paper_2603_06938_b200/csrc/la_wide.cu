@@ -1,5 +1,5 @@
-// Linear attention with a decay for each head on the tensor cores, heads of 128 values (bf16; 64 or 128 keys): the
-// same five steps per tile of 128 tokens as in la_tiles.cu, with all values of a head in one CTA, so that scores and masks
+// Linear attention with a decay for each head on the tensor cores, heads of 65 to 128 values (bf16; up to 128
+// entries of keys; made up with zeros as there): the same five steps per tile of 128 tokens as in la_tiles.cu, with all values of a head in one CTA, so that scores and masks
 // are made once.  What makes room for that in shared memory (two or three stages of Q, K and V, the bf16 state):
 //   w V   is made transposed, [DV, tokens], straight into tensor memory, a quarter of a tile at a time and two of them in
 //         turn, and is the A operand of KV:  D = (w V)^T K
@@ -88,7 +88,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     const LaJob &j = a.job[ji];
     const bool rev = j.reverse != 0;
     // four parts where the state is a result; two where only the read of it is, whose copy is rounded to bf16
-    const int parts = j.s_out ? 4 : 2, ring = 8 / parts;       // quarters of w V there is room for
+    const int parts = j.s_out && (STATE_ONLY || (seg == nall - 1 && part == nparts - 1)) ? 4 : 2, ring = 8 / parts;       // quarters of w V there is room for
     const int place = rev ? nall - 1 - seg : seg;
     const int t_begin = min(a.L, place * len), t_end = min(a.L, t_begin + len);
     const int nwalk = (t_end - t_begin + LT - 1) / LT;
@@ -183,7 +183,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             if (STATE_ONLY || NQ > 1 || t < n_pre || t >= ntiles) return;
 #pragma unroll 1
             for (int r = tile_at(t) + lane; r < tile_at(t) + tile_n(t); r += 32) {
-                const char *p = (const char *)((const __nv_bfloat16 *)j.q + ((int64_t)b * a.L + r) * j.ldq + (int64_t)(h / j.rq) * DK);
+                const char *p = (const char *)((const __nv_bfloat16 *)j.q + ((int64_t)b * a.L + r) * j.ldq + (int64_t)(h / j.rq) * j.dk);
 #pragma unroll
                 for (int o = 0; o < DK * 2; o += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + o));
             }
@@ -314,8 +314,9 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const uint32_t keep = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
         constexpr int NC = DK / 2;
         const uint32_t srow = quarter + TM_S + half * NC;
-        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)DK * DV;
-        const int64_t at0 = j.transposed ? (int64_t)half * NC * DV + i : (int64_t)i * DK + half * NC, step = j.transposed ? DV : 1;
+        const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)j.dk * j.dv;
+        const int64_t step = j.transposed ? j.dv : 1, at0 = j.transposed ? half * NC * step + i : (int64_t)i * j.dk + half * NC;
+        const int nd = i < j.dv ? j.dk - half * NC : 0;          // entries of this thread's that the state has (in eights)
         if (!STATE_ONLY) {                       // the state that enters
             const float *from = seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
                                 : j.s_in ? j.s_in + bh * ssize
@@ -325,7 +326,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             for (int c = 0; c < NC; c += 16) {
                 uint32_t x[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = from ? __float_as_uint(dec * from[at0 + (c + e) * step]) : 0u;
+                for (int e = 0; e < 16; ++e) x[e] = from && c + (e & 8) < nd ? __float_as_uint(dec * from[at0 + (c + e) * step]) : 0u;
                 __syncwarp();
                 tc::tmem_st16(srow + c, x);
             }
@@ -438,7 +439,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::tmem_ld16(srow + c, x);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) to[at0 + (c + e) * step] = ntiles > 0 ? __uint_as_float(x[e]) : 0.f;
+                for (int e = 0; e < 16; ++e)
+                    if (c + (e & 8) < nd) to[at0 + (c + e) * step] = ntiles > 0 ? __uint_as_float(x[e]) : 0.f;
             }
         }
     } else if (warp >= WARP_W && warp < WARP_O) {
@@ -560,7 +562,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::tmem_ld_wait();
                 if (odd) {                       // what is not finite, for the rows that see it
                     const __nv_bfloat16 *v = (const __nv_bfloat16 *)j.v + ((int64_t)b * a.L + at) * j.ldv +
-                                             (int64_t)(h / j.rv) * DV + half * 64 + c;
+                                             (int64_t)(h / j.rv) * j.dv + half * 64 + c;
 #pragma unroll 1
                     for (int jj = 0; jj < n; ++jj) {
                         uint32_t p[8], pw = 0;   // (the eight columns that hold token jj)
@@ -572,9 +574,15 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                         const float pf = __uint_as_float(jj & 1 ? pw & 0xffff0000u : pw << 16);
                         if (rev ? jj >= r : jj <= r) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const float u = __bfloat162float(v[jj * j.ldv + e]);
-                                if (!isfinite(u)) y[e] = __float_as_uint(fmaf(pf, u, __uint_as_float(y[e])));
+                            for (int g = 0; g < 32; g += 8) {
+                                if (half * 64 + c + g >= j.dv) continue;
+                                const uint4 u4 = *reinterpret_cast<const uint4 *>(v + jj * j.ldv + g);
+                                const uint32_t in[4] = {u4.x, u4.y, u4.z, u4.w};
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const float u = __uint_as_float(e & 1 ? in[e >> 1] & 0xffff0000u : in[e >> 1] << 16);
+                                    if (!isfinite(u)) y[g + e] = __float_as_uint(fmaf(pf, u, __uint_as_float(y[g + e])));
+                                }
                             }
                         }
                     }
@@ -587,9 +595,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 }
                 if (j.o_f32) {
                     if (r < n) {
-                        uint4 *p = reinterpret_cast<uint4 *>((float *)j.o + ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * DV + half * 64 + c);
+                        uint4 *p = reinterpret_cast<uint4 *>((float *)j.o + ((int64_t)b * a.L + at + r) * j.ldo + (int64_t)h * j.dv + half * 64 + c);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                        for (int e = 0; e < 8; ++e)
+                            if (half * 64 + c + (4 * e & ~7) < j.dv) p[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
                     }
                 } else {
 #pragma unroll
@@ -640,14 +649,16 @@ bool run_wide(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 double la_cuts(int64_t items, int nt, int sm_count, LaArgs *a)
 {
     // Whole waves of walks first, what is left shared so that its CTAs end together: a tile that only carries the state takes
-    // about half the time of the others, so each part is half as long as the one in front.
+    // 0.58 of the time of the others, so each part is 0.42 of the length of the one in front (4 sequences of 8192, 16 heads:
+    // 167 us; with halves 172).
+    constexpr double RATIO = 0.42;
     const int64_t whole = items / sm_count * sm_count, rest = items - whole;
     double best = (double)ceil_div64(items, sm_count) * nt;
     a->whole = (int)items;
     a->ncut = 1;
     if (rest == 0) return best;
     for (int m = 2; m <= 4 && m <= nt; ++m) {
-        const double first = nt / (2.0 - pow(0.5, m - 1));
+        const double first = nt * (1.0 - RATIO) / (1.0 - pow(RATIO, m));
         const double cost = (double)(whole / sm_count) * nt + (double)ceil_div64(rest * m, sm_count) * (first + 1.0);
         if (cost >= best) continue;
         best = cost;
@@ -656,7 +667,7 @@ double la_cuts(int64_t items, int nt, int sm_count, LaArgs *a)
         double at = 0;
         for (int c = 0; c < m; ++c) {
             a->cut[c] = std::max(c, (int)(at + 0.5));
-            at += first * pow(0.5, c);
+            at += first * pow(RATIO, c);
         }
         a->cut[m] = nt;
         for (int c = m - 1; c > 0; --c) a->cut[c] = std::min(a->cut[c], a->cut[c + 1] - 1);
@@ -680,7 +691,7 @@ int launch_la_wide(LaunchCtx &ctx, const LaArgs &all, bool states, int sm_count)
             (!states && !j.o_f32 && !la_stream_map(ctx.tmaps, &maps.o[i], j.o, j.dv, a.H, a.L, a.B, j.ldo)))
             return SWIMBA_ERR_CUDA;
     }
-    const bool ok = a.job[0].dk == 64 ? (states ? run_wide<64, true>(ctx, maps, a) : run_wide<64, false>(ctx, maps, a))
+    const bool ok = a.job[0].dk <= 64 ? (states ? run_wide<64, true>(ctx, maps, a) : run_wide<64, false>(ctx, maps, a))
                                       : (states ? run_wide<128, true>(ctx, maps, a) : run_wide<128, false>(ctx, maps, a));
     return ok ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }

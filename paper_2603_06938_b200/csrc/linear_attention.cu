@@ -519,7 +519,7 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
     // 0.7 of a tile each, in pieces that fill the SMs), their chain (0.15 a piece) and two more launches (about 4).
     const int nt = ceil_div(L, LA_TILE_SEG);
     const int64_t items = (int64_t)njobs * B * H;
-    const bool wide = P == 128 && (njobs == 1 || N == 128);
+    const bool wide = P > 64 && (njobs == 1 || N > 64);
     double best = 1e30;
     for (int n = 1; n <= std::min(most, nt); ++n) {
         const int len = ceil_div(nt, n), ns = ceil_div(nt, len);

@@ -240,6 +240,22 @@ def test_no_token_sees_a_later_one(dtype, N, P, t):
         assert torch.equal(g[0][0, :t], grads[0][0, :t]) and torch.equal(g[0][0, t + 1:], grads[0][0, t + 1:])
 
 
+@pytest.mark.parametrize("L", [5, 300, 1100])
+@pytest.mark.parametrize("N,P", [(16, 8), (112, 72), (48, 120), (128, 8), (80, 64), (16, 128)])
+def test_heads_between_the_tiles_sizes(N, P, L):
+    """Head sizes that tiles of 64 or 128 entries hold with a margin: states, shared heads and strided rows of the head's
+    own size, and nothing of the head beside it."""
+    i = ref.inputs("bf16", 2, L, 4, 2, N, P, seed=N + P + L, decays=[-0.002, -0.03], grad=True, state=L != 300)
+    check_forward(i, *run_forward(i, packed=L == 1100))
+    check_backward(i, run_backward(i, packed=L == 1100))
+
+
+@pytest.mark.parametrize("t", [0, 63, 128, 290])
+@pytest.mark.parametrize("N,P", [(96, 80), (112, 40), (16, 72)])
+def test_no_token_sees_a_later_one_between_the_tiles_sizes(N, P, t):
+    test_no_token_sees_a_later_one("bf16", N, P, t)
+
+
 @pytest.mark.parametrize("dtype,N,P", [("bf16", 128, 128), ("bf16", 48, 64), ("fp32", 64, 64)])
 def test_captured_replayed_and_on_two_streams(dtype, N, P):
     i = ref.inputs(dtype, 1, 500, 2, 2, N, P, seed=21, grad=True, decays=[-0.01])
