@@ -5,8 +5,10 @@
 // A row is read once: its entries stay in registers between the sums and the results, eight of them in each of
 // NV places a thread; the statistics are fp32 and in two passes over the registers (mean, then squares around it).
 // Instruction issue bounds these kernels as soon as it can (2048 entries a row by 256 threads: 77 us forward, 154
-// backward of 32768 rows; a copy of the same bytes takes 45): few threads a row, so that the sums across threads are
-// shared by many entries, and arithmetic on pairs.
+// backward of 32768 rows): few threads a row, so that the sums across threads are shared by many entries, arithmetic on pairs,
+// and places at distances known when compiling.  So that forward takes 47 us, 5.7 TB/s (a copy of the same bytes 45), with the
+// weights in shared memory (from the L1 cache, whose wavefronts they half fill, 61).  Backward takes 108 us, 3.7 TB/s, with
+// 45 % of the issue slots in use and two blocks an SM, whose warps wait for each other's sums and for shared memory.
 #include <algorithm>
 
 #include "la.h"
@@ -46,10 +48,26 @@ __device__ __forceinline__ void put8(__nv_bfloat16 *p, const uint64_t (&v)[4])
 {
     *reinterpret_cast<uint4 *>(p) = make_uint4(tc::f32x2_bf16(v[0]), tc::f32x2_bf16(v[1]), tc::f32x2_bf16(v[2]), tc::f32x2_bf16(v[3]));
 }
+// Entries that are taken apart anew in every pass over them: as fp32 they would fill the registers of a second block.
+__device__ __forceinline__ void anew(Raw8h &r) { asm volatile("" : "+r"(r.a.x), "+r"(r.a.y), "+r"(r.a.z), "+r"(r.a.w)); }
+__device__ __forceinline__ void anew(Raw8f &) {}
 __device__ __forceinline__ float both(uint64_t v)
 {
     const float2 f = tc::f32x2_get(v);
     return f.x + f.y;
+}
+
+// Weights in shared memory: of every eight the first four, then the second four of all, so that threads side by side read side
+// by side (in place, 32 bytes a thread, half of every wavefront goes unused).
+__device__ __forceinline__ void stage_weights(float *to, const float *from, float none, int n)
+{
+    for (int i = threadIdx.x; i < n; i += LN_THREADS) to[(i >> 2 & 1) * (n >> 1) + (i >> 3) * 4 + (i & 3)] = from ? from[i] : none;
+}
+__device__ __forceinline__ void staged_pairs(const float *w, int half, uint64_t (&v)[4])      // half: entries of all over 2
+{
+    const float4 a = *reinterpret_cast<const float4 *>(w), b = *reinterpret_cast<const float4 *>(w + half);
+    v[0] = tc::f32x2(a.x, a.y); v[1] = tc::f32x2(a.z, a.w);
+    v[2] = tc::f32x2(b.x, b.y); v[3] = tc::f32x2(b.z, b.w);
 }
 
 // How a block of 256 threads lies over rows: `team` threads (a power of two) per group, gpb groups of a row and rpb rows
@@ -111,7 +129,7 @@ template <int K> __device__ __forceinline__ void team_sum(float (&v)[K], int tea
     }
 }
 
-// R rows (or sets of rpb rows) at a time: their loads are in flight together and one barrier serves their sums.
+// Few entries a thread (NV 1 or 2 places), whose weights stay in registers.  R rows (or sets of rpb rows) at a time: their loads are in flight together and one barrier serves their sums.
 template <typename T, int NV, int R>
 __global__ void __launch_bounds__(LN_THREADS)
 layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict__ wt, const float *__restrict__ bias,
@@ -127,19 +145,16 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict_
     const int64_t D = (int64_t)groups * width, step = (int64_t)gridDim.x * rpb;
     const float inv = 1.f / width;
     const float *wg = wt + (int64_t)g * width, *bg = bias + (int64_t)g * width;
-    // few entries a thread: their weights stay in registers; more: they come from the L1 cache with every row
-    uint64_t w[NV > 2 ? 1 : NV][4], b[NV > 2 ? 1 : NV][4];
-    auto weights = [&](int c, uint64_t (&wv)[4], uint64_t (&bv)[4]) {
+    uint64_t w[NV][4], b[NV][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { wv[e] = tc::f32x2(1.f, 1.f); bv[e] = 0ull; }
-        if (mine && c < width) {
-            if (wt) load_pairs(wg + c, wv);
-            if (bias) load_pairs(bg + c, bv);
-        }
-    };
-    if constexpr (NV <= 2)
+    for (int i = 0; i < NV; ++i) {
+        const int c = (t + i * team) * 8;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) weights((t + i * team) * 8, w[i], b[i]);
+        for (int e = 0; e < 4; ++e) { w[i][e] = tc::f32x2(1.f, 1.f); b[i][e] = 0ull; }
+        if (!mine || c >= width) continue;
+        if (wt) load_pairs(wg + c, w[i]);
+        if (bias) load_pairs(bg + c, b[i]);
+    }
     int turn = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += R * step) {
         uint64_t v[R][NV][4];
@@ -189,18 +204,98 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict_
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * team) * 8;
-                uint64_t wv[4], bv[4], o[4];
-                if constexpr (NV > 2) weights(c, wv, bv);
+                uint64_t o[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    o[e] = NV > 2 ? tc::f32x2_fma(tc::f32x2_mul(v[k][i][e], rs2), wv[e], bv[e])
-                                  : tc::f32x2_fma(tc::f32x2_mul(v[k][i][e], rs2), w[NV > 2 ? 0 : i][e], b[NV > 2 ? 0 : i][e]);
+                for (int e = 0; e < 4; ++e) o[e] = tc::f32x2_fma(tc::f32x2_mul(v[k][i][e], rs2), w[i][e], b[i][e]);
                 if (mine && r < rows && c < width) put8(y + r * D + (int64_t)g * width + c, o);
             }
             if (mine && r < rows && t == 0) {
                 if (mean) mean[r * groups + g] = mu[k];
                 if (rstd) rstd[r * groups + g] = rs;
             }
+        }
+    }
+}
+
+// More entries a thread (NV 4 or 8 places) of one row at a time.  The weights come from shared memory with every row, the
+// entries stay as they were loaded.  TEAM: the team, where it is a warp (0: any), so that a thread's places lie at distances
+// known when compiling (with those and without the defaults of missing weights: half the instructions).
+template <typename T, int NV, int TEAM>
+__global__ void __launch_bounds__(LN_THREADS, sizeof(T) == 2 && !(NV == 8 && TEAM) ? 3 : 2)
+layer_norm_wide_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict__ wt, const float *__restrict__ bias,
+                       int64_t rows, int groups, int width, float eps, int any_team, int gpb, int rpb, T *__restrict__ y,
+                       float *__restrict__ mean, float *__restrict__ rstd)
+{
+    extern __shared__ __align__(16) float staged[];
+    __shared__ __align__(16) float red[2 * 8];
+    grid_dep_launch();
+    const int team = TEAM ? TEAM : any_team;
+    const int tid = threadIdx.x, t = tid % team, slot = tid / team;
+    const int g = blockIdx.y * gpb + slot % gpb, rslot = slot / gpb;
+    const bool mine = rslot < rpb && g < groups;
+    grid_dep_wait();
+    const int64_t D = (int64_t)groups * width, step = (int64_t)gridDim.x * rpb;
+    const float inv = 1.f / width;
+    const int g0 = blockIdx.y * gpb, nw = min(gpb, groups - g0) * width;
+    const float *sw = staged + (slot % gpb * width >> 1) + t * 4, *sb = sw + nw;
+    stage_weights(staged, wt ? wt + (int64_t)g0 * width : nullptr, 1.f, nw);
+    stage_weights(staged + nw, bias ? bias + (int64_t)g0 * width : nullptr, 0.f, nw);
+    __syncthreads();
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * rpb; r0 < rows; r0 += step) {
+        const int64_t r = r0 + rslot;
+        const bool live = mine && r < rows;
+        const T *px = x + r * ldx + (int64_t)g * width + t * 8;
+        T *py = y + r * D + (int64_t)g * width + t * 8;
+        typename Raw8<T>::type raw[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            raw[i] = {};
+            if (live && (t + i * team) * 8 < width) load_raw8(px + i * team * 8, raw[i]);
+        }
+        uint64_t v[4], a2[2] = {0ull, 0ull};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            pairs8(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a2[e & 1] = tc::f32x2_add(a2[e & 1], v[e]);
+        }
+        float s[1] = {both(tc::f32x2_add(a2[0], a2[1]))};
+        team_sum(s, team, red, turn);
+        const float mu = s[0] * inv;
+        const uint64_t m2 = tc::f32x2(-mu, -mu);
+        a2[0] = a2[1] = 0ull;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if ((t + i * team) * 8 >= width) continue;
+            anew(raw[i]);
+            pairs8(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = tc::f32x2_add(v[e], m2);
+                a2[e & 1] = tc::f32x2_fma(v[e], v[e], a2[e & 1]);
+            }
+        }
+        s[0] = both(tc::f32x2_add(a2[0], a2[1]));
+        team_sum(s, team, red, turn);
+        const float rs = rsqrtf(s[0] * inv + eps);
+        const uint64_t rs2 = tc::f32x2(rs, rs);
+        if (live && t == 0) {
+            if (mean) mean[r * groups + g] = mu;
+            if (rstd) rstd[r * groups + g] = rs;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!live || (t + i * team) * 8 >= width) continue;
+            uint64_t w[4], b[4], o[4];
+            asm volatile("" ::: "memory");               // (not all weights at once: they would not fit the registers)
+            staged_pairs(sw + i * team * 4, nw >> 1, w);
+            staged_pairs(sb + i * team * 4, nw >> 1, b);
+            anew(raw[i]);
+            pairs8(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = tc::f32x2_fma(tc::f32x2_mul(tc::f32x2_add(v[e], m2), rs2), w[e], b[e]);
+            put8(py + i * team * 8, o);
         }
     }
 }
@@ -407,6 +502,7 @@ int ln_blocks(const LnShape &s, int64_t rows, int sm_count, int per_sm)
     const int64_t need = ceil_div64(rows, s.rpb);
     return (int)std::min<int64_t>(need, std::max(1, per_sm * sm_count / s.ychunks));
 }
+constexpr size_t LN_ROOM = 220 * 1024;     // of shared memory on an SM
 constexpr int LN_GRAD_BLOCKS = 2;          // per SM, resident together: each leaves D partial sums twice
 constexpr size_t LN_GRAD_ROOM = 100 * 1024;  // of shared memory for one of them, where its rows are short enough
 
@@ -419,6 +515,22 @@ int run_norm(LaunchCtx &ctx, const LnShape &s, const void *x, int64_t ldx, const
     launch_kernel(layer_norm_kernel<T, NV, R>, dim3(ln_blocks(s, rows, sm_count, resident), s.ychunks), dim3(LN_THREADS),
                   0, ctx.stream, true, (const T *)x, ldx, w, b, rows, groups, width, eps, s.team, s.gpb, s.rpb, (T *)y,
                   mean, rstd);
+    ctx.end();
+    return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
+}
+
+template <typename T, int NV, int TEAM>
+int run_norm_wide(LaunchCtx &ctx, const LnShape &s, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
+                  int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd)
+{
+    const auto kern = layer_norm_wide_kernel<T, NV, TEAM>;
+    static const int fitting = ln_resident(kern);
+    const size_t smem = (size_t)2 * s.gpb * width * sizeof(float);
+    if (!ensure_dynamic_smem((const void *)kern, smem)) return SWIMBA_ERR_CUDA;
+    const int resident = std::max(1, std::min<int>(fitting, (int)(LN_ROOM / smem)));
+    ctx.begin(STAGE_LAYER_NORM);
+    launch_kernel(kern, dim3(ln_blocks(s, rows, sm_count, resident), s.ychunks), dim3(LN_THREADS), smem, ctx.stream, true,
+                  (const T *)x, ldx, w, b, rows, groups, width, eps, s.team, s.gpb, s.rpb, (T *)y, mean, rstd);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
@@ -452,18 +564,19 @@ int run_backward(LaunchCtx &ctx, const LnShape &s, const void *dy, const void *x
 
 }  // namespace
 
-// Rows (or sets of rpb rows) a thread takes at a time: enough bytes in flight without spilling.
-constexpr int ln_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+// Rows (or sets of rpb rows) a thread of few places takes at a time: enough bytes in flight without spilling.
+constexpr int ln_rows(int nv) { return nv == 1 ? 4 : 2; }
 
 int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
                       int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd)
 {
     const LnShape s = ln_shape(groups, width, LN_FORWARD_PLACES);
-#define LN_RUN(T, NV) run_norm<T, NV, ln_rows(NV)>(ctx, s, x, ldx, w, b, rows, groups, width, eps, sm_count, y, mean, rstd)
-    if (dtype == SWIMBA_DTYPE_FP32)
-        return s.nv == 1 ? LN_RUN(float, 1) : s.nv == 2 ? LN_RUN(float, 2) : s.nv == 4 ? LN_RUN(float, 4) : LN_RUN(float, 8);
-    return s.nv == 1 ? LN_RUN(__nv_bfloat16, 1) : s.nv == 2 ? LN_RUN(__nv_bfloat16, 2)
-           : s.nv == 4 ? LN_RUN(__nv_bfloat16, 4) : LN_RUN(__nv_bfloat16, 8);
+#define LN_ARGS ctx, s, x, ldx, w, b, rows, groups, width, eps, sm_count, y, mean, rstd
+#define LN_RUN(T) (s.nv == 1   ? run_norm<T, 1, ln_rows(1)>(LN_ARGS) : s.nv == 2 ? run_norm<T, 2, ln_rows(2)>(LN_ARGS) \
+                   : s.nv == 4 ? s.team == 32 ? run_norm_wide<T, 4, 32>(LN_ARGS) : run_norm_wide<T, 4, 0>(LN_ARGS)     \
+                   : s.team == 32 ? run_norm_wide<T, 8, 32>(LN_ARGS) : run_norm_wide<T, 8, 0>(LN_ARGS))
+    return dtype == SWIMBA_DTYPE_FP32 ? LN_RUN(float) : LN_RUN(__nv_bfloat16);
+#undef LN_ARGS
 #undef LN_RUN
 }
 
