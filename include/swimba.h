@@ -416,7 +416,7 @@ int swimba_balance_loss(swimba_handle *h, const swimba_weights *w, const void *u
  * swimba_profile_read synchronises that stream and returns how many kernels the most recent call
  * (for swimba_forward_host: its last batch slice) launched (at most max_entries), with kernel_ids[i] in 1..37 (1 router + grouping by
  * expert (for fewer than about 28000 tokens the launch also computes the SSD step sizes), 4 expert GEMM, 5 slot mix, 6 SIMT projection, 7 fp32 chunked SSM and packed decode tokens, 8 decode update, 9 SSD
- * tile kernel, 10 segment scan, 11 SSD step sizes and decays, 12 slot stream assembly, 13 slot sum, 14 small-batch projection (short forwards too), 15 convolution + SiLU, 16 gated norm, 17 step-size columns, 18 adjoint recurrence pass, 19 clearing of a gradient call's outputs, 20 weight / logit adjoints, 21 router-matrix gradient, 22 expert-matrix gradient, 23 states at the tile boundaries for the adjoint, 24 state-only SSD pass, 25 linear attention token by token, 26 its segment states, 27 their chain, 28 linear attention by tiles, 29 sum over shared heads, 30 linear attention step, 31 layer norm, 32 its gradients, 33 sums of its weight gradients, 34 counts of the balance loss, 35 its pass over the tokens, 36 its router-matrix gradient, 37 its sums; 2 and 3 are not in use) and ms[i] its duration in milliseconds.
+ * tile kernel, 10 segment scan, 11 SSD step sizes and decays, 12 slot stream assembly, 13 slot sum, 14 small-batch projection (short forwards too), 15 convolution + SiLU, 16 gated norm, 17 step-size columns, 18 adjoint recurrence pass, 19 clearing of a gradient call's outputs, 20 weight / logit adjoints, 21 router-matrix gradient, 22 expert-matrix gradient, 23 states at the tile boundaries for the adjoint, 24 state-only SSD pass, 25 linear attention by chunks in fp32, 26 its segment states, 27 their chain, 28 linear attention by tiles, 29 sum over shared heads, 30 linear attention step, 31 layer norm, 32 its gradients, 33 sums of its weight gradients, 34 counts of the balance loss, 35 its pass over the tokens, 36 its router-matrix gradient, 37 its sums; 2 and 3 are not in use) and ms[i] its duration in milliseconds.
  * Both arrays are HOST arrays. */
 int swimba_profile(swimba_handle *h, int enable);
 int swimba_profile_read(swimba_handle *h, int32_t *kernel_ids, float *ms, int32_t max_entries);

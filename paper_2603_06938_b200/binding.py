@@ -543,7 +543,7 @@ KERNEL_NAMES = {1: "router_topk", 4: "expert_gemm",
                 9: "ssd_tiles", 10: "segment_scan", 11: "ssd_scalars", 12: "slot_streams",
                 13: "slot_sum", 14: "project_small", 15: "conv_silu", 16: "gated_rmsnorm",
                 17: "dt_columns", 18: "ssd_adjoint", 19: "clear", 20: "dpi_dg", 21: "dw_router",
-                22: "dw_expert", 23: "adjoint_states", 24: "ssd_state", 25: "la_steps", 26: "la_states", 27: "la_chain", 28: "la_tiles", 29: "la_head_sum",
+                22: "dw_expert", 23: "adjoint_states", 24: "ssd_state", 25: "la_chunks", 26: "la_states", 27: "la_chain", 28: "la_tiles", 29: "la_head_sum",
                 30: "la_step", 31: "layer_norm", 32: "layer_norm_backward", 33: "layer_norm_sum", 34: "balance_count",
                 35: "balance_tokens", 36: "balance_dw", 37: "balance_sum"}
 

@@ -40,11 +40,11 @@ int check_sizes(swimba_handle *h, int32_t B, int32_t L)
     return SWIMBA_OK;
 }
 
-// Workspace of a call of njobs jobs: the segment states of each, then (gradients with shared heads) the per-head
-// gradients of queries and keys in fp32.
+// Workspace of a call of njobs jobs: the segment states of each, a copy of the states that enter, then (gradients with
+// shared heads) the per-head gradients of queries and keys in fp32.
 struct LaLayout {
     int seg_len, nseg, per;
-    size_t seg[LA_MAX_JOBS], dq, dk, total;
+    size_t seg[LA_MAX_JOBS], entry, dq, dk, total;
 };
 LaLayout la_layout(const swimba_handle *h, int B, int L, int njobs)
 {
@@ -56,6 +56,8 @@ LaLayout la_layout(const swimba_handle *h, int B, int L, int njobs)
         l.seg[i] = off;
         off += align_up(la_segment_bytes(c.dtype, B, L, c.n_heads, c.d_state, c.head_dim, njobs, h->sm_count));
     }
+    l.entry = off;
+    off += align_up((size_t)B * c.n_heads * c.head_dim * c.d_state * sizeof(float));
     l.dq = l.dk = off;
     if (njobs > 1 && c.n_groups != c.n_heads) {
         const size_t n = align_up((size_t)B * L * c.n_heads * c.d_state * sizeof(float));
@@ -64,6 +66,23 @@ LaLayout la_layout(const swimba_handle *h, int B, int L, int njobs)
     }
     l.total = std::max<size_t>(off, kAlign);
     return l;
+}
+
+// States that enter and states that leave may be one tensor.  Blocks of one walk or job that read it need not have started
+// when those of another are done and write it, so they read a copy.
+int la_keep_entry(const swimba_handle *h, LaunchCtx &ctx, LaArgs &a, float *room)
+{
+    const float *shared = nullptr;
+    for (int i = 0; i < a.njobs; ++i)
+        for (int o = 0; o < a.njobs; ++o)
+            if (a.job[i].s_in && a.job[i].s_in == a.job[o].s_out) shared = a.job[i].s_in;
+    // (one job's whole walks: every block reads what it will write itself; walks of more than 64 values may be shared)
+    if (!shared || (a.njobs == 1 && a.nseg == 1 && (h->cfg.head_dim <= 64 || a.L <= 128))) return SWIMBA_OK;
+    const size_t n = (size_t)a.B * a.H * h->cfg.head_dim * h->cfg.d_state * sizeof(float);
+    if (cudaMemcpyAsync(room, shared, n, cudaMemcpyDeviceToDevice, ctx.stream) != cudaSuccess) return SWIMBA_ERR_CUDA;
+    for (int i = 0; i < a.njobs; ++i)
+        if (a.job[i].s_in == shared) a.job[i].s_in = room;
+    return SWIMBA_OK;
 }
 
 }  // namespace
@@ -107,7 +126,9 @@ int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void
     const int r = c.n_heads / c.n_groups;
     a.job[0] = LaJob{q, k, v, ldq, ldk, ldv, r, r, 1, c.d_state, c.head_dim, 0, 0, state_in, state_out, o, HP, 0,
                      scale, scale, 1.f, (float *)((char *)workspace + l.seg[0])};
-    return close_ctx(h, ctx, launch_la(ctx, c.dtype, a, h->sm_count), "linear attention launch failed");
+    rc = la_keep_entry(h, ctx, a, (float *)((char *)workspace + l.entry));
+    if (rc == SWIMBA_OK) rc = launch_la(ctx, c.dtype, a, h->sm_count);
+    return close_ctx(h, ctx, rc, "linear attention launch failed");
 }
 
 size_t swimba_linear_attention_backward_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L)
@@ -156,7 +177,8 @@ int swimba_linear_attention_backward(swimba_handle *h, const float *log_decay, c
     a.job[0] = LaJob{d_o, v, k, HP, ldv, ldk, 1, 1, r, P, N, 0, 1, state_in, nullptr, gq, HN, shared, scale, scale, 1.f, seg[0]};
     a.job[1] = LaJob{v, d_o, q, ldv, HP, ldq, 1, 1, r, P, N, 1, 1, d_state_out, nullptr, gk, HN, shared, scale, 1.f, scale, seg[1]};
     a.job[2] = LaJob{k, q, d_o, ldk, ldq, HP, r, r, 1, N, P, 1, 0, d_state_out, d_state_in, dv, HP, 0, scale, 1.f, scale, seg[2]};
-    rc = launch_la(ctx, c.dtype, a, h->sm_count);
+    rc = la_keep_entry(h, ctx, a, (float *)(ws + l.entry));
+    if (rc == SWIMBA_OK) rc = launch_la(ctx, c.dtype, a, h->sm_count);
     if (rc == SWIMBA_OK && shared) {
         rc = launch_la_head_sum(ctx, c.dtype, (const float *)gq, (int64_t)B * L, c.n_groups, r, N, dq);
         if (rc == SWIMBA_OK)

@@ -19,7 +19,7 @@ enum Stage {
     STAGE_SLOT_SUM = 13, STAGE_PROJECT_SMALL = 14, STAGE_CONV = 15, STAGE_GATED_NORM = 16,
     STAGE_DT_COLUMNS = 17, STAGE_SSD_ADJOINT = 18, STAGE_CLEAR = 19, STAGE_DPI_DG = 20,
     STAGE_DW_ROUTER = 21, STAGE_DW_EXPERT = 22, STAGE_ADJOINT_STATES = 23, STAGE_SSD_STATE = 24,
-    STAGE_LA_STEPS = 25, STAGE_LA_STATES = 26, STAGE_LA_CHAIN = 27, STAGE_LA_TILES = 28, STAGE_LA_HEAD_SUM = 29,
+    STAGE_LA_CHUNKS = 25, STAGE_LA_STATES = 26, STAGE_LA_CHAIN = 27, STAGE_LA_TILES = 28, STAGE_LA_HEAD_SUM = 29,
     STAGE_LA_STEP = 30, STAGE_LAYER_NORM = 31, STAGE_LAYER_NORM_BACKWARD = 32, STAGE_LAYER_NORM_SUM = 33,
     STAGE_BALANCE_COUNT = 34, STAGE_BALANCE_TOKENS = 35, STAGE_BALANCE_DW = 36, STAGE_BALANCE_SUM = 37,
 };

@@ -370,7 +370,7 @@ template <typename T> int launch_steps(LaunchCtx &ctx, const LaArgs &a)
         const int rc = launch_chain(ctx, a);
         if (rc != SWIMBA_OK) return rc;
     }
-    ctx.begin(STAGE_LA_STEPS);
+    ctx.begin(STAGE_LA_CHUNKS);
     launch_kernel(la_chunks_kernel<T, false>, dim3(one * a.nseg, slices), dim3(256), outputs, ctx.stream, true, a, dk);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;

@@ -240,6 +240,46 @@ def test_no_token_sees_a_later_one(dtype, N, P, t):
         assert torch.equal(g[0][0, :t], grads[0][0, :t]) and torch.equal(g[0][0, t + 1:], grads[0][0, t + 1:])
 
 
+@pytest.mark.parametrize("dtype,B,H,N,P,L", [("bf16", 5, 14, 128, 128, 700), ("bf16", 1, 2, 64, 64, 1900), ("fp32", 1, 2, 32, 64, 900),
+                                             ("bf16", 2, 100, 128, 128, 300)])
+def test_states_in_place_where_blocks_share_a_walk(dtype, B, H, N, P, L):
+    """States that go back to where they came from, when several blocks read what one of them writes in the end: the bits of
+    separate buffers, eagerly and replayed."""
+    i = ref.inputs(dtype, B, L, H, H, N, P, seed=41, grad=True, decays=[-0.001, -0.02])
+    want_o, want_s = run_forward(i)
+    want_g = run_backward(i)
+    d, h = put(i, False), ref.handle(i)
+    o, s, ds = torch.empty_like(d["v"]), d["s0"].clone(), d["ds"].clone()
+    dq, dk, dv = torch.empty_like(d["q"]), torch.empty_like(d["k"]), torch.empty_like(d["v"])
+    ws = torch.empty(sb.swimba_linear_attention_workspace_bytes(h, B, L), dtype=torch.uint8, device="cuda")
+    wb = torch.empty(sb.swimba_linear_attention_backward_workspace_bytes(h, B, L), dtype=torch.uint8, device="cuda")
+
+    def call():
+        sb.swimba_linear_attention(h, d["g"], d["q"], d["k"], d["v"], s, B, L, i["scale"], o, s, ws)
+        sb.swimba_linear_attention_backward(h, d["g"], d["q"], d["k"], d["v"], d["s0"], d["do"], ds, B, L, i["scale"], dq, dk,
+                                            dv, ds, wb)
+
+    def same():
+        torch.cuda.synchronize()
+        assert torch.equal(o, want_o) and torch.equal(s, want_s)
+        assert all(torch.equal(a, b) for a, b in zip((dq, dk, dv, ds), want_g))
+        s.copy_(d["s0"])
+        ds.copy_(d["ds"])
+        for t in (o, dq, dk, dv):
+            t.fill_(float("nan"))
+
+    call()
+    same()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        graph.replay()
+        same()
+    assert sb.swimba_status(h) == 0
+
+
 @pytest.mark.parametrize("L", [5, 300, 1100])
 @pytest.mark.parametrize("N,P", [(16, 8), (112, 72), (48, 120), (128, 8), (80, 64), (16, 128)])
 def test_heads_between_the_tiles_sizes(N, P, L):
