@@ -64,14 +64,15 @@ __device__ __forceinline__ LaDecay la_decay(float g)
     return LaDecay{(float)l, (float)(l - (double)(float)l)};
 }
 
-// w v in bf16 parts, for two values and their weights at a time.  A weight goes in as three bf16 parts of its own; the
-// remainder of a bf16 product is itself a bf16 number, so a fused multiply-add gives it exactly:
-//   four parts  wh v and its remainder, wm v, its remainder and wl v in one (together 2^-24 of w v)
-//   two parts   wh v, its remainder and wm v in one (2^-17)
-__device__ __forceinline__ void la_split(float w0, float w1, uint32_t (&p)[3])
+// w v in bf16 parts:
+//   three parts  in fp32, each part what is left of the product behind those in front (2^-24 of it)
+//   two parts    with the weight in two bf16 parts of its own (wh, wm): wh v; and its remainder, which is itself a bf16
+//                number and so comes exactly from a fused multiply-add, with wm v in one (2^-17)
+// The two parts of the weights of two values:
+__device__ __forceinline__ void la_split(float w0, float w1, uint32_t (&p)[2])
 {
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 2; ++i) {
         p[i] = tc::pack_bf16x2(w0, w1);
         w0 -= __uint_as_float(p[i] << 16);
         w1 -= __uint_as_float(p[i] & 0xffff0000u);

@@ -360,7 +360,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                     for (int k = 0; k < 4; ++k)      // (an exponent of all ones, infinity or NaN, carries into the sign's place)
                         odd |= (in[k] & 0x7f807f80u) + 0x00800080u;
                     if (parts == 2) {
-                        uint32_t wp[3];
+                        uint32_t wp[2];
                         la_split(w[z], w[z], wp);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {

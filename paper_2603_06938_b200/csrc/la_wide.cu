@@ -25,7 +25,7 @@ constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
 // warps: copies, products, tensor memory, spare; 8 for the masks and, while scores are made, the state, 8 for w V, 8 for o
 constexpr int THREADS = 896;
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_ALLOC = 2, WARP_MASK = 4, WARP_W = 12, WARP_O = 20;
-// tensor memory columns: scores and over them P (bf16), O, S, w V of quarters of a tile: four of them in two parts, or two in four
+// tensor memory columns: scores and over them P (bf16), O, S, w V of quarters of a tile: four of them in two parts, or two in three
 constexpr uint32_t TM_QK = 0, TM_O = 128, TM_S = 256, TM_VW = 384, TM_COLS = 512;
 
 template <int DK> struct Sm {
@@ -43,15 +43,17 @@ struct Small {
     alignas(16) float pow_col[32];           // factors of a score block's columns
     float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
     float pow[LT + 1];                       // lambda^m
-    float weight[LT];                        // of a whole tile's tokens in w V
-    alignas(16) uint32_t wsplit[LT / 2][4];  // their parts, two tokens at a time
+    alignas(16) float weight[LT];            // of a whole tile's tokens in w V
+    alignas(16) uint32_t wsplit[LT / 2][2];  // their bf16 parts, two tokens at a time
 };
-static_assert(offsetof(Small, pow_col) % 16 == 0 && offsetof(Small, wsplit) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
+static_assert(offsetof(Small, pow_col) % 16 == 0 && offsetof(Small, weight) % 16 == 0 && offsetof(Small, wsplit) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
 
 struct Maps {
     CUtensorMap q[LA_MAX_JOBS], k[LA_MAX_JOBS], v[LA_MAX_JOBS], o[LA_MAX_JOBS];
 };
 
+__device__ __forceinline__ float low_half(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high_half(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 __device__ __forceinline__ uint32_t bits2(uint32_t a, uint32_t b) { return tc::pack_bf16x2(__uint_as_float(a), __uint_as_float(b)); }
 
 // STATE_ONLY: from a zero state, and only the end state is kept (in seg).
@@ -87,8 +89,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     const int h = (int)(id % a.H), b = (int)(id / a.H);
     const LaJob &j = a.job[ji];
     const bool rev = j.reverse != 0;
-    // four parts where the state is a result; two where only the read of it is, whose copy is rounded to bf16
-    const int parts = j.s_out && (STATE_ONLY || (seg == nall - 1 && part == nparts - 1)) ? 4 : 2, ring = 8 / parts;       // quarters of w V there is room for
+    // three parts where the state is a result; two where only the read of it is, whose copy is rounded to bf16
+    const int parts = j.s_out && (STATE_ONLY || (seg == nall - 1 && part == nparts - 1)) ? 3 : 2, ring = 8 / parts;       // quarters of w V there is room for
     const int place = rev ? nall - 1 - seg : seg;
     const int t_begin = min(a.L, place * len), t_end = min(a.L, t_begin + len);
     const int nwalk = (t_end - t_begin + LT - 1) / LT;
@@ -152,9 +154,9 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     else if (tid >= 512 && tid < 640) sm->weight[tid - 512] = j.scale_a * exp2f((rev ? tid - 511 : 639 - tid) * g2);
     else if (tid >= 640 && tid < 704) {
         const int q = 2 * (tid - 640);
-        uint32_t p[3];
+        uint32_t p[2];
         la_split(j.scale_a * exp2f((rev ? q + 1 : 127 - q) * g2), j.scale_a * exp2f((rev ? q + 2 : 126 - q) * g2), p);
-        *reinterpret_cast<uint4 *>(sm->wsplit[tid - 640]) = make_uint4(p[0], p[1], p[2], 0u);
+        *reinterpret_cast<uint2 *>(sm->wsplit[tid - 640]) = make_uint2(p[0], p[1]);
     }
     tc::tc_fence_before();
     __syncthreads();
@@ -239,7 +241,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
 #pragma unroll 1
             for (int qd = 0; qd < 4; ++qd) {
                 const int buf = qd & (ring - 1);
-                tc::mbar_wait(&sm->vw_full[buf], parts == 4 ? qd >> 1 : t & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->vw_full[buf], parts == 3 ? qd >> 1 : t & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 if (leader) {
                     uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + qd * 4096));
@@ -459,7 +461,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             __nv_bfloat162 odd = la_pair(0u);         // becomes NaN with the first entry that is not finite
 #pragma unroll 1
             for (int qd = 0; qd < 4; ++qd) {
-                uint32_t r[8], w[4][3];
+                uint32_t r[8], w[4][2];               // (weights of two tokens: three parts as floats, two in bf16 parts)
                 const uint32_t at = src0 + s * VB + qd * 4096;
                 tc::ldmatrix_x4_trans(at, r[0], r[1], r[2], r[3]);
                 tc::ldmatrix_x4_trans(at + 2048, r[4], r[5], r[6], r[7]);      // (16 tokens on: same swizzle)
@@ -467,19 +469,22 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 if (t >= n_pre && n == LT) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(sm->wsplit[(j0 >> 1) + c * 4]);
-                        w[c][0] = x.x; w[c][1] = x.y; w[c][2] = x.z;
+                        const uint2 x = *reinterpret_cast<const uint2 *>(parts == 3 ? (const uint32_t *)&sm->weight[j0 + c * 8]
+                                                                                    : sm->wsplit[(j0 >> 1) + c * 4]);
+                        w[c][0] = x.x; w[c][1] = x.y;
                     }
                 } else {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const int jj = j0 + c * 8;
-                        la_split(jj < n ? tail * sm->weight[jj + shift] : 0.f, jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f, w[c]);
+                        const float w0 = jj < n ? tail * sm->weight[jj + shift] : 0.f, w1 = jj + 1 < n ? tail * sm->weight[jj + 1 + shift] : 0.f;
+                        if (parts == 3) { w[c][0] = __float_as_uint(w0); w[c][1] = __float_as_uint(w1); }
+                        else la_split(w0, w1, w[c]);
                     }
                 }
                 const int buf = qd & (ring - 1);
                 if (4 * t + qd >= ring) {             // (what stood in this place of the ring has been multiplied)
-                    tc::mbar_wait(&sm->vw_done[buf], (parts == 4 ? qd >> 1 : t & 1) ^ 1, abort_flag, d_status);
+                    tc::mbar_wait(&sm->vw_done[buf], (parts == 3 ? qd >> 1 : t & 1) ^ 1, abort_flag, d_status);
                     tc::tc_fence_after();
                 }
                 if (!STATE_ONLY)
@@ -487,26 +492,31 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     for (int e = 0; e < 8; ++e) odd = __hfma2(la_pair(r[e]), la_pair(0u), odd);
                 const uint32_t dst = to + buf * parts * 16;
                 uint32_t p[8];
-                // (the remainder of a bf16 product is a bf16 number: la.h)
+                if (parts == 2) {                     // (the remainder of a bf16 product is a bf16 number: la.h)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = la_bits(__hmul2(la_pair(w[e >> 1][0]), la_pair(r[e])));
-                tc::tmem_st_16x128b_x4(dst, p);
+                    for (int e = 0; e < 8; ++e) p[e] = la_bits(__hmul2(la_pair(w[e >> 1][0]), la_pair(r[e])));
+                    tc::tmem_st_16x128b_x4(dst, p);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = la_bits(__hfma2(la_pair(w[e >> 1][0]), la_pair(r[e]), __hneg2(la_pair(p[e]))));
-                if (parts == 2) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = la_bits(__hfma2(la_pair(w[e >> 1][1]), la_pair(r[e]), la_pair(p[e])));
+                    for (int e = 0; e < 8; ++e) {
+                        const __nv_bfloat162 rest = __hfma2(la_pair(w[e >> 1][0]), la_pair(r[e]), __hneg2(la_pair(p[e])));
+                        p[e] = la_bits(__hfma2(la_pair(w[e >> 1][1]), la_pair(r[e]), rest));
+                    }
                     tc::tmem_st_16x128b_x4(dst + 16, p);
                 } else {
-                    tc::tmem_st_16x128b_x4(dst + 16, p);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = la_bits(__hmul2(la_pair(w[e >> 1][1]), la_pair(r[e])));
-                    tc::tmem_st_16x128b_x4(dst + 32, p);
+                    uint32_t p1[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        p[e] = la_bits(__hfma2(la_pair(w[e >> 1][2]), la_pair(r[e]),
-                                               __hfma2(la_pair(w[e >> 1][1]), la_pair(r[e]), __hneg2(la_pair(p[e])))));
-                    tc::tmem_st_16x128b_x4(dst + 48, p);
+                        p[e] = tc::pack_bf16x2(__uint_as_float(w[e >> 1][0]) * low_half(r[e]), __uint_as_float(w[e >> 1][1]) * high_half(r[e]));
+                    tc::tmem_st_16x128b_x4(dst, p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x0 = fmaf(__uint_as_float(w[e >> 1][0]), low_half(r[e]), -low_half(p[e]));
+                        const float x1 = fmaf(__uint_as_float(w[e >> 1][1]), high_half(r[e]), -high_half(p[e]));
+                        p1[e] = tc::pack_bf16x2(x0, x1);
+                        p[e] = tc::pack_bf16x2(x0 - low_half(p1[e]), x1 - high_half(p1[e]));
+                    }
+                    tc::tmem_st_16x128b_x4(dst + 16, p1);
+                    tc::tmem_st_16x128b_x4(dst + 32, p);
                 }
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
@@ -649,9 +659,9 @@ bool run_wide(LaunchCtx &ctx, const Maps &maps, const LaArgs &a)
 double la_cuts(int64_t items, int nt, int sm_count, LaArgs *a)
 {
     // Whole waves of walks first, what is left shared so that its CTAs end together: a tile that only carries the state takes
-    // 0.58 of the time of the others, so each part is 0.42 of the length of the one in front (4 sequences of 8192, 16 heads:
-    // 167 us; with halves 172).
-    constexpr double RATIO = 0.42;
+    // three quarters of the time of the others where the state is a result (w V in three parts), so each part is a quarter as
+    // long as the one in front (4 sequences of 8192, 16 heads: 186 us; 0.36 as long 190; whole walks 227, segments 192).
+    constexpr double RATIO = 0.25;
     const int64_t whole = items / sm_count * sm_count, rest = items - whole;
     double best = (double)ceil_div64(items, sm_count) * nt;
     a->whole = (int)items;

@@ -516,7 +516,7 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
         return;
     }
     // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states (about
-    // 0.7 of a tile each, in pieces that fill the SMs), their chain (0.15 a piece) and two more launches (about 4).
+    // 0.7 of a tile each, in pieces that fill the SMs), their chain (0.15 a piece) and two more launches (about 9).
     const int nt = ceil_div(L, LA_TILE_SEG);
     const int64_t items = (int64_t)njobs * B * H;
     const bool wide = P > 64 && (njobs == 1 || N > 64);
@@ -529,7 +529,7 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
             states = 1e30;
             for (int p = 1; p <= 4 && p * ns <= std::min(most, nt); ++p) {
                 if (len % p != 0) continue;
-                const double c = 0.7 * ceil_div64(items * (ns - 1) * p, sm_count) * (len / p) + 4 + 0.15 * ns * p;
+                const double c = 0.7 * ceil_div64(items * (ns - 1) * p, sm_count) * (len / p) + 9 + 0.15 * ns * p;
                 if (c < states) { states = c; pieces = p; }
             }
         }
