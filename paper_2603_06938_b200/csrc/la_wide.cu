@@ -6,7 +6,9 @@
 //   S     lies in tensor memory in fp32, [DV, DK]; between two tiles it is read, rounded for QS and scaled by lambda^n,
 //         and KV adds to it
 //   O     one region: Q S^T, scaled row by row in place, then P V on top
-// Shared memory is what bounds such a tile: 7860 cycles of reads and writes for two CTAs of 64 values each against 3900 here.
+// Shared memory bounds such a tile first: 7860 cycles of reads and writes for two CTAs of 64 values each against 3900 here;
+// the chain scores - masks - P V - o of a tile is not much shorter.  Measured, 4 sequences of 8192 tokens, 16 heads of
+// 128 x 128: 186 us (floor 82), 3.6 us a tile and CTA, 64 walks on 128 SMs; their gradients, 192 walks, 414 us (floor 144).
 #include <algorithm>
 #include <cmath>
 #include <cstddef>

@@ -1,5 +1,5 @@
-// Linear attention with a decay for each head: the CUDA-core kernel (fp32, and bf16 head sizes that the
-// tensor-core kernel does not take), the chain of segment states, the sum over shared heads and the
+// Linear attention with a decay for each head: the CUDA-core kernel (fp32, and bf16 heads of more than 128
+// entries, which the tensor-core kernels do not take), the chain of segment states, the sum over shared heads and the
 // single-token step.  What a job is: la.h.
 #include <algorithm>
 #include <type_traits>
@@ -128,7 +128,11 @@ __device__ __forceinline__ void chunk_state(const float *sk, int ld, const float
 // in the order of the walk and the state S in shared memory:
 //   P_ij = scale_p lambda^(i - j) q_i k_j  (j <= i),   o_i = sum_j P_ij v_j + scale_c lambda^(i + first) S^T q_i
 //   S <- lambda^n S + sum_j k_j (scale_a lambda^(n - j - first) v_j)^T
-// (first = 1 walking forward, 0 backward).  A thread works a few rows by two columns of each product.
+// (first = 1 walking forward, 0 backward).  A thread works a few rows by two columns of each product.  Chunks, because a
+// recurrence token by token spends four operations on an entry of the state and as many shuffles as operations on its sums:
+// gradients of 2 x 1000 tokens, 16 heads of 128 x 128, fp32: 556 us, by tokens 1139; 256 tokens of 8 heads of 16 x 64: 36 us,
+// by tokens in segments 63.  Bound by reads of shared memory (a chunk of 128 keys takes 18000 cycles, a third of them in
+// fused multiply-adds) and, with few heads, by the latency of a chunk's four phases (6000 cycles).
 // STATE_ONLY: from a zero state, and only the end state is kept (in seg).
 template <typename T, bool STATE_ONLY>
 __global__ void __launch_bounds__(256)
@@ -307,7 +311,7 @@ la_chunks_kernel(const __grid_constant__ LaArgs a, int dk_most)
 }  // namespace
 
 // seg[.., i] holds the end state of piece i - 1 from a zero entry (i >= 1); on exit the state that enters piece i.  One
-// thread per four entries walks a sequence's pieces.
+// thread per four entries walks a sequence's pieces.  (7 us for 9 pieces of 16 heads of 64 x 64: a launch and nine latencies.)
 __global__ void __launch_bounds__(256)
 la_chain_kernel(const __grid_constant__ LaArgs a)
 {
@@ -401,7 +405,8 @@ la_head_sum_kernel(const float *__restrict__ part, int64_t nout, int r, int N, T
 
 // One token for each of B sequences: S <- lambda S + v k^T (fp32, from s_in to s_out), o = scale S q.
 // A group of LR lanes owns ROWS rows of a head's state at a time, four entries of each row a lane, all of whose
-// loads are in flight before the first is used.  Bound by the state's bytes, read and written once.
+// loads are in flight before the first is used.  Bound by the state's bytes, read and written once: 128 sequences of 16 heads
+// of 128 x 128 take 53 us, 5.1 TB/s (a copy reaches 6.6); of one sequence, 12 us a call, it is the launch.
 constexpr int ST_ROWS = 8;
 template <typename T, int LR>
 __global__ void __launch_bounds__(256)
@@ -483,9 +488,9 @@ void run_step_n(LaunchCtx &ctx, const float *log_decay, const void *q, int64_t l
 }  // namespace
 
 namespace {
-// What a segment's length is a multiple of: token-by-token segments have 64 tokens at least, tiles 128.
+// What a segment has at least, by chunks 64 tokens, and what its length is a multiple of by tiles.
 constexpr int LA_STEP_SEG = 64, LA_TILE_SEG = 128;
-// The most segments a sequence is cut into: token by token, as many as give every SM two blocks; by tiles, as many
+// The most segments a sequence is cut into: by chunks, as many as give every SM two blocks; by tiles, as many
 // as fill four waves (pieces included).
 int la_most(bool tiles, int B, int H, int N, int P, int njobs, int sm_count)
 {
