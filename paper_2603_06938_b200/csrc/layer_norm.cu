@@ -10,6 +10,7 @@
 // weights in shared memory (from the L1 cache, whose wavefronts they half fill, 61).  Backward takes 108 us, 3.7 TB/s, with
 // 45 % of the issue slots in use and two blocks an SM, whose warps wait for each other's sums and for shared memory.
 #include <algorithm>
+#include <climits>
 
 #include "la.h"
 #include "tc05.cuh"
@@ -76,7 +77,8 @@ struct LnShape {
     int team, nv, gpb, rpb, ychunks;
 };
 // most: places a thread at most while a warp or part of one has a row (wider rows take more warps first, then more places).
-inline LnShape ln_shape(int groups, int width, int most)
+// room: entries of the groups that a block works at most, where a thread has more than two places (but one group always fits).
+inline LnShape ln_shape(int groups, int width, int most, int room)
 {
     LnShape s;
     const int chunks = width / 8;
@@ -87,12 +89,14 @@ inline LnShape ln_shape(int groups, int width, int most)
     while (s.team < LN_THREADS && s.team * s.nv < chunks) s.team *= 2;
     while (s.team * s.nv < chunks) s.nv *= 2;
     s.gpb = std::min(groups, LN_THREADS / s.team);
+    if (s.nv > 2) s.gpb = std::max(1, std::min(s.gpb, room / width));
     s.ychunks = ceil_div(groups, s.gpb);
     s.gpb = ceil_div(groups, s.ychunks);
     s.rpb = LN_THREADS / (s.team * s.gpb);
     return s;
 }
 constexpr int LN_FORWARD_PLACES = 8, LN_BACKWARD_PLACES = 4;
+constexpr int LN_FORWARD_ROOM = 8192;     // (their weights, 64 KB, leave an SM three blocks)
 
 // Sums over the threads of a team.  A team wider than a warp meets in `red` (8 floats per sum), of which there are two,
 // taken in turn, so that one barrier of the team a call is enough; every thread of the team calls it.
@@ -570,7 +574,7 @@ constexpr int ln_rows(int nv) { return nv == 1 ? 4 : 2; }
 int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, const float *w, const float *b, int64_t rows,
                       int groups, int width, float eps, int sm_count, void *y, float *mean, float *rstd)
 {
-    const LnShape s = ln_shape(groups, width, LN_FORWARD_PLACES);
+    const LnShape s = ln_shape(groups, width, LN_FORWARD_PLACES, LN_FORWARD_ROOM);
 #define LN_ARGS ctx, s, x, ldx, w, b, rows, groups, width, eps, sm_count, y, mean, rstd
 #define LN_RUN(T) (s.nv == 1   ? run_norm<T, 1, ln_rows(1)>(LN_ARGS) : s.nv == 2 ? run_norm<T, 2, ln_rows(2)>(LN_ARGS) \
                    : s.nv == 4 ? s.team == 32 ? run_norm_wide<T, 4, 32>(LN_ARGS) : run_norm_wide<T, 4, 0>(LN_ARGS)     \
@@ -582,7 +586,7 @@ int launch_layer_norm(LaunchCtx &ctx, int dtype, const void *x, int64_t ldx, con
 
 size_t layer_norm_partial_bytes(int64_t rows, int groups, int width, int sm_count)
 {
-    const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES);
+    const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES, INT_MAX);
     return (size_t)ln_blocks(s, rows, sm_count, LN_GRAD_BLOCKS) * 2 * groups * width * sizeof(float);
 }
 
@@ -590,7 +594,7 @@ int launch_layer_norm_backward(LaunchCtx &ctx, int dtype, const void *dy, const 
                                const float *mean, const float *rstd, int64_t rows, int groups, int width, int sm_count,
                                void *dx, float *dw, float *db, float *partial)
 {
-    const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES);
+    const LnShape s = ln_shape(groups, width, LN_BACKWARD_PLACES, INT_MAX);
 #define LN_RUN(T, NV) run_backward<T, NV>(ctx, s, dy, x, ldx, w, mean, rstd, rows, groups, width, sm_count, dx, partial)
     int rc;
     if (dtype == SWIMBA_DTYPE_FP32)

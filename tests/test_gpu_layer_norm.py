@@ -74,6 +74,14 @@ def test_norm_and_gradients(dtype, rows, groups, width):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,groups,width", [(50, 8, 2048), (7, 5, 1032), (900, 3, 4096), (3, 2, 16384), (40, 9, 776), (700, 1, 2056)])
+def test_wide_groups(dtype, rows, groups, width):
+    """Groups of several places a thread: some of them, or one, to a block."""
+    run(dtype, rows, groups, width, seed=rows)
+    run(dtype, rows, groups, width, weights=False, margin=8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_without_weights_strided_rows_and_a_large_mean(dtype):
     run(dtype, 77, 2, 128, weights=False, margin=64)
     run(dtype, 40, 1, 512, margin=8, offset=100.0)
