@@ -29,6 +29,7 @@ namespace {
 
 constexpr int LT = 128;                      // tokens per tile
 constexpr int LDV = 64;                      // columns of v
+constexpr int MARKS = 4;                     // places of the marks of tiles whose V is not all finite
 constexpr int PARTS = 3;                     // bf16 parts of w V at most
 constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
 // warps: copies, products, tensor memory, spare; 8 for the masks, 8 for w V, 8 for the state, 4 for o.  Every role's loops
@@ -50,7 +51,9 @@ struct Small {
     uint64_t qk_full, qk_read, p_full, qs_done, pv_done, vw_full[4], kv_done[4], kv_read, s_full, o_free;
     uint32_t tmem;
     int abort_flag;
-    int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
+    // 1 + the tile whose V is not all finite, in place t % 4: with three stages of V the warps of w V mark tile t + 2 while
+    // the epilogue may still look for the mark of t and the masks for that of t - 1
+    int odd_tile[MARKS];
     alignas(16) float pow_col[32];           // factors of a score block's columns
     float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
     float pow[LT + 1];                       // lambda^m
@@ -117,7 +120,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             tc::mbar_init(&sm->vw_full[s], 8);
             tc::mbar_init(&sm->kv_done[s], 1);
         }
-        sm->odd_tile[0] = sm->odd_tile[1] = 0;
+        for (int i = 0; i < MARKS; ++i) sm->odd_tile[i] = 0;
         tc::mbar_init(&sm->qk_full, 1);
         tc::mbar_init(&sm->qk_read, 8);
         tc::mbar_init(&sm->p_full, 8);
@@ -318,7 +321,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                 }
                 if (k == 0 && t > 0) {           // (P has been read, by the epilogue too where V was not all finite)
                     tc::mbar_wait(&sm->pv_done, (t - 1) & 1, abort_flag, d_status);
-                    if (((volatile int *)sm->odd_tile)[(t - 1) & 1] == t) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
+                    if (((volatile int *)sm->odd_tile)[(t - 1) % MARKS] == t) tc::mbar_wait(&sm->o_free, (t - 1) & 1, abort_flag, d_status);
                     tc::tc_fence_after();
                 }
                 tc::tmem_st16(to + k * 16, o);
@@ -397,7 +400,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                         if ((in & 0x7f800000u) == 0x7f800000u) in &= 0xffffu;
                         *at = in;
                     }
-                    ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
+                    ((volatile int *)sm->odd_tile)[t % MARKS] = t + 1;
                 }
                 tc::fence_proxy_async_smem();
                 __syncwarp();
@@ -489,7 +492,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             tc::mbar_wait(&sm->qs_done, t & 1, abort_flag, d_status);
             tc::mbar_wait(&sm->pv_done, t & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
+            const bool odd = ((volatile int *)sm->odd_tile)[t % MARKS] == t + 1;
             uint8_t *stage = smem + L::V + s * SLAB;
 #pragma unroll 1
             for (int c = 0; c < 64; c += 16) {

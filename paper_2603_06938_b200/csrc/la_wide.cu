@@ -22,6 +22,7 @@ namespace {
 
 constexpr int LT = 128;                      // tokens per tile
 constexpr int DV = 128;
+constexpr int MARKS = 4;                     // places of the marks of tiles whose V is not all finite
 constexpr uint32_t SLAB = LT * 128;          // 128 rows of 64 bf16
 constexpr uint32_t VB = 2 * SLAB;            // bytes of a V tile
 // warps: copies, products, tensor memory, spare; 8 for the masks and, while scores are made, the state, 8 for w V, 8 for o
@@ -41,7 +42,7 @@ struct Small {
     uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, s_scaled, kv_done, vw_full[4], vw_done[4];
     uint32_t tmem;
     int abort_flag;
-    int odd_tile[2];                         // 1 + the tile whose V is not all finite, by parity
+    int odd_tile[MARKS];                     // 1 + the tile whose V is not all finite, in place t % 4 (as in la_tiles.cu)
     alignas(16) float pow_col[32];           // factors of a score block's columns
     float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
     float pow[LT + 1];                       // lambda^m
@@ -125,7 +126,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             tc::mbar_init(&sm->vw_full[s], 8);
             tc::mbar_init(&sm->vw_done[s], 1);
         }
-        sm->odd_tile[0] = sm->odd_tile[1] = 0;
+        for (int i = 0; i < MARKS; ++i) sm->odd_tile[i] = 0;
         tc::mbar_init(&sm->qk_full, 1);
         tc::mbar_init(&sm->p_full, 8);
         tc::mbar_init(&sm->qs_done, 1);
@@ -304,7 +305,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             if (t + 1 < ntiles) {
                 // the next scores go where P stands, which the epilogue reads too if V was not all finite
                 tc::mbar_wait(&sm->pv_done, f & 1, abort_flag, d_status);
-                if (((volatile int *)sm->odd_tile)[t & 1] == t + 1) tc::mbar_wait(&sm->o_free, f & 1, abort_flag, d_status);
+                if (((volatile int *)sm->odd_tile)[t % MARKS] == t + 1) tc::mbar_wait(&sm->o_free, f & 1, abort_flag, d_status);
                 scores(t + 1);
             }
         }
@@ -525,7 +526,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 __syncwarp();
                 if (t >= n_pre && qd == 3 && __any_sync(0xffffffffu, __hisnan(odd.x) || __hisnan(odd.y))) {
                     // what is not finite gives way to zeros, now that all of it has been read; PV comes behind KV
-                    ((volatile int *)sm->odd_tile)[t & 1] = t + 1;
+                    ((volatile int *)sm->odd_tile)[t % MARKS] = t + 1;
                     const int col = lg * 16 + (lane & 15);
 #pragma unroll 1
                     for (int i = lane >> 4; i < LT; i += 2) {
@@ -564,7 +565,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             if (lane == 0) tc::mbar_arrive(&sm->o_scaled);
             tc::mbar_wait(&sm->pv_done, f & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            const bool odd = ((volatile int *)sm->odd_tile)[t & 1] == t + 1;
+            const bool odd = ((volatile int *)sm->odd_tile)[t % MARKS] == t + 1;
             uint8_t *stage = smem + L::V + s * VB + half * SLAB;
 #pragma unroll 1
             for (int c = 0; c < 64; c += 32) {
