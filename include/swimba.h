@@ -348,8 +348,9 @@ int swimba_route_mix_static(swimba_handle *h, const swimba_weights *w, const voi
  *         token, the layout of the mixer's states; state_out may be state_in itself
  *   o     [B,L,H,P] dtype
  * With state_in / state_out a prompt can be worked in pieces (chunked prefill) and then by steps.  A token
- * is seen by no token before it and by no other sequence, whatever its bits.  head_dim % 8 == 0; B <= 65535;
- * B == 0 or L == 0 is a no-op.  Sums and states are fp32. */
+ * is seen by no token before it and by no other sequence, whatever its bits.  head_dim % 8 == 0; B <= 65535,
+ * L <= 2^30, B * L < 2^31 (the workspace queries give 0 beyond that); B == 0 or L == 0 is a no-op.  Sums and states
+ * are fp32. */
 size_t swimba_linear_attention_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L);
 int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void *q, int64_t ldq, const void *k,
                             int64_t ldk, const void *v, int64_t ldv, const float *state_in, int32_t B, int32_t L,

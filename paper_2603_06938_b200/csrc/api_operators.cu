@@ -29,11 +29,17 @@ int check_rows(swimba_handle *h, const void *p, int64_t ld, int64_t width)
         return fail(h, SWIMBA_ERR_MISALIGNED, "rows must start at multiples of 16 bytes");
     return SWIMBA_OK;
 }
+// Sequences of a call.  The kernels hold places in a sequence in 32 bits, one tile or segment beyond its end at most.
+constexpr int kMaxSequences = 65535, kMaxTokens = 1 << 30;
+bool la_sizes(int32_t B, int32_t L)
+{
+    return B <= kMaxSequences && L <= kMaxTokens && (int64_t)B * L < (int64_t)1 << 31;
+}
 int check_sizes(swimba_handle *h, int32_t B, int32_t L)
 {
     if (B < 0 || L < 0) return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "negative B or L");
-    if (B > 65535) return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "more than 65535 sequences per call");
-    if ((int64_t)B * L >= (int64_t)1 << 31) return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "B * L must stay below 2^31");
+    if (!la_sizes(B, L))
+        return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "more than 65535 sequences, 2^30 tokens of one, or B * L beyond 2^31");
     if ((int64_t)B * h->cfg.n_heads >= (int64_t)1 << 24)
         return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "B * n_heads must stay below 2^24");
     if (h->cfg.head_dim % 8 != 0) return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "head_dim must be a multiple of 8");
@@ -91,7 +97,7 @@ extern "C" {
 
 size_t swimba_linear_attention_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L)
 {
-    if (!h || B <= 0 || L <= 0) return 0;
+    if (!h || B <= 0 || L <= 0 || !la_sizes(B, L)) return 0;
     return la_layout(h, B, L, 1).total;
 }
 
@@ -133,7 +139,7 @@ int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void
 
 size_t swimba_linear_attention_backward_workspace_bytes(const swimba_handle *h, int32_t B, int32_t L)
 {
-    if (!h || B <= 0 || L <= 0) return 0;
+    if (!h || B <= 0 || L <= 0 || !la_sizes(B, L)) return 0;
     return la_layout(h, B, L, 3).total;
 }
 
