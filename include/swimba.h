@@ -343,7 +343,7 @@ int swimba_route_mix_static(swimba_handle *h, const swimba_weights *w, const voi
  *   q, k  [B,L,G,N] dtype, v [B,L,H,P] dtype: the row of token t of sequence b starts ld (ldq, ldk, ldv)
  *         times b*L + t elements behind the pointer, so that they may be columns of a wider matrix (the
  *         mixed streams BC [T,S] of swimba_route_mix: k = BC, q = BC + G*N, ldk = ldq = S); ld is at least
- *         the row and a multiple of 16 bytes
+ *         the row, a multiple of 16 bytes and at most 2^31 elements, and L rows lie within 2^40 bytes
  *   state_in [B,H,P,N] float or NULL (zeros), state_out [B,H,P,N] float or NULL: the state behind the last
  *         token, the layout of the mixer's states; state_out may be state_in itself
  *   o     [B,L,H,P] dtype

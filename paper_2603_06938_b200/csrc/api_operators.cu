@@ -46,6 +46,14 @@ int check_sizes(swimba_handle *h, int32_t B, int32_t L)
     return SWIMBA_OK;
 }
 
+// A sequence of rows ld apart: within the 2^40 bytes that the strides of a tensor map reach.
+int check_reach(swimba_handle *h, int64_t ld, int32_t L)
+{
+    if (ld * (int64_t)elt_size(h->cfg.dtype) * L >= (int64_t)1 << 40)
+        return fail(h, SWIMBA_ERR_UNSUPPORTED_SHAPE, "the rows of a sequence must lie within 2^40 bytes");
+    return SWIMBA_OK;
+}
+
 // Workspace of a call of njobs jobs: the segment states of each, a copy of the states that enter, then (gradients with
 // shared heads) the per-head gradients of queries and keys in fp32.
 struct LaLayout {
@@ -118,6 +126,8 @@ int swimba_linear_attention(swimba_handle *h, const float *log_decay, const void
     if ((rc = check_rows(h, q, ldq, GN)) != SWIMBA_OK || (rc = check_rows(h, k, ldk, GN)) != SWIMBA_OK ||
         (rc = check_rows(h, v, ldv, HP)) != SWIMBA_OK)
         return rc;
+    for (int64_t ld : {ldq, ldk, ldv, HP})
+        if ((rc = check_reach(h, ld, L)) != SWIMBA_OK) return rc;
     if (!aligned16(log_decay) || !aligned16(state_in) || !aligned16(o) || !aligned16(state_out) || !aligned16(workspace))
         return fail(h, SWIMBA_ERR_MISALIGNED, "tensors must be 16-byte aligned");
     const LaLayout l = la_layout(h, B, L, 1);
@@ -162,6 +172,8 @@ int swimba_linear_attention_backward(swimba_handle *h, const float *log_decay, c
     if ((rc = check_rows(h, q, ldq, GN)) != SWIMBA_OK || (rc = check_rows(h, k, ldk, GN)) != SWIMBA_OK ||
         (rc = check_rows(h, v, ldv, HP)) != SWIMBA_OK || (rc = check_rows(h, d_o, HP, HP)) != SWIMBA_OK)
         return rc;
+    for (int64_t ld : {ldq, ldk, ldv, HP, HN})
+        if ((rc = check_reach(h, ld, L)) != SWIMBA_OK) return rc;
     if (!aligned16(log_decay) || !aligned16(state_in) || !aligned16(d_state_out) || !aligned16(dq) || !aligned16(dk) ||
         !aligned16(dv) || !aligned16(d_state_in) || !aligned16(workspace))
         return fail(h, SWIMBA_ERR_MISALIGNED, "tensors must be 16-byte aligned");

@@ -89,10 +89,9 @@ size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs,
 // Tensor map of [B, L, streams, D], rows ld apart, for boxes of 128 tokens of 64 entries of one stream.  Rows behind
 // the sequence read as zeros and are not written.
 bool la_stream_map(TmapCache *cache, CUtensorMap *m, const void *p, int D, int streams, int L, int B, int64_t ld);
-// The tensor-core kernels (la_tiles.cu): the head sizes they take, whether the rows are within their reach, their launches
-// (states: the pass that leaves every segment's end state).
+// The tensor-core kernels (la_tiles.cu): the head sizes they take, their launches (states: the pass that leaves every
+// segment's end state).
 bool la_tiles_shape(int dtype, int N, int P);
-bool la_tiles_reach(const LaArgs &a);
 int launch_la_tiles(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);
 int launch_la_wide(LaunchCtx &ctx, const LaArgs &a, bool states, int sm_count);      // those of more than 64 values (la_wide.cu)
 // Runs the jobs: per-segment states, their chain, outputs; or outputs alone when nseg == 1.

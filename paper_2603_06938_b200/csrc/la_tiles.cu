@@ -610,15 +610,6 @@ bool la_tiles_shape(int dtype, int N, int P)
     return dtype == SWIMBA_DTYPE_BF16 && N <= 128 && P <= 128;
 }
 
-bool la_tiles_reach(const LaArgs &a)
-{
-    // (a tensor map's strides stay below 2^40 bytes, which in this memory only a sequence of one token exceeds: never one that is cut)
-    for (int i = 0; i < a.njobs; ++i)
-        for (int64_t ld : {a.job[i].ldq, a.job[i].ldk, a.job[i].ldv})
-            if (ld * 2 * a.L >= (int64_t)1 << 40) return false;
-    return true;
-}
-
 int launch_la_tiles(LaunchCtx &ctx, const LaArgs &all, bool states, int sm_count)
 {
     // jobs of one pair of head sizes, made up to 64 or 128 with zeros by the copies, go in one launch

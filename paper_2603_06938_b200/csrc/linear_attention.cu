@@ -564,7 +564,7 @@ size_t la_segment_bytes(int dtype, int B, int L, int H, int N, int P, int njobs,
 
 int launch_la(LaunchCtx &ctx, int dtype, const LaArgs &a, int sm_count)
 {
-    if (!la_tiles_shape(dtype, a.job[0].dk, a.job[0].dv) || !la_tiles_reach(a))
+    if (!la_tiles_shape(dtype, a.job[0].dk, a.job[0].dv))
         return dtype == SWIMBA_DTYPE_FP32 ? launch_steps<float>(ctx, a) : launch_steps<__nv_bfloat16>(ctx, a);
     if (a.nseg > 1) {
         int rc = launch_la_tiles(ctx, a, true, sm_count);
