@@ -49,6 +49,7 @@ template <int DK> struct Sm {
 struct Small {
     uint64_t full_q[3], full_k[3], full_v[3], free_q[3], free_k[3], free_v[3];
     uint64_t qk_full, qk_read, p_full, qs_done, pv_done, vw_full[4], kv_done[4], kv_read, s_full, o_free;
+    uint64_t d_free[2];                      // (states alone) D has been read
     uint32_t tmem;
     int abort_flag;
     // 1 + the tile whose V is not all finite, in place t % 4: with three stages of V the warps of w V mark tile t + 2 while
@@ -106,6 +107,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
     static_assert(NS * L::QB >= PARTS * SLAB, "w V over Q");
     auto vw_slot = [](int t, int hf) { return STATE_ONLY ? (t & 1) * 2 + hf : hf; };
     auto vw_phase = [](int t) { return STATE_ONLY ? t >> 1 : t; };
+    // D; for the states alone those of two tiles in turn, the second where scores would be
+    auto d_of = [](int t) { return STATE_ONLY && (t & 1) ? TM_QK : TM_KV; };
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) {
@@ -129,6 +132,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         tc::mbar_init(&sm->kv_read, 8);
         tc::mbar_init(&sm->s_full, 8);
         tc::mbar_init(&sm->o_free, 4);
+        tc::mbar_init(&sm->d_free[0], 8);
+        tc::mbar_init(&sm->d_free[1], 8);
         *abort_flag = 0;
         tc::fence_mbar_init();
     }
@@ -222,8 +227,10 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             const int s = t % NS;
             const uint32_t ph = (t / NS) & 1;
             // KV, by halves of the tile: w V of one is made while the other is multiplied.  It does not wait for the state.
-            if (STATE_ONLY) tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
-            else if (t > 0) tc::mbar_wait(&sm->kv_read, (t - 1) & 1, abort_flag, d_status);
+            if (STATE_ONLY) {
+                tc::mbar_wait(&sm->full_k[s], ph, abort_flag, d_status);
+                if (t > 1) tc::mbar_wait(&sm->d_free[t & 1], ((t >> 1) - 1) & 1, abort_flag, d_status);
+            } else if (t > 0) tc::mbar_wait(&sm->kv_read, (t - 1) & 1, abort_flag, d_status);
 #pragma unroll 1
             for (int hf = 0; hf < 2; ++hf) {
                 const int u = vw_slot(t, hf);
@@ -234,11 +241,10 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                     const uint64_t w = tc::smem_desc_fresh(tc::smem_desc_advance(u < 2 ? dW : dW2, hf * 8192));
 #pragma unroll
                     for (int kk = 0; kk < LT / 32; ++kk)
-                        tc::mma_ss(tm + TM_KV, tc::smem_desc_advance(k, kk * 2048), tc::smem_desc_advance(w, kk * 2048), id_kv,
-                                   hf + kk + (STATE_ONLY ? t : 0) > 0);
+                        tc::mma_ss(tm + d_of(t), tc::smem_desc_advance(k, kk * 2048), tc::smem_desc_advance(w, kk * 2048), id_kv,
+                                   hf + kk > 0);
                     tc::mma_commit(&sm->kv_done[u]);
                     if (hf == 1) tc::mma_commit(&sm->free_k[s]);
-                    if (STATE_ONLY && hf == 1 && t == ntiles - 1) tc::mma_commit(&sm->qs_done);
                 }
                 __syncwarp();
             }
@@ -341,7 +347,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         for (int t = 0; t < ntiles; ++t) {
             const int s = t % NS, n = tile_n(t);
             tc::mbar_wait(&sm->full_v[s], (t / NS) & 1, abort_flag, d_status);
-            // (states alone: every tile's additions as they are at the end of the walk, so that all tiles add up in D)
+            // (states alone: every tile's additions as they are at the end of the walk)
             const float tail = STATE_ONLY ? scale_a * exp2f((rev ? tile_at(t) - t_begin : t_end - tile_at(t) - n) * g2) : scale_a;
             const uint32_t off = tc::sw128_offset(r0, ltid & 7);           // (32 rows on: 4096 bytes, same swizzle)
             uint32_t odd = 0;
@@ -414,7 +420,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         constexpr int NC = DK == 128 ? 32 : 16;
         const int q4 = warp & 3, d = (q4 * 32 + lane) % DK;
         const int cc = (warp - WARP_STATE) / 4 * 32 + (DK == 128 ? 0 : (q4 >> 1) * 16);
-        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + TM_KV + cc;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + cc;
         const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)j.dk * j.dv;
         const int64_t step = j.transposed ? 1 : j.dk, at0 = j.transposed ? (int64_t)d * j.dv + cc : cc * step + d;
         const int nv = d < j.dk ? j.dv - cc : 0;             // columns of this thread's that the state has (in eights)
@@ -434,41 +440,46 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->s_full);
         };
-        const uint64_t one = tc::f32x2(1.f, 1.f);
-        auto collect = [&](float dec) {          // S <- dec S + D
+        // S <- dec S + D, the small parts of D first, so that S is rounded once a tile.  (The accumulators of the products cut
+        // where this rounds: tiles that added up in D would lose 2^-24 of all they hold with each of eight products, always
+        // towards zero: 1e-5 after 57 tiles of a head that forgets nothing.)
+        auto collect = [&](uint32_t from, float dec) {
             const uint64_t dec2 = tc::f32x2(dec, dec);
 #pragma unroll
-            for (int k = 0; k < NC; k += 16) {
-                uint32_t x[16], y[16];
-                tc::tmem_ld16(row + k, x);
-                tc::tmem_ld16(row + LDV + k, y);
+            for (int k = 0; k < NC; k += 8) {
+                uint32_t x[8], y[8], z[8];
+                tc::tmem_ld8(from + LDV + k, x);
+                tc::tmem_ld8(from + k, y);
+                if (parts == 3) tc::tmem_ld8(from + 2 * LDV + k, z);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    st[k / 2 + e] = tc::f32x2_fma(dec2, st[k / 2 + e], tc::f32x2_fma(one, pair_of(x[2 * e], x[2 * e + 1]), pair_of(y[2 * e], y[2 * e + 1])));
-                if (parts == 3) {
-                    tc::tmem_ld16(row + 2 * LDV + k, x);
-                    tc::tmem_ld_wait();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) st[k / 2 + e] = tc::f32x2_fma(one, pair_of(x[2 * e], x[2 * e + 1]), st[k / 2 + e]);
+                for (int e = 0; e < 4; ++e) {
+                    uint64_t &s = st[k / 2 + e];
+                    uint64_t d = pair_of(x[2 * e], x[2 * e + 1]);
+                    if (parts == 3) d = tc::f32x2_add(d, pair_of(z[2 * e], z[2 * e + 1]));
+                    d = tc::f32x2_add(d, pair_of(y[2 * e], y[2 * e + 1]));
+                    s = tc::f32x2_fma(dec2, s, d);
                 }
             }
         };
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             if (t > 0) tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
             publish();
-            const float dec = sm->pow[tile_n(t)];
+            const int n = tile_n(t);
             tc::mbar_wait(&sm->kv_done[1], t & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            collect(dec);
+            collect(row + TM_KV, sm->pow[n]);
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->kv_read);
         }
-        if (STATE_ONLY && ntiles > 0) {
-            tc::mbar_wait(&sm->qs_done, 0, abort_flag, d_status);      // (every product)
+        for (int t = 0; t < (STATE_ONLY ? ntiles : 0); ++t) {
+            tc::mbar_wait(&sm->kv_done[vw_slot(t, 1)], vw_phase(t) & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            collect(1.f);
+            collect(row + d_of(t), 1.f);
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->d_free[t & 1]);
         }
         float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
                     : seg == a.nseg - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;

@@ -40,6 +40,7 @@ template <int DK> struct Sm {
 struct Small {
     uint64_t full_q[2], full_k[3], full_v[3], free_q[2], free_k[3], free_v[3];
     uint64_t qk_full, p_full, qs_done, o_scaled, pv_done, o_free, s_full, s_scaled, kv_done, vw_full[4], vw_done[4];
+    uint64_t d_full[2], d_free[2];           // the additions of a tile that only carries the state: made, added
     uint32_t tmem;
     int abort_flag;
     int odd_tile[MARKS];                     // 1 + the tile whose V is not all finite, in place t % 4 (as in la_tiles.cu)
@@ -102,7 +103,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     // this CTA's tiles: those in front of n_pre only carry the state; barriers that the others alone use count from there
     const int n_pre = STATE_ONLY ? nwalk : nparts > 1 ? a.cut[part] : 0;
     const int ntiles = STATE_ONLY || nparts == 1 ? nwalk : a.cut[part + 1];
-    const int pre = n_pre > 0 ? 1 : 0;
+    // D, of two such tiles in turn where scores and o will be
+    auto d_of = [](int t) { return t & 1 ? TM_O : TM_QK; };
     // tokens walked behind tile t in front of tile n_pre; tile -1: all of them
     auto tokens_left = [&](int t) {
         return rev ? (t < 0 ? t_end : tile_at(t)) - (n_pre > 0 ? tile_at(n_pre - 1) : t_end)
@@ -136,6 +138,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         tc::mbar_init(&sm->s_full, 8);
         tc::mbar_init(&sm->s_scaled, 8);
         tc::mbar_init(&sm->kv_done, 1);
+        for (int s = 0; s < 2; ++s) {
+            tc::mbar_init(&sm->d_full[s], 1);
+            tc::mbar_init(&sm->d_free[s], STATE_ONLY ? 16 : 8);
+        }
         *abort_flag = 0;
         tc::fence_mbar_init();
     }
@@ -239,8 +245,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             __syncwarp();
         };
-        // KV, by quarters of the tile
-        auto add = [&](int t, bool done) {
+        // KV, by quarters of the tile: onto S; of a tile that only carries the state, into D
+        auto add = [&](int t) {
+            const bool alone = t < n_pre;
+            const uint32_t to = tm + (alone ? d_of(t) : TM_S);
 #pragma unroll 1
             for (int qd = 0; qd < 4; ++qd) {
                 const int buf = qd & (ring - 1);
@@ -250,25 +258,28 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + qd * 4096));
 #pragma unroll 1
                     for (int p = 0; p < parts; ++p) {
-                        tc::mma_ts(tm + TM_S, tm + TM_VW + (buf * parts + p) * 16, k, id_kv, !STATE_ONLY || t + qd + p > 0);
-                        tc::mma_ts(tm + TM_S, tm + TM_VW + (buf * parts + p) * 16 + 8, tc::smem_desc_advance(k, 2048), id_kv, 1);
+                        tc::mma_ts(to, tm + TM_VW + (buf * parts + p) * 16, k, id_kv, !alone || qd + p > 0);
+                        tc::mma_ts(to, tm + TM_VW + (buf * parts + p) * 16 + 8, tc::smem_desc_advance(k, 2048), id_kv, 1);
                     }
                     tc::mma_commit(&sm->vw_done[buf]);
                     if (qd == 3) {
-                        if (done) tc::mma_commit(&sm->kv_done);
+                        tc::mma_commit(alone ? &sm->d_full[t & 1] : &sm->kv_done);
                         tc::mma_commit(&sm->free_k[t % NK]);
                     }
                 }
                 __syncwarp();
             }
         };
-        if (!STATE_ONLY && pre) tc::mbar_wait(&sm->s_scaled, 0, abort_flag, d_status);         // (the state that enters is there)
 #pragma unroll 1
         for (int t = 0; t < n_pre; ++t) {
             tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
-            add(t, t == n_pre - 1);
+            if (t > 1) tc::mbar_wait(&sm->d_free[t & 1], ((t >> 1) - 1) & 1, abort_flag, d_status);
+            add(t);
         }
-        if (ntiles > n_pre) scores(n_pre);
+        if (ntiles > n_pre) {                // (scores and o come where D stood)
+            for (int t = max(0, n_pre - 2); t < n_pre; ++t) tc::mbar_wait(&sm->d_free[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            scores(n_pre);
+        }
 #pragma unroll 1
         for (int t = n_pre; t < ntiles; ++t) {
             const int f = t - n_pre;
@@ -287,8 +298,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::mma_commit(&sm->free_q[f % NQ]);
             }
             __syncwarp();
-            tc::mbar_wait(&sm->s_scaled, (f + pre) & 1, abort_flag, d_status);
-            add(t, true);
+            tc::mbar_wait(&sm->s_scaled, f & 1, abort_flag, d_status);
+            add(t);
             // PV, on top of the scaled carried part (and behind KV: by then w V has been made of all of V, where o is staged)
             tc::mbar_wait(&sm->full_v[t % NV], (t / NV) & 1, abort_flag, d_status);
             tc::mbar_wait(&sm->p_full, f & 1, abort_flag, d_status);
@@ -309,10 +320,49 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 scores(t + 1);
             }
         }
-    } else if (warp >= WARP_MASK && warp < WARP_W) {
+    } else if (STATE_ONLY && ((warp >= WARP_MASK && warp < WARP_W) || warp >= WARP_O)) {
+        // ------------------------------------------------------------------ the state alone, a quarter of a value's row per
+        // thread: every tile's additions by themselves, and added up here, where sums are rounded, not cut
+        constexpr int NC = DK / 4;
+        const int q4 = warp & 3, i = q4 * 32 + lane, c0 = (warp < WARP_W ? (warp - WARP_MASK) >> 2 : 2 + ((warp - WARP_O) >> 2)) * NC;
+        const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + c0;
+        uint64_t st[NC / 2];
+#pragma unroll
+        for (int e = 0; e < NC / 2; ++e) st[e] = 0ull;
+        for (int t = 0; t < ntiles; ++t) {
+            tc::mbar_wait(&sm->d_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < NC; c += 16) {
+                uint32_t x[16];
+                tc::tmem_ld16(row + d_of(t) + c, x);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    st[c / 2 + e] = tc::f32x2_add(st[c / 2 + e], tc::f32x2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])));
+            }
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sm->d_free[t & 1]);
+        }
+        const int64_t ssize = (int64_t)j.dk * j.dv, step = j.transposed ? j.dv : 1;
+        float *to = j.seg + (((int64_t)b * a.H + h) * nall + seg + 1) * ssize + (j.transposed ? c0 * step + i : (int64_t)i * j.dk + c0);
+        const int nd = i < j.dv ? j.dk - c0 : 0;                 // entries of this thread's that the state has (in eights)
+#pragma unroll
+        for (int e = 0; e < NC; e += 2) {
+            if ((e & ~7) >= nd) continue;
+            const float2 v = tc::f32x2_get(st[e / 2]);
+            to[e * step] = v.x;
+            to[(e + 1) * step] = v.y;
+        }
+    } else if (!STATE_ONLY && warp >= WARP_MASK && warp < WARP_W) {
         // ------------------------------------------------------------------ masks: half a row of the scores per thread, its
         // result over the first half of what it was made from; and the state, half a value's row per thread: between two
-        // tiles its bf16 copy for QS goes to shared memory and it is scaled where it stands
+        // tiles its bf16 copy for QS goes to shared memory and it is scaled where it stands.
+        // The accumulators of the products cut where other sums round.  S, with 24 products a tile added to it, would lose up to
+        // 2^-23 of all it holds with each, always towards zero (2.5e-5 of a state of 64 tiles).  Where the state is a result, what
+        // the copy holds is therefore taken out of S until the tile's products are in: they add up beside what a tile forgets
+        // of it and 2^-9 (5e-7, whatever the memory).  Heads that forget more than half of it in a tile have no use for that.
         const int q4 = warp & 3, half = (warp - WARP_MASK) >> 2, i = q4 * 32 + lane;
         const uint32_t quarter = tmem + ((uint32_t)(q4 * 32) << 16), row = quarter + TM_QK + half * 64;
         const float scale_p = j.scale_p;
@@ -322,11 +372,11 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         const int64_t bh = (int64_t)b * a.H + h, ssize = (int64_t)j.dk * j.dv;
         const int64_t step = j.transposed ? j.dv : 1, at0 = j.transposed ? half * NC * step + i : (int64_t)i * j.dk + half * NC;
         const int nd = i < j.dv ? j.dk - half * NC : 0;          // entries of this thread's that the state has (in eights)
-        if (!STATE_ONLY) {                       // the state that enters
+        if (n_pre < ntiles) {                    // the state that enters
             const float *from = seg > 0  ? j.seg + (bh * a.nseg + seg) * a.per * ssize
                                 : j.s_in ? j.s_in + bh * ssize
                                          : nullptr;
-            const float dec = pre ? exp2f(tokens_left(-1) * g2) : 1.f;
+            const float dec = n_pre > 0 ? exp2f(tokens_left(-1) * g2) : 1.f;
 #pragma unroll 1
             for (int c = 0; c < NC; c += 16) {
                 uint32_t x[16];
@@ -336,16 +386,38 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 tc::tmem_st16(srow + c, x);
             }
             tc::tmem_st_wait();
-            if (pre) {
+            // and what the tiles in front add to it, as it is in front of the first tile that this CTA gives outputs of
+            for (int t = 0; t < n_pre; ++t) {
+                tc::mbar_wait(&sm->d_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
+                tc::tc_fence_after();
+                const uint32_t d = quarter + d_of(t) + half * NC;
+#pragma unroll 1
+                for (int c = 0; c < NC; c += 16) {
+                    uint32_t x[16], y[16];
+                    tc::tmem_ld16(srow + c, x);
+                    tc::tmem_ld16(d + c, y);
+                    tc::tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(y[e]));
+                    tc::tmem_st16(srow + c, x);
+                }
+                tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&sm->s_scaled);
-                tc::mbar_wait(&sm->kv_done, 0, abort_flag, d_status);
-                tc::tc_fence_after();
+                if (lane == 0) tc::mbar_arrive(&sm->d_free[t & 1]);
             }
         }
+        const bool take = parts == 3 && sm->pow[LT] >= 0.5f;
         uint8_t *copy = smem + L::S + i * 128 + (DK == 128 ? half * SLAB : 0);       // (its chunks of 16 bytes are swizzled by the row)
-        const int chunk0 = DK == 128 ? 0 : half * 4;
+        auto copy_of = [&](int c) { return reinterpret_cast<uint4 *>(copy + ((((DK == 128 ? 0 : half * 4) + (c >> 3)) ^ (i & 7)) * 16)); };
+        auto put_back = [](uint32_t *v, const uint4 &c) {            // eight entries and what their copy holds of them
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __float_as_uint(__uint_as_float(v[2 * e]) + low_half(w[e]));
+                v[2 * e + 1] = __float_as_uint(__uint_as_float(v[2 * e + 1]) + high_half(w[e]));
+            }
+        };
         // the state that enters tile t; the copy first: QS runs while the state is scaled for KV to add to
         auto hand_over = [&](int t) {
             const float dec = sm->pow[tile_n(t)];
@@ -364,10 +436,21 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                         if (pass == 0) {
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const uint32_t *v = r + 8 * e;
-                                *reinterpret_cast<uint4 *>(copy + (((chunk0 + (cz >> 3) + e) ^ (i & 7)) * 16)) = make_uint4(
-                                    bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
+                                uint32_t *v = r + 8 * e;
+                                uint4 *at = copy_of(cz + 8 * e);
+                                if (take && t > n_pre) put_back(v, *at);
+                                *at = make_uint4(bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
                             }
+                            if (take && t > n_pre) tc::tmem_st16(srow + cz, r);
+                        } else if (take) {
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                const uint32_t c2 = bits2(r[e], r[e + 1]);
+                                const float s0 = __uint_as_float(r[e]), s1 = __uint_as_float(r[e + 1]);
+                                r[e] = __float_as_uint(fmaf(dec, s0, -low_half(c2)));
+                                r[e + 1] = __float_as_uint(fmaf(dec, s1, -high_half(c2)));
+                            }
+                            tc::tmem_st16(srow + cz, r);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
@@ -376,8 +459,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     }
                 }
                 tc::tmem_ld_wait();
+                tc::tmem_st_wait();
                 if (pass == 0) tc::fence_proxy_async_smem();
-                else tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(pass == 0 ? &sm->s_full : &sm->s_scaled);
@@ -424,28 +507,29 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->p_full);
             if (t + 1 < ntiles) {
-                tc::mbar_wait(&sm->kv_done, (f + pre) & 1, abort_flag, d_status);
+                tc::mbar_wait(&sm->kv_done, f & 1, abort_flag, d_status);
                 tc::mbar_wait(&sm->qs_done, f & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 hand_over(t + 1);
             }
         }
-        float *to = STATE_ONLY ? j.seg + (bh * nall + seg + 1) * ssize
-                    : seg == a.nseg - 1 && part == nparts - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
-        if (to) {
-            if (ntiles > 0) {
-                tc::mbar_wait(&sm->kv_done, STATE_ONLY ? 0 : (ntiles - n_pre - 1 + pre) & 1, abort_flag, d_status);
-                tc::tc_fence_after();
-            }
+        float *to = seg == a.nseg - 1 && part == nparts - 1 && j.s_out ? j.s_out + bh * ssize : nullptr;
+        if (to) {                                // (what the copy holds of it is still there)
+            tc::mbar_wait(&sm->kv_done, (ntiles - n_pre - 1) & 1, abort_flag, d_status);
+            tc::tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < NC; c += 16) {
                 uint32_t x[16];
                 __syncwarp();
                 tc::tmem_ld16(srow + c, x);
                 tc::tmem_ld_wait();
+                if (take) {
+                    put_back(x, *copy_of(c));
+                    put_back(x + 8, *copy_of(c + 8));
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (c + (e & 8) < nd) to[at0 + (c + e) * step] = ntiles > 0 ? __uint_as_float(x[e]) : 0.f;
+                    if (c + (e & 8) < nd) to[at0 + (c + e) * step] = __uint_as_float(x[e]);
             }
         }
     } else if (warp >= WARP_W && warp < WARP_O) {
