@@ -58,6 +58,7 @@ struct Small {
     alignas(16) float pow_col[32];           // factors of a score block's columns
     float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
     float pow[LT + 1];                       // lambda^m
+    LaDecay whole[8];                        // lambda^LT (where the state is a result, in two floats), for each warp of the state
 };
 
 static_assert(offsetof(Small, pow_col) % 16 == 0 && Sm<64>::SMALL % 16 == 0 && Sm<128>::SMALL % 16 == 0, "read in fours");
@@ -443,8 +444,8 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         // S <- dec S + D, the small parts of D first, so that S is rounded once a tile.  (The accumulators of the products cut
         // where this rounds: tiles that added up in D would lose 2^-24 of all they hold with each of eight products, always
         // towards zero: 1e-5 after 57 tiles of a head that forgets nothing.)
-        auto collect = [&](uint32_t from, float dec) {
-            const uint64_t dec2 = tc::f32x2(dec, dec);
+        auto collect = [&](uint32_t from, LaDecay dec) {
+            const uint64_t hi2 = tc::f32x2(dec.hi, dec.hi), lo2 = tc::f32x2(dec.lo, dec.lo);
 #pragma unroll
             for (int k = 0; k < NC; k += 8) {
                 uint32_t x[8], y[8], z[8];
@@ -458,17 +459,22 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
                     uint64_t d = pair_of(x[2 * e], x[2 * e + 1]);
                     if (parts == 3) d = tc::f32x2_add(d, pair_of(z[2 * e], z[2 * e + 1]));
                     d = tc::f32x2_add(d, pair_of(y[2 * e], y[2 * e + 1]));
-                    s = tc::f32x2_fma(dec2, s, d);
+                    if (!STATE_ONLY && parts == 3) d = tc::f32x2_fma(lo2, s, d);
+                    s = tc::f32x2_fma(hi2, s, d);
                 }
             }
         };
+        if (!STATE_ONLY) {
+            if (lane == 0) sm->whole[warp - WARP_STATE] = parts == 3 ? la_decay(a.log_decay[h], LT) : LaDecay{sm->pow[LT], 0.f};
+            __syncwarp();
+        }
         for (int t = 0; t < (STATE_ONLY ? 0 : ntiles); ++t) {
             if (t > 0) tc::mbar_wait(&sm->qs_done, (t - 1) & 1, abort_flag, d_status);
             publish();
             const int n = tile_n(t);
             tc::mbar_wait(&sm->kv_done[1], t & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            collect(row + TM_KV, sm->pow[n]);
+            collect(row + TM_KV, n == LT ? sm->whole[warp - WARP_STATE] : LaDecay{sm->pow[n], 0.f});
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->kv_read);
@@ -476,7 +482,7 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         for (int t = 0; t < (STATE_ONLY ? ntiles : 0); ++t) {
             tc::mbar_wait(&sm->kv_done[vw_slot(t, 1)], vw_phase(t) & 1, abort_flag, d_status);
             tc::tc_fence_after();
-            collect(row + d_of(t), 1.f);
+            collect(row + d_of(t), LaDecay{1.f, 0.f});
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sm->d_free[t & 1]);

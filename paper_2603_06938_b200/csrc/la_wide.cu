@@ -47,6 +47,7 @@ struct Small {
     alignas(16) float pow_col[32];           // factors of a score block's columns
     float pow_diag[64];                      // scale_p lambda^|m - 31|: the block on the diagonal
     float pow[LT + 1];                       // lambda^m
+    LaDecay whole[8];                        // lambda^LT in two floats, for each warp of the state
     alignas(16) float weight[LT];            // of a whole tile's tokens in w V
     alignas(16) uint32_t wsplit[LT / 2][2];  // their bf16 parts, two tokens at a time
 };
@@ -407,7 +408,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 if (lane == 0) tc::mbar_arrive(&sm->d_free[t & 1]);
             }
         }
-        const bool take = parts == 3 && sm->pow[LT] >= 0.5f;
+        LaDecay &whole = sm->whole[warp - WARP_MASK];
+        if (lane == 0) whole = parts == 3 ? la_decay(a.log_decay[h], LT) : LaDecay{sm->pow[LT], 0.f};
+        __syncwarp();
+        const bool take = parts == 3 && whole.hi >= 0.5f;
         uint8_t *copy = smem + L::S + i * 128 + (DK == 128 ? half * SLAB : 0);       // (its chunks of 16 bytes are swizzled by the row)
         auto copy_of = [&](int c) { return reinterpret_cast<uint4 *>(copy + ((((DK == 128 ? 0 : half * 4) + (c >> 3)) ^ (i & 7)) * 16)); };
         auto put_back = [](uint32_t *v, const uint4 &c) {            // eight entries and what their copy holds of them
@@ -420,7 +424,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         };
         // the state that enters tile t; the copy first: QS runs while the state is scaled for KV to add to
         auto hand_over = [&](int t) {
-            const float dec = sm->pow[tile_n(t)];
+            const LaDecay dec = tile_n(t) == LT ? whole : LaDecay{sm->pow[tile_n(t)], 0.f};
             uint32_t x[2][16];
 #pragma unroll 1
             for (int pass = 0; pass < 2; ++pass) {
@@ -447,13 +451,13 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                             for (int e = 0; e < 16; e += 2) {
                                 const uint32_t c2 = bits2(r[e], r[e + 1]);
                                 const float s0 = __uint_as_float(r[e]), s1 = __uint_as_float(r[e + 1]);
-                                r[e] = __float_as_uint(fmaf(dec, s0, -low_half(c2)));
-                                r[e + 1] = __float_as_uint(fmaf(dec, s1, -high_half(c2)));
+                                r[e] = __float_as_uint(fmaf(dec.lo, s0, fmaf(dec.hi, s0, -low_half(c2))));
+                                r[e + 1] = __float_as_uint(fmaf(dec.lo, s1, fmaf(dec.hi, s1, -high_half(c2))));
                             }
                             tc::tmem_st16(srow + cz, r);
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
+                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec.hi * __uint_as_float(r[e]));
                             tc::tmem_st16(srow + cz, r);
                         }
                     }

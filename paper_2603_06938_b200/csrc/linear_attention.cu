@@ -322,10 +322,10 @@ la_chain_kernel(const __grid_constant__ LaArgs a)
     const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4;
     if (i >= ssize) return;
     const int h = (int)(blockIdx.y % a.H);
-    const double l2 = la_log2_decay(a.log_decay[h]);
+    const float log_decay = a.log_decay[h];
     // every piece but the sequence's last, the first of a walk backward, is whole (and behind the last there may be empty ones)
     const int len = a.seg_len / a.per, all = a.nseg * a.per, last = (a.nseg - 1) * a.per;
-    const float whole = (float)exp2(l2 * len);
+    const LaDecay whole = la_decay(log_decay, len);
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.s_in) s = *reinterpret_cast<const float4 *>(j.s_in + blockIdx.y * ssize + i);
     float *p = j.seg + (int64_t)blockIdx.y * all * ssize + i;
@@ -333,11 +333,11 @@ la_chain_kernel(const __grid_constant__ LaArgs a)
     for (int g = 1; g <= last; ++g) {
         const float4 l = *reinterpret_cast<const float4 *>(p + g * ssize);
         const int tokens = j.reverse ? a.L - (all - g) * len : len;        // of the piece in front
-        const float lam = tokens >= len ? whole : (float)exp2(l2 * max(0, tokens));
-        s.x = fmaf(lam, s.x, l.x);
-        s.y = fmaf(lam, s.y, l.y);
-        s.z = fmaf(lam, s.z, l.z);
-        s.w = fmaf(lam, s.w, l.w);
+        const LaDecay lam = tokens >= len ? whole : la_decay(log_decay, max(0, tokens));
+        s.x = fmaf(lam.hi, s.x, fmaf(lam.lo, s.x, l.x));
+        s.y = fmaf(lam.hi, s.y, fmaf(lam.lo, s.y, l.y));
+        s.z = fmaf(lam.hi, s.z, fmaf(lam.lo, s.z, l.z));
+        s.w = fmaf(lam.hi, s.w, fmaf(lam.lo, s.w, l.w));
         *reinterpret_cast<float4 *>(p + g * ssize) = s;
     }
 }

@@ -66,3 +66,22 @@ def test_states_of_slow_heads(B, L, H, N, P, tiles, g):
     want = torch.exp(decay.double())[:, None, None] * state(decay, q.flip(1), do.flip(1))
     worst = float(((ds.double() - want).abs() / want).max())
     assert worst <= bound(tiles), f"d state: {worst:.2e} of {bound(tiles):.2e}"
+
+
+@pytest.mark.parametrize("B,L,H,N,P", [(4, 16384, 37, 64, 64), (4, 16384, 37, 128, 128), (1, 65536, 2, 64, 64), (1, 65536, 3, 128, 128)])
+def test_the_decay_itself(B, L, H, N, P):
+    """A state that nothing is added to decays by lambda a token: over many entries the roundings of its products cancel, and
+    what is left is the error of the factor, multiplied up.  (128 tiles, each off by half of 2^-24 the same way: 2^-18.)"""
+    z = torch.zeros(B, L, H, max(N, P), dtype=torch.bfloat16, device="cuda")
+    assert N == P
+    s0 = 1 + torch.rand(B, H, P, N, generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    decay = torch.full((H,), -2.3e-5, device="cuda")
+    h = handle(H, N, P)
+    ws = workspace(h, B, L)
+    o, s = torch.empty_like(z), torch.empty_like(s0)
+    sb.swimba_linear_attention(h, decay, z, z, z, s0, B, L, 1.0, o, s, ws)
+    assert sb.swimba_status(h) == 0
+    # (the decay's exponent is rounded to 32 bits once: as many parts in 2^24 as lambda^L has e-folds)
+    want = torch.exp(decay.double() * L)[:, None, None] * s0.double()
+    mean = float(((s.double() - want) / want).mean())
+    assert abs(mean) <= U * (1 + 2.3e-5 * L), f"{mean:.2e}"
