@@ -186,7 +186,7 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict_
         float mu[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            mu[k] = s[k] * inv;
+            mu[k] = s[k] / width;            // (not times 1 / width: a row of equal entries has them as its mean)
             const uint64_t m2 = tc::f32x2(-mu[k], -mu[k]);
             uint64_t a2[2] = {0ull, 0ull};
 #pragma unroll
@@ -266,7 +266,7 @@ layer_norm_wide_kernel(const T *__restrict__ x, int64_t ldx, const float *__rest
         }
         float s[1] = {both(tc::f32x2_add(a2[0], a2[1]))};
         team_sum(s, team, red, turn);
-        const float mu = s[0] * inv;
+        const float mu = s[0] / width;       // (not times 1 / width: a row of equal entries has them as its mean)
         const uint64_t m2 = tc::f32x2(-mu, -mu);
         a2[0] = a2[1] = 0ull;
 #pragma unroll
@@ -387,9 +387,10 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, co
             const int lr = q * a.rpb + rslot;
             const int64_t r = ch * per + lr;
             const bool live = mine && r < a.rows;
-            const float rs = live ? rstd[r * a.groups + g0 + gl] : 0.f, mr = live ? -mean[r * a.groups + g0 + gl] * rs : 0.f;
+            // (x - mu, then times rstd: x rstd - mu rstd would leave a rounding of mu rstd where x is mu)
+            const float rs = live ? rstd[r * a.groups + g0 + gl] : 0.f, mu = live ? mean[r * a.groups + g0 + gl] : 0.f;
             const T *px = ring + st * stage + (int64_t)lr * seg + gl * a.width, *pd = px + (int64_t)per * seg;
-            const uint64_t rs2 = tc::f32x2(rs, rs), mr2 = tc::f32x2(mr, mr);
+            const uint64_t rs2 = tc::f32x2(rs, rs), m2 = tc::f32x2(-mu, -mu);
             uint64_t s0 = 0ull, s1 = 0ull;
             if (live) {
 #pragma unroll
@@ -402,7 +403,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, co
                     load_pairs(pw + c, w);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint64_t xh = tc::f32x2_fma(xv[e], rs2, mr2), z = tc::f32x2_mul(dv[e], w[e]);
+                        const uint64_t xh = tc::f32x2_mul(tc::f32x2_add(xv[e], m2), rs2), z = tc::f32x2_mul(dv[e], w[e]);
                         s0 = tc::f32x2_add(s0, z);
                         s1 = tc::f32x2_fma(z, xh, s1);
                         aw[i][e] = tc::f32x2_fma(dv[e], xh, aw[i][e]);
@@ -427,7 +428,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, co
                     load_pairs(pw + c, w);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        o[e] = tc::f32x2_fma(tc::f32x2_mul(dv[e], w[e]), rs2, tc::f32x2_fma(tc::f32x2_fma(xv[e], rs2, mr2), c12, c02));
+                        o[e] = tc::f32x2_fma(tc::f32x2_mul(dv[e], w[e]), rs2, tc::f32x2_fma(tc::f32x2_mul(tc::f32x2_add(xv[e], m2), rs2), c12, c02));
                     put8(dx + r * a.D + (int64_t)(g0 + gl) * a.width + c, o);
                 }
             }
