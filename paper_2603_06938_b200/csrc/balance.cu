@@ -323,8 +323,9 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
                 *reinterpret_cast<uint32_t *>(r1 + 16) = tc::pack_bf16x2(d1[2], d1[3]);
             }
         }
-        // (du, or zeros in the place of padding, were written by ordinary stores where bulk copies read and write next)
-        if (du || ok != 0xffffu) tc::fence_proxy_async_smem();
+        // du, or zeros in the place of padding, were written by ordinary stores where bulk copies read and write next.  (For
+        // every tile: to know here whether there was padding costs a register too many, 84 us instead of 81.)
+        tc::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&sm.done[s]);
     }
