@@ -146,7 +146,8 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
         int64_t it = 0;
         for (int64_t t = blockIdx.x; t < ntiles; t += gridDim.x, ++it) {
             const int s = (int)(it & 1);
-            tc::mbar_wait(&sm.done[s], (uint32_t)((it >> 1) & 1), &sm.abort_flag, d_status);
+            const bool done = tc::mbar_wait(&sm.done[s], (uint32_t)((it >> 1) & 1), &sm.abort_flag, d_status);
+            if (!__all_sync(0xffffffffu, done)) break;
             if (du && lane < BF_TOK && t * BF_TOK + lane < Tn) {
                 tc::bulk_store(du + (t * BF_TOK + lane) * F, sU + (s * BF_TOK + lane) * pitch, (uint32_t)(F * 2));
                 tc::bulk_commit_group();
@@ -155,6 +156,7 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
             __syncwarp();
             load(t + 2 * (int64_t)gridDim.x, s);
         }
+        tc::settle_copies(&sm.abort_flag);
         return;
     }
     // (from here on the warps that calculate)

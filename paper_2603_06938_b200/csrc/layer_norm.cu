@@ -349,7 +349,8 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, co
         const int64_t ch = blockIdx.x + i * gridDim.x;
         if (ch >= nchunks) return;
         const int s = (int)(i % a.stages);
-        tc::mbar_wait(&empty[s], (uint32_t)((i / a.stages) & 1) ^ 1, &abort_flag, d_status);
+        const bool room = tc::mbar_wait(&empty[s], (uint32_t)((i / a.stages) & 1) ^ 1, &abort_flag, d_status);
+        if (!__all_sync(0xffffffffu, room)) return;
         const int64_t r0 = ch * per;
         const int n = (int)min((int64_t)per, a.rows - r0);
         const uint32_t bytes = (uint32_t)(seg * sizeof(T));
@@ -436,6 +437,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, const T *__restrict__ x, co
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&empty[st]);
     }
+    tc::settle_copies(&abort_flag);
     if (!partial) return;
     // the rows of a block side by side: their sums meet in shared memory, in order (every stage that was filled has been
     // taken; what is left of the ring is room enough)

@@ -82,6 +82,14 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     }
 }
 
+// After a wait has run out: time (5 ms) for the copies that this thread block still has in flight, which nobody may have waited
+// for, to land before its shared memory goes to another.
+__device__ __forceinline__ void settle_copies(volatile int *abort_flag) {
+    if (!*abort_flag) return;
+    const long long t0 = clock64();
+    while (clock64() - t0 < 10000000ll) {}
+}
+
 // ---------------------------------------------------------------- proxies / async copies
 // Orders generic-proxy writes to shared memory before later async-proxy (TMA / tcgen05) reads.
 __device__ __forceinline__ void fence_proxy_async_smem() {
