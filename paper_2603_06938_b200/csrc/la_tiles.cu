@@ -444,21 +444,29 @@ la_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArg
         // S <- dec S + D, the small parts of D first, so that S is rounded once a tile.  (The accumulators of the products cut
         // where this rounds: tiles that added up in D would lose 2^-24 of all they hold with each of eight products, always
         // towards zero: 1e-5 after 57 tiles of a head that forgets nothing.)
+        constexpr int AT = DK == 128 ? 8 : 16;               // columns at a time (128 keys fill the registers with S)
+        auto load = [](uint32_t from, uint32_t (&r)[AT]) {
+            if constexpr (AT == 8) tc::tmem_ld8(from, r);
+            else tc::tmem_ld16(from, r);
+        };
         auto collect = [&](uint32_t from, LaDecay dec) {
             const uint64_t hi2 = tc::f32x2(dec.hi, dec.hi), lo2 = tc::f32x2(dec.lo, dec.lo);
 #pragma unroll
-            for (int k = 0; k < NC; k += 8) {
-                uint32_t x[8], y[8], z[8];
-                tc::tmem_ld8(from + LDV + k, x);
-                tc::tmem_ld8(from + k, y);
-                if (parts == 3) tc::tmem_ld8(from + 2 * LDV + k, z);
+            for (int k = 0; k < NC; k += AT) {
+                uint32_t x[AT], y[AT];
+                load(from + LDV + k, x);
+                if (parts == 3) {
+                    load(from + 2 * LDV + k, y);
+                    tc::tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < AT; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(y[e]));
+                }
+                load(from + k, y);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < AT / 2; ++e) {
                     uint64_t &s = st[k / 2 + e];
-                    uint64_t d = pair_of(x[2 * e], x[2 * e + 1]);
-                    if (parts == 3) d = tc::f32x2_add(d, pair_of(z[2 * e], z[2 * e + 1]));
-                    d = tc::f32x2_add(d, pair_of(y[2 * e], y[2 * e + 1]));
+                    uint64_t d = tc::f32x2_add(pair_of(x[2 * e], x[2 * e + 1]), pair_of(y[2 * e], y[2 * e + 1]));
                     if (!STATE_ONLY && parts == 3) d = tc::f32x2_fma(lo2, s, d);
                     s = tc::f32x2_fma(hi2, s, d);
                 }

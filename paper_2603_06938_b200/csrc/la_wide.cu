@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstddef>
+#include <type_traits>
 
 #include "la.h"
 #include "tc05.cuh"
@@ -104,7 +105,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
     // this CTA's tiles: those in front of n_pre only carry the state; barriers that the others alone use count from there
     const int n_pre = STATE_ONLY ? nwalk : nparts > 1 ? a.cut[part] : 0;
     const int ntiles = STATE_ONLY || nparts == 1 ? nwalk : a.cut[part + 1];
-    // D, of two such tiles in turn where scores and o will be
+    // where only the read of the state is (bf16) those tiles add up in S; else in D, of two tiles in turn where scores and o will be
+    const bool apart = parts == 3;
     auto d_of = [](int t) { return t & 1 ? TM_O : TM_QK; };
     // tokens walked behind tile t in front of tile n_pre; tile -1: all of them
     auto tokens_left = [&](int t) {
@@ -246,10 +248,8 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             __syncwarp();
         };
-        // KV, by quarters of the tile: onto S; of a tile that only carries the state, into D
-        auto add = [&](int t) {
-            const bool alone = t < n_pre;
-            const uint32_t to = tm + (alone ? d_of(t) : TM_S);
+        // KV, by quarters of the tile, onto S or (fresh) into D; done: the barrier behind it
+        auto add = [&](int t, auto fresh, uint32_t to, uint64_t *done) {
 #pragma unroll 1
             for (int qd = 0; qd < 4; ++qd) {
                 const int buf = qd & (ring - 1);
@@ -259,12 +259,12 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                     uint64_t k = tc::smem_desc_fresh(tc::smem_desc_advance(dKt, t % NK * L::QB + qd * 4096));
 #pragma unroll 1
                     for (int p = 0; p < parts; ++p) {
-                        tc::mma_ts(to, tm + TM_VW + (buf * parts + p) * 16, k, id_kv, !alone || qd + p > 0);
+                        tc::mma_ts(to, tm + TM_VW + (buf * parts + p) * 16, k, id_kv, !decltype(fresh)::value || qd + p > 0);
                         tc::mma_ts(to, tm + TM_VW + (buf * parts + p) * 16 + 8, tc::smem_desc_advance(k, 2048), id_kv, 1);
                     }
                     tc::mma_commit(&sm->vw_done[buf]);
                     if (qd == 3) {
-                        tc::mma_commit(alone ? &sm->d_full[t & 1] : &sm->kv_done);
+                        if (done) tc::mma_commit(done);
                         tc::mma_commit(&sm->free_k[t % NK]);
                     }
                 }
@@ -274,11 +274,18 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
 #pragma unroll 1
         for (int t = 0; t < n_pre; ++t) {
             tc::mbar_wait(&sm->full_k[t % NK], (t / NK) & 1, abort_flag, d_status);
-            if (t > 1) tc::mbar_wait(&sm->d_free[t & 1], ((t >> 1) - 1) & 1, abort_flag, d_status);
-            add(t);
+            if (apart) {                     // (what stood in D has been added)
+                if (t > 1) tc::mbar_wait(&sm->d_free[t & 1], ((t >> 1) - 1) & 1, abort_flag, d_status);
+                add(t, std::true_type{}, tm + d_of(t), &sm->d_full[t & 1]);
+            } else {                         // (the state that enters is in S; of the states alone the first tile clears it)
+                if (!STATE_ONLY && t == 0) tc::mbar_wait(&sm->d_free[0], 0, abort_flag, d_status);
+                uint64_t *done = t == n_pre - 1 ? &sm->d_full[0] : nullptr;
+                if (STATE_ONLY && t == 0) add(t, std::true_type{}, tm + TM_S, done);
+                else add(t, std::false_type{}, tm + TM_S, done);
+            }
         }
         if (ntiles > n_pre) {                // (scores and o come where D stood)
-            for (int t = max(0, n_pre - 2); t < n_pre; ++t) tc::mbar_wait(&sm->d_free[t & 1], (t >> 1) & 1, abort_flag, d_status);
+            for (int t = apart ? max(0, n_pre - 2) : n_pre; t < n_pre; ++t) tc::mbar_wait(&sm->d_free[t & 1], (t >> 1) & 1, abort_flag, d_status);
             scores(n_pre);
         }
 #pragma unroll 1
@@ -300,7 +307,7 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             __syncwarp();
             tc::mbar_wait(&sm->s_scaled, f & 1, abort_flag, d_status);
-            add(t);
+            add(t, std::false_type{}, tm + TM_S, &sm->kv_done);
             // PV, on top of the scaled carried part (and behind KV: by then w V has been made of all of V, where o is staged)
             tc::mbar_wait(&sm->full_v[t % NV], (t / NV) & 1, abort_flag, d_status);
             tc::mbar_wait(&sm->p_full, f & 1, abort_flag, d_status);
@@ -323,20 +330,20 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
         }
     } else if (STATE_ONLY && ((warp >= WARP_MASK && warp < WARP_W) || warp >= WARP_O)) {
         // ------------------------------------------------------------------ the state alone, a quarter of a value's row per
-        // thread: every tile's additions by themselves, and added up here, where sums are rounded, not cut
+        // thread: where it is a result, every tile's additions by themselves, and added up here, where sums are rounded, not cut
         constexpr int NC = DK / 4;
         const int q4 = warp & 3, i = q4 * 32 + lane, c0 = (warp < WARP_W ? (warp - WARP_MASK) >> 2 : 2 + ((warp - WARP_O) >> 2)) * NC;
         const uint32_t row = tmem + ((uint32_t)(q4 * 32) << 16) + c0;
         uint64_t st[NC / 2];
 #pragma unroll
         for (int e = 0; e < NC / 2; ++e) st[e] = 0ull;
-        for (int t = 0; t < ntiles; ++t) {
+        for (int t = 0; t < (apart ? ntiles : min(ntiles, 1)); ++t) {
             tc::mbar_wait(&sm->d_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
             tc::tc_fence_after();
 #pragma unroll
             for (int c = 0; c < NC; c += 16) {
                 uint32_t x[16];
-                tc::tmem_ld16(row + d_of(t) + c, x);
+                tc::tmem_ld16(row + (apart ? d_of(t) : TM_S) + c, x);
                 tc::tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -388,7 +395,14 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
             }
             tc::tmem_st_wait();
             // and what the tiles in front add to it, as it is in front of the first tile that this CTA gives outputs of
-            for (int t = 0; t < n_pre; ++t) {
+            if (!apart && n_pre > 0) {
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sm->d_free[0]);
+                tc::mbar_wait(&sm->d_full[0], 0, abort_flag, d_status);
+                tc::tc_fence_after();
+            }
+            for (int t = 0; t < (apart ? n_pre : 0); ++t) {
                 tc::mbar_wait(&sm->d_full[t & 1], (t >> 1) & 1, abort_flag, d_status);
                 tc::tc_fence_after();
                 const uint32_t d = quarter + d_of(t) + half * NC;
@@ -408,10 +422,10 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 if (lane == 0) tc::mbar_arrive(&sm->d_free[t & 1]);
             }
         }
+        const bool take = parts == 3 && sm->pow[LT] >= 0.5f;
         LaDecay &whole = sm->whole[warp - WARP_MASK];
-        if (lane == 0) whole = parts == 3 ? la_decay(a.log_decay[h], LT) : LaDecay{sm->pow[LT], 0.f};
+        if (take && lane == 0) whole = la_decay(a.log_decay[h], LT);
         __syncwarp();
-        const bool take = parts == 3 && whole.hi >= 0.5f;
         uint8_t *copy = smem + L::S + i * 128 + (DK == 128 ? half * SLAB : 0);       // (its chunks of 16 bytes are swizzled by the row)
         auto copy_of = [&](int c) { return reinterpret_cast<uint4 *>(copy + ((((DK == 128 ? 0 : half * 4) + (c >> 3)) ^ (i & 7)) * 16)); };
         auto put_back = [](uint32_t *v, const uint4 &c) {            // eight entries and what their copy holds of them
@@ -422,52 +436,62 @@ la_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LaArgs
                 v[2 * e + 1] = __float_as_uint(__uint_as_float(v[2 * e + 1]) + high_half(w[e]));
             }
         };
+        // half a row of the state through f, 16 columns at a time; then the barrier of the pass, the copy's or the one for S
+        auto pass_over = [&](auto &&f, bool copy_pass) {
+            uint32_t x[2][16];
+            tc::tmem_ld16(srow, x[0]);
+#pragma unroll 1
+            for (int c = 0; c < NC; c += 32) {
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const int cz = c + z * 16;
+                    tc::tmem_ld_wait();
+                    tc::tmem_ld16(srow + (cz + 16) % NC, x[z ^ 1]);    // (behind the last: the first once more, unused)
+                    f(cz, x[z]);
+                }
+            }
+            tc::tmem_ld_wait();
+            tc::tmem_st_wait();
+            if (copy_pass) tc::fence_proxy_async_smem();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(copy_pass ? &sm->s_full : &sm->s_scaled);
+        };
+        auto put_copy = [&](int c, const uint32_t (&r)[16]) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 8)
+                *copy_of(c + e) = make_uint4(bits2(r[e], r[e + 1]), bits2(r[e + 2], r[e + 3]), bits2(r[e + 4], r[e + 5]), bits2(r[e + 6], r[e + 7]));
+        };
         // the state that enters tile t; the copy first: QS runs while the state is scaled for KV to add to
         auto hand_over = [&](int t) {
-            const LaDecay dec = tile_n(t) == LT ? whole : LaDecay{sm->pow[tile_n(t)], 0.f};
-            uint32_t x[2][16];
-#pragma unroll 1
-            for (int pass = 0; pass < 2; ++pass) {
-                tc::tmem_ld16(srow, x[0]);
-#pragma unroll 1
-                for (int c = 0; c < NC; c += 32) {
+            if (!take) {
+                const float dec = sm->pow[tile_n(t)];
+                pass_over([&](int c, uint32_t (&r)[16]) { put_copy(c, r); }, true);
+                pass_over([&](int c, uint32_t (&r)[16]) {
 #pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const int cz = c + z * 16;
-                        uint32_t (&r)[16] = x[z];
-                        tc::tmem_ld_wait();
-                        tc::tmem_ld16(srow + (cz + 16) % NC, x[z ^ 1]);    // (behind the last: the first once more, unused)
-                        if (pass == 0) {
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                uint32_t *v = r + 8 * e;
-                                uint4 *at = copy_of(cz + 8 * e);
-                                if (take && t > n_pre) put_back(v, *at);
-                                *at = make_uint4(bits2(v[0], v[1]), bits2(v[2], v[3]), bits2(v[4], v[5]), bits2(v[6], v[7]));
-                            }
-                            if (take && t > n_pre) tc::tmem_st16(srow + cz, r);
-                        } else if (take) {
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const uint32_t c2 = bits2(r[e], r[e + 1]);
-                                const float s0 = __uint_as_float(r[e]), s1 = __uint_as_float(r[e + 1]);
-                                r[e] = __float_as_uint(fmaf(dec.lo, s0, fmaf(dec.hi, s0, -low_half(c2))));
-                                r[e + 1] = __float_as_uint(fmaf(dec.lo, s1, fmaf(dec.hi, s1, -high_half(c2))));
-                            }
-                            tc::tmem_st16(srow + cz, r);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec.hi * __uint_as_float(r[e]));
-                            tc::tmem_st16(srow + cz, r);
-                        }
+                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(dec * __uint_as_float(r[e]));
+                    tc::tmem_st16(srow + c, r);
+                }, false);
+            } else {
+                const LaDecay dec = tile_n(t) == LT ? whole : LaDecay{sm->pow[tile_n(t)], 0.f};
+                pass_over([&](int c, uint32_t (&r)[16]) {
+                    if (t > n_pre) {
+                        put_back(r, *copy_of(c));
+                        put_back(r + 8, *copy_of(c + 8));
+                        tc::tmem_st16(srow + c, r);
                     }
-                }
-                tc::tmem_ld_wait();
-                tc::tmem_st_wait();
-                if (pass == 0) tc::fence_proxy_async_smem();
-                tc::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(pass == 0 ? &sm->s_full : &sm->s_scaled);
+                    put_copy(c, r);
+                }, true);
+                pass_over([&](int c, uint32_t (&r)[16]) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        const uint32_t c2 = bits2(r[e], r[e + 1]);
+                        const float s0 = __uint_as_float(r[e]), s1 = __uint_as_float(r[e + 1]);
+                        r[e] = __float_as_uint(fmaf(dec.lo, s0, fmaf(dec.hi, s0, -low_half(c2))));
+                        r[e + 1] = __float_as_uint(fmaf(dec.lo, s1, fmaf(dec.hi, s1, -high_half(c2))));
+                    }
+                    tc::tmem_st16(srow + c, r);
+                }, false);
             }
         };
         if (ntiles > n_pre) hand_over(n_pre);

@@ -68,6 +68,7 @@ def run_wide(n, nq, state_only, rng):
     ring = rng.choice([2, 4])                             # quarters of w V there is room for
     need.update({f"vw_{k}{i}": 1 for i in range(ring) for k in ("full", "done")})
     need.update({f"d_full{i}": 1 for i in range(2)} | {f"d_free{i}": 2 if state_only else 1 for i in range(2)})
+    apart = rng.random() < 0.5                            # (the state is a result)
     bars, buf = Bars(need), Buffers()
     odd = lambda t: t >= n_pre and t % 3 == 1
     async_ops = []
@@ -104,12 +105,15 @@ def run_wide(n, nq, state_only, rng):
                 def ready(t=t, qd=qd):
                     buf.read(f"vw{qd % ring}", 4 * t + qd)
                     bars.arrive(f"vw_done{qd % ring}")
-                    if qd == 0 and t < n_pre:             # (the first product of a tile clears D)
+                    if qd == 0 and t == 0 < n_pre and not apart and not state_only:
+                        buf.read("s_entry", 0)
+                    if qd == 0 and t < n_pre and apart:   # (the first product of a tile clears D)
                         buf.write(region(t), ("d", t), 2 if state_only else 1)
                     if qd == 3:
                         buf.read(slot("k", t), t)
                         if t < n_pre:
-                            bars.arrive(f"d_full{t & 1}")
+                            if apart or t == n_pre - 1:
+                                bars.arrive(f"d_full{t & 1 if apart else 0}")
                         else:
                             buf.read("s_scaled", t)
                             buf.write("s", t + 1, 1)
@@ -118,11 +122,11 @@ def run_wide(n, nq, state_only, rng):
                 queue.append(ready)
         for t in range(n_pre):
             yield f"full_{slot('k', t)}", t // ns["k"]
-            if t > 1:
-                yield f"d_free{t & 1}", (t >> 1) - 1
+            if t > 1 if apart else t == 0 and not state_only:
+                yield f"d_free{t & 1}", (t >> 1) - 1 if apart else 0
             yield from add(t)
         if n > n_pre:
-            for t in range(max(0, n_pre - 2), n_pre):
+            for t in range(max(0, n_pre - 2) if apart else n_pre, n_pre):
                 yield f"d_free{t & 1}", t >> 1
             yield from scores(n_pre)
         for t in range(n_pre, n):
@@ -156,7 +160,13 @@ def run_wide(n, nq, state_only, rng):
             buf.write("s_scaled", t, 1)
             yield None
             bars.arrive("s_scaled")
-        for t in range(n_pre):
+        if not apart and n_pre:                           # the state that enters is there; tiles add to it in place
+            if not state_only:
+                buf.write("s_entry", 0, 1)
+                yield None
+                bars.arrive("d_free0")
+            yield "d_full0", 0
+        for t in range(n_pre if apart else 0):
             yield f"d_full{t & 1}", t >> 1
             buf.read(region(t), ("d", t))
             yield None
@@ -223,7 +233,7 @@ def run_wide(n, nq, state_only, rng):
 @pytest.mark.parametrize("n", [1, 2, 3, 4, 7, 20])
 def test_every_wait_ends_and_no_buffer_is_lost(n, ns, state_only):
     rng = random.Random(n * 10 + ns)
-    for _ in range(150):
+    for _ in range(250):
         run_wide(n, ns - 1, state_only, rng)
         if state_only:
             run_states(n, ns, rng)
