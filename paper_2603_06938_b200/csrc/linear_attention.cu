@@ -463,11 +463,11 @@ la_step_kernel(const float *__restrict__ log_decay, const T *__restrict__ q, int
 
 template <typename T, int LR>
 void run_step(LaunchCtx &ctx, const float *log_decay, const void *q, int64_t ldq, const void *k, int64_t ldk,
-              const void *v, int64_t ldv, const float *s_in, int B, int H, int G, int P, int N, float scale, void *o,
-              float *s_out)
+              const void *v, int64_t ldv, const float *s_in, int B, int H, int G, int P, int N, float scale,
+              int sm_count, void *o, float *s_out)
 {
     const int64_t nwork = (int64_t)B * H * ceil_div(P, ST_ROWS);
-    const int threads = nwork * LR >= 148 * 256 ? 256 : 64;     // (few rows: spread over the SMs)
+    const int threads = nwork * LR >= sm_count * 256 ? 256 : 64;     // (few rows: spread over the SMs)
     launch_kernel(la_step_kernel<T, LR>, dim3((unsigned)ceil_div64(nwork * LR, threads)), dim3(threads), 0, ctx.stream,
                   true, log_decay, (const T *)q, ldq, (const T *)k, ldk, (const T *)v, ldv, s_in, nwork, H, G, P, N,
                   scale, (T *)o, s_out);
@@ -475,14 +475,14 @@ void run_step(LaunchCtx &ctx, const float *log_decay, const void *q, int64_t ldq
 
 template <typename T>
 void run_step_n(LaunchCtx &ctx, const float *log_decay, const void *q, int64_t ldq, const void *k, int64_t ldk,
-                const void *v, int64_t ldv, const float *s_in, int B, int H, int G, int P, int N, float scale, void *o,
-                float *s_out)
+                const void *v, int64_t ldv, const float *s_in, int B, int H, int G, int P, int N, float scale,
+                int sm_count, void *o, float *s_out)
 {
     // lanes per row: no more than the row has groups of four entries
-    if (N >= 128) run_step<T, 32>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, o, s_out);
-    else if (N >= 64) run_step<T, 16>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, o, s_out);
-    else if (N >= 32) run_step<T, 8>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, o, s_out);
-    else run_step<T, 4>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, o, s_out);
+    if (N >= 128) run_step<T, 32>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, sm_count, o, s_out);
+    else if (N >= 64) run_step<T, 16>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, sm_count, o, s_out);
+    else if (N >= 32) run_step<T, 8>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, sm_count, o, s_out);
+    else run_step<T, 4>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, sm_count, o, s_out);
 }
 
 }  // namespace
@@ -592,12 +592,11 @@ int launch_la_step(LaunchCtx &ctx, int dtype, const float *log_decay, const void
                    int64_t ldk, const void *v, int64_t ldv, const float *s_in, int B, int H, int G, int P, int N,
                    float scale, int sm_count, void *o, float *s_out)
 {
-    (void)sm_count;
     ctx.begin(STAGE_LA_STEP);
     if (dtype == SWIMBA_DTYPE_FP32)
-        run_step_n<float>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, o, s_out);
+        run_step_n<float>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, sm_count, o, s_out);
     else
-        run_step_n<__nv_bfloat16>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, o, s_out);
+        run_step_n<__nv_bfloat16>(ctx, log_decay, q, ldq, k, ldk, v, ldv, s_in, B, H, G, P, N, scale, sm_count, o, s_out);
     ctx.end();
     return cudaGetLastError() == cudaSuccess ? SWIMBA_OK : SWIMBA_ERR_CUDA;
 }
