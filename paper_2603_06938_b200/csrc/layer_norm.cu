@@ -58,6 +58,15 @@ __device__ __forceinline__ float both(uint64_t v)
     return f.x + f.y;
 }
 
+// s / width from 1 / width, with what is left of s put right (one Newton step): a row of equal entries has them as its mean, to
+// the bit, where the product alone is off by 2^-24.  (A division takes registers enough to change how many blocks an SM
+// holds: 32768 x 2048 forward 50 us instead of 46.)
+__device__ __forceinline__ float ln_mean(float s, int width, float inv)
+{
+    const float m = s * inv;
+    return fmaf(fmaf(-m, (float)width, s), inv, m);
+}
+
 // Weights in shared memory: of every eight the first four, then the second four of all, so that threads side by side read side
 // by side (in place, 32 bytes a thread, half of every wavefront goes unused).
 __device__ __forceinline__ void stage_weights(float *to, const float *from, float none, int n)
@@ -186,7 +195,7 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, const float *__restrict_
         float mu[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            mu[k] = s[k] / width;            // (not times 1 / width: a row of equal entries has them as its mean)
+            mu[k] = ln_mean(s[k], width, inv);
             const uint64_t m2 = tc::f32x2(-mu[k], -mu[k]);
             uint64_t a2[2] = {0ull, 0ull};
 #pragma unroll
@@ -266,7 +275,7 @@ layer_norm_wide_kernel(const T *__restrict__ x, int64_t ldx, const float *__rest
         }
         float s[1] = {both(tc::f32x2_add(a2[0], a2[1]))};
         team_sum(s, team, red, turn);
-        const float mu = s[0] / width;       // (not times 1 / width: a row of equal entries has them as its mean)
+        const float mu = ln_mean(s[0], width, inv);
         const uint64_t m2 = tc::f32x2(-mu, -mu);
         a2[0] = a2[1] = 0ull;
 #pragma unroll
