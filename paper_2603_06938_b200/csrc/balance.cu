@@ -69,8 +69,8 @@ __device__ __forceinline__ float share_difference(int count, int valid, int k, i
 // dg enters the products as bf16 parts: three for dW, an fp32 result (2^-24 of it), two for du, which is bf16 itself.  With
 // up to eight experts the first two parts lie side by side, as the rows (dW) or the depth (du) of one product.
 // The work between two barriers is short and its latency counts: eight warps that also made the copies took 88 us for 32768
-// tokens, F = 2048, E = 8 (FMA kernels with u read twice: 284 us for the call).  Now the call takes 82 us (floor 41), counts
-// and sums included: 268 MB in the main pass, whose warps wait at its barriers more than for memory.
+// tokens, F = 2048, E = 8 (FMA kernels with u read twice: 284 us for the call).  Now the call takes 81 us (floor 41), counts
+// and sums included (E = 16: 108): 268 MB in the main pass, whose warps wait at its barriers more than for memory.
 // ------------------------------------------------------------------------------------------
 constexpr int BF_TOK = 16, BF_WARPS = 16, BF_NT = 16;      // tokens of a tile, warps, most n-tiles of 8 features a warp has
 constexpr int BF_MATH = BF_WARPS * 32, BF_THREADS = BF_MATH + 32;        // and one warp for the copies
@@ -356,7 +356,9 @@ balance_fused_kernel(const __nv_bfloat16 *__restrict__ u, const __nv_bfloat16 *_
 }
 
 // Any F % 8 == 0, E <= 64, both types: a warp per BL_TOKENS tokens; logits by FMA with the features across the
-// lanes, softmax with the experts across the lanes, then dg (kept for dW when asked) and du.
+// lanes, softmax with the experts across the lanes, then dg (kept for dW when asked) and du.  Bound by those FMAs and a second
+// read of u: the call, 32768 tokens, takes 459 us for bf16, F = 4096, E = 8 (floor 82), 839 for F = 2048, E = 32 (floor 41),
+// and 360 in fp32 for F = 2048, E = 8 (floor 82).
 template <typename T>
 __global__ void __launch_bounds__(256)
 balance_tokens_kernel(const T *__restrict__ u, const T *__restrict__ W, const uint8_t *__restrict__ valid, int64_t Tn,

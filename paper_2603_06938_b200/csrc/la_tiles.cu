@@ -11,9 +11,9 @@
 // rounded to bf16 (a term of o, which is bf16 itself, passes one of the two).  w V is not: it goes into the state and is
 // taken as the sum of bf16 parts, one product each: three where the state is a result (2^-24 of it), else two (2^-17).
 //
-// Measured, 65536 tokens of 16 heads of 64 x 64 (floor 82 us): cut into segments, the states alone 64 us (238 MB read, 3.7
+// Measured, 65536 tokens of 16 heads of 64 x 64 (floor 82 us): cut into segments, the states alone 65 us (238 MB read, 3.7
 // TB/s; their loads alone take 50, the rest is shared memory, 176 KB of reads and writes a tile against 128 bytes a cycle),
-// their chain 7, the outputs 111 (537 MB, 4.8 TB/s; the loads and stores without the making of w V 97).
+// their chain 7, the outputs 112 (537 MB, 4.8 TB/s; the loads and stores without the making of w V 97).
 //
 // A token's bits reach nobody in front of it: scores are masked by selection, and entries of V that are infinite or NaN,
 // which a zero of P would turn into NaN, are zeros in PV; the epilogue adds them to the rows that see them.

@@ -4,11 +4,12 @@
 //   w V   is made transposed, [DV, tokens], straight into tensor memory, a quarter of a tile at a time and two of them in
 //         turn, and is the A operand of KV:  D = (w V)^T K
 //   S     lies in tensor memory in fp32, [DV, DK]; between two tiles it is read, rounded for QS and scaled by lambda^n,
-//         and KV adds to it
+//         and KV adds to it (where the state is a result, without what the copy for QS holds of it)
 //   O     one region: Q S^T, scaled row by row in place, then P V on top
 // Shared memory bounds such a tile first: 7860 cycles of reads and writes for two CTAs of 64 values each against 3900 here;
 // the chain scores - masks - P V - o of a tile is not much shorter.  Measured, 4 sequences of 8192 tokens, 16 heads of
-// 128 x 128: 186 us (floor 82), 3.6 us a tile and CTA, 64 walks on 128 SMs; their gradients, 192 walks, 414 us (floor 144).
+// 128 x 128: 190 us (floor 82), 3.7 us a tile and CTA, 64 walks on 128 SMs; without an exit state 152, 3.0 us a tile; their
+// gradients, 192 walks, 428 us (floor 144).
 #include <algorithm>
 #include <cmath>
 #include <cstddef>
@@ -775,7 +776,8 @@ double la_cuts(int64_t items, int nt, int sm_count, LaArgs *a)
 {
     // Whole waves of walks first, what is left shared so that its CTAs end together: a tile that only carries the state takes
     // three quarters of the time of the others where the state is a result (w V in three parts), so each part is a quarter as
-    // long as the one in front (4 sequences of 8192, 16 heads: 186 us; 0.36 as long 190; whole walks 227, segments 192).
+    // long as the one in front (4 sequences of 8192, 16 heads: 195 us; 0.21 as long 214, 0.17 209; whole walks 279, two
+    // segments 210, four 259).
     constexpr double RATIO = 0.25;
     const int64_t whole = items / sm_count * sm_count, rest = items - whole;
     double best = (double)ceil_div64(items, sm_count) * nt;

@@ -7,8 +7,9 @@
 // Instruction issue bounds these kernels as soon as it can (2048 entries a row by 256 threads: 77 us forward, 154
 // backward of 32768 rows): few threads a row, so that the sums across threads are shared by many entries, arithmetic on pairs,
 // and places at distances known when compiling.  So that forward takes 47 us, 5.7 TB/s (a copy of the same bytes 45), with the
-// weights in shared memory (from the L1 cache, whose wavefronts they half fill, 61).  Backward takes 108 us, 3.7 TB/s, with
-// 45 % of the issue slots in use and two blocks an SM, whose warps wait for each other's sums and for shared memory.
+// weights in shared memory (from the L1 cache, whose wavefronts they half fill, 61).  Backward takes 111 us, 3.6 TB/s, with
+// 45 % of the issue slots in use and two blocks an SM, whose warps wait for each other's sums and for shared memory.  In fp32
+// 103 and 214 us (floors 82 and 123).
 #include <algorithm>
 #include <climits>
 

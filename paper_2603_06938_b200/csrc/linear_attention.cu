@@ -406,7 +406,8 @@ la_head_sum_kernel(const float *__restrict__ part, int64_t nout, int r, int N, T
 // One token for each of B sequences: S <- lambda S + v k^T (fp32, from s_in to s_out), o = scale S q.
 // A group of LR lanes owns ROWS rows of a head's state at a time, four entries of each row a lane, all of whose
 // loads are in flight before the first is used.  Bound by the state's bytes, read and written once: 128 sequences of 16 heads
-// of 128 x 128 take 53 us, 5.1 TB/s (a copy reaches 6.6); of one sequence, 12 us a call, it is the launch.
+// of 128 x 128 take 52 us, 5.2 TB/s (a copy reaches 6.6).  Of one sequence a call takes 12 us, half of them the Python binding's
+// checks of three strided tensors (the layer norm, one launch too, takes 6).
 constexpr int ST_ROWS = 8;
 template <typename T, int LR>
 __global__ void __launch_bounds__(256)
@@ -506,7 +507,9 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
     const int most = la_most(tiles, B, H, N, P, njobs, sm_count);
     if (!tiles) {
         // Waves of blocks times chunks, in chunks: the outputs, and, where sequences are cut, the pass for the states (half of
-        // that) and two more launches (about 6).
+        // that) and two more launches (about 6).  Measured (us): 1024 tokens of 16 heads of 16 x 64, whole 92, two segments 75,
+        // four 50, eight (chosen) 35; gradients of 2 x 1000 tokens of 16 heads of 128 x 128, whole (chosen) 557, two 522; of 256
+        // tokens of 8 heads of 16 x 64, whole (chosen) 32, two 32, four 24.
         const int64_t blocks = (int64_t)njobs * B * H * ceil_div(std::max(N, P), LA_COLS);
         double best = 1e30;
         for (int n = 1; n <= std::min(most, ceil_div(L, LA_STEP_SEG)); ++n) {
@@ -522,6 +525,10 @@ void la_plan(int dtype, int B, int L, int H, int N, int P, int njobs, int sm_cou
     }
     // Waves of CTAs times tiles per CTA, in tiles: the outputs, and, where sequences are cut, the pass for the states (about
     // 0.7 of a tile each, in pieces that fill the SMs), their chain (0.15 a piece) and two more launches (about 9).
+    // Measured (us), 16 heads of 64 x 64: 65536 tokens, whole 824, five segments 283, nine (chosen) 175, 18 204; 8192 tokens,
+    // whole 119, four 50, eight 38, nine 37, 16 46 (chosen: within 2 of the best); 2048 tokens, whole 32, four 23, eight
+    // (chosen) 20; 1024 tokens, whole (chosen) 19, two 20, four 19; 4 x 8192 tokens, whole 113, two (chosen) 90, four 110.
+    // 16 heads of 128 x 128, 8192 tokens: whole 258, shared walks 173, four segments 123, nine (chosen) 98.
     const int nt = ceil_div(L, LA_TILE_SEG);
     const int64_t items = (int64_t)njobs * B * H;
     const bool wide = P > 64 && (njobs == 1 || N > 64);

@@ -76,3 +76,13 @@ def test_captured_and_accumulated():
         # either side adds the same eight runs of partial sums n times: as many roundings of a running sum that stays
         # within n times the result and the magnitudes of one call's terms (and those twice over, for their own rounding)
         assert bool(((t["dW"] - n * want["dW"]).abs() <= 16 * n * 2.0 ** -24 * (n * want["dW"].abs() + 2 * mag)).all())
+
+
+def test_the_same_expert_twice():
+    """A token whose active set names an expert twice counts it twice, in either form of the counts."""
+    for T, F, E, k in ((500, 256, 8, 2), (9000, 256, 8, 2), (300, 264, 40, 3)):
+        u, W, idx, valid = bl.make("bf16", T, F, E, k, seed=T)
+        idx[:, 0] = idx[:, -1]
+        t, rc = bl.call(bl.handle("bf16", F, E, k), u.cuda(), W.cuda(), idx.cuda(), valid.cuda(), T, F, E)
+        assert rc == 0
+        bl.check(t, bl.reference(u, W, idx, valid, E, k), "bf16", T, F, E)
