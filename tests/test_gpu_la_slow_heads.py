@@ -85,3 +85,31 @@ def test_the_decay_itself(B, L, H, N, P):
     want = torch.exp(decay.double() * L)[:, None, None] * s0.double()
     mean = float(((s.double() - want) / want).mean())
     assert abs(mean) <= U * (1 + 2.3e-5 * L), f"{mean:.2e}"
+
+
+@pytest.mark.parametrize("t", [0, 37, 100, 126])
+@pytest.mark.parametrize("N,P", [(64, 64), (128, 64), (64, 128), (128, 128), (48, 80)])
+def test_one_term(N, P, t):
+    """A state that one token of a tile adds to is one product, weight times value times key.  Of it 18 parts in 2^24: the
+    weight's exponent, rounded twice, of less than 1 (1), exp2f twice (8), two products (2), three bf16 parts (1) and as
+    many additions that cut (6).  Two bf16 parts would leave up to 2^-17, 128 parts."""
+    B, L, H = 2, 128, 4
+    gen = torch.Generator("cuda").manual_seed(t)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)
+    q, k, v, do = (torch.zeros(B, L, H, n, dtype=torch.bfloat16, device="cuda") for n in (N, N, P, P))
+    for x in (q, k, v, do):
+        x[:, t] = r(*x[:, t].shape)
+    decay = torch.tensor([-0.004, -0.003, -0.002, -0.001], device="cuda")
+    scale = 0.37
+    h = handle(H, N, P)
+    ws = workspace(h, B, L)
+    o, s, ds = torch.empty_like(v), torch.empty(B, H, P, N, device="cuda"), torch.empty(B, H, P, N, device="cuda")
+    sb.swimba_linear_attention(h, decay, q, k, v, None, B, L, scale, o, s, ws)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    sb.swimba_linear_attention_backward(h, decay, q, k, v, None, do, None, B, L, scale, dq, dk, dv, ds, ws)
+    assert sb.swimba_status(h) == 0
+    lam = torch.exp(decay.double())[:, None, None]
+    one = lambda a, b: a[:, t, :, :, None].double() * b[:, t, :, None, :].double()
+    f32 = float(torch.tensor(scale))
+    for got, want in ((s, lam ** (L - 1 - t) * one(v, k)), (ds, f32 * lam ** (t + 1) * one(do, q))):
+        assert bool(((got.double() - want).abs() <= 18 * U * want.abs()).all()), float(((got.double() - want) / want).abs().max())
